@@ -79,7 +79,12 @@ enum {
     MOSAIC_BSA_ERR_WORKSPACE = -6, /* workspace missing or too small */
     MOSAIC_BSA_ERR_ALIGN = -7,     /* a tensor base pointer is not 16-byte aligned */
     MOSAIC_BSA_ERR_LAUNCH = -8,    /* HIP refused a launch (see hipGetLastError) */
-    MOSAIC_BSA_ERR_OP = -9         /* unknown op for mosaic_bsa_workspace_bytes */
+    MOSAIC_BSA_ERR_OP = -9,        /* unknown op for mosaic_bsa_workspace_bytes */
+    MOSAIC_BSA_ERR_ROTATION = -10, /* rotation: rotary_dim, axes, layout or scaling */
+    MOSAIC_BSA_ERR_STRIDE = -11,   /* a stride that is negative, too large, or 0 where
+                                      an output has more than one entry */
+    MOSAIC_BSA_ERR_WINDOW = -12    /* window: negative sinks, ring too small for the
+                                      window, or a ring in a backward pass */
 };
 
 enum { MOSAIC_BSA_F32 = 0, MOSAIC_BSA_BF16 = 1 };
@@ -283,6 +288,192 @@ int mosaic_bsa_bwd_three_branch(const mosaic_bsa_params *params, int32_t local_h
                                 const int32_t *sel_idx, const void *fwd_workspace,
                                 void *dq, void *dk, void *dv, float *dgates,
                                 void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * ---------------------------------------------------------------------------
+ * What sits next to the attention: the rotation of queries and keys by their
+ * positions, their norms, and attention inside a sliding window.
+ *
+ * Tensors of these entry points are [batch, heads, tokens, head_dim] with any
+ * strides of the first three dimensions (channels are consecutive), so that q, k
+ * and v may be parts of one projection's output [batch, tokens, heads, head_dim]
+ * and gradients may be written into such a tensor.  Everything else is as above:
+ * device pointers, caller-owned buffers, the caller's stream, checks on the host
+ * before anything is enqueued.
+ * ---------------------------------------------------------------------------
+ */
+/* Strides in elements.  token == 0: a contiguous [batch, heads, tokens, head_dim]
+ * tensor (batch and head are then ignored).  batch or head may be 0 in an input
+ * that is shared by all of them, never in an output that has more than one. */
+typedef struct {
+    int64_t batch, head, token;
+} mosaic_bsa_strides;
+
+enum { MOSAIC_BSA_ROTATE_HALVES = 0, MOSAIC_BSA_ROTATE_PAIRS = 1 };
+enum {
+    MOSAIC_BSA_SCALE_NONE = 0,
+    MOSAIC_BSA_SCALE_LINEAR = 1,   /* every frequency divided by factor */
+    MOSAIC_BSA_SCALE_BASE = 2,     /* theta * factor^(d / (d - 2)): the lowest frequency
+                                      divided by factor, the highest kept */
+    MOSAIC_BSA_SCALE_RAMP = 3      /* by parts (YaRN, Peng et al. 2023): with r = original_tokens
+                                      * frequency / 2 pi turns over the trained length,
+                                      frequencies with r >= beta_fast are kept, with r <=
+                                      beta_slow divided by factor, in between linearly; the
+                                      rotated channels are multiplied by 0.1 ln(factor) + 1 */
+};
+#define MOSAIC_BSA_MAX_PAIRS 64
+
+/* A rotation, in host memory, filled by mosaic_bsa_rotation_init and not changed by
+ * any call.  Channels 0 .. rotary_dim - 1 are rotated, the others pass.  They belong to
+ * `axes` coordinates (1, or 2 for rows and columns of a grid) in that order, d =
+ * rotary_dim / axes channels each; pair i of an axis turns by position * theta^(-2 i / d)
+ * (stretched as above) and is made of channels (i, i + d/2) of the axis (HALVES) or
+ * (2 i, 2 i + 1) (PAIRS):
+ *   (a, b) -> magnitude * (a cos - b sin, b cos + a sin)
+ * Frequencies are kept as turns per position in units of 2^-64, so that any 32-bit
+ * position gives its angle to 2^-32 turns. */
+typedef struct {
+    int32_t rotary_dim, axes, layout;
+    float magnitude;
+    uint64_t turns[MOSAIC_BSA_MAX_PAIRS];
+} mosaic_bsa_rotation;
+
+/*
+ * Fills *out.  rotary_dim: 0 .. 128, a multiple of 2 * axes.  theta > 0 (10000 in the
+ * paper).  scaling: MOSAIC_BSA_SCALE_*; factor >= 1; original_tokens > 0 and beta_fast >
+ * beta_slow > 0 for RAMP (0, 0: 32 and 1).  inv_freq: NULL, or d / 2 frequencies in radians
+ * per position that replace theta and the scaling (the magnitude is 1 then).
+ */
+int mosaic_bsa_rotation_init(int32_t rotary_dim, int32_t axes, int32_t layout, double theta,
+                             int32_t scaling, double factor, double original_tokens,
+                             double beta_fast, double beta_slow, const double *inv_freq,
+                             mosaic_bsa_rotation *out);
+
+typedef struct {
+    int32_t batch, tokens;     /* B, N */
+    int32_t heads, kv_heads;   /* heads of q, and of k and v (0 = heads) */
+    int32_t head_dim;          /* 32, 64 or 128 */
+    int32_t dtype;             /* MOSAIC_BSA_F32 or _BF16 */
+    int32_t cache_tokens;      /* rows of k_out and v_out when `rows` is given */
+    int32_t position_batch;    /* int32 values from one batch entry's positions to the
+                                  next's; 0: all share [N, axes] */
+    float norm_eps;            /* norm forms: added to the mean square */
+    mosaic_bsa_strides q, k, v, q_out, k_out, v_out;
+} mosaic_bsa_heads_params;
+
+/*
+ * Rotation of q and k by their positions, q_out = R q, k_out = R k.
+ *   positions  in   device, int32 [N, axes] or [B, N, axes]; NULL (axes 1): 0 .. N - 1
+ *   q, k, v    in   device; k and k_out may both be NULL, and so may v and v_out
+ *   rows       in   device, int32 [B, N], or NULL.  Given: token n of batch entry b goes to
+ *                   row rows[b, n] of k_out and v_out, [B, kv_heads, cache_tokens, D] (a
+ *                   key/value cache); a row outside [0, cache_tokens) is not written.
+ *                   Two tokens of one entry must not name the same row.
+ *   q_out, k_out    out  device; may be q and k (same strides)
+ *   v_out           out  device: v as it is
+ * Base pointers and strides need the element's alignment only; 16 bytes are fastest.
+ * Sums and products run in fp32; the result is rounded once.
+ */
+int mosaic_bsa_rope_fwd(const mosaic_bsa_heads_params *params, const mosaic_bsa_rotation *rotation,
+                        const int32_t *positions, const void *q, const void *k, const void *v,
+                        const int32_t *rows, void *q_out, void *k_out, void *v_out,
+                        void *hip_stream);
+/*
+ * Gradient of mosaic_bsa_rope_fwd (without rows and v): dq = R^T dq_out, dk = R^T dk_out.
+ * params->q, k: strides of dq, dk; q_out, k_out: strides of dq_out, dk_out.  dq may be dq_out,
+ * dk may be dk_out (same strides).
+ */
+int mosaic_bsa_rope_bwd(const mosaic_bsa_heads_params *params, const mosaic_bsa_rotation *rotation,
+                        const int32_t *positions, const void *dq_out, const void *dk_out, void *dq,
+                        void *dk, void *hip_stream);
+/*
+ * Root-mean-square norm of every query and key head and the rotation in one pass:
+ *   q_out = R (q_weight * q / sqrt(mean(q^2) + norm_eps)), k likewise with k_weight.
+ *   q_weight, k_weight  in  device, fp32 [D]
+ * Otherwise as mosaic_bsa_rope_fwd.
+ */
+int mosaic_bsa_qk_norm_rope_fwd(const mosaic_bsa_heads_params *params,
+                                const mosaic_bsa_rotation *rotation, const int32_t *positions,
+                                const void *q, const void *k, const void *v,
+                                const float *q_weight, const float *k_weight, const int32_t *rows,
+                                void *q_out, void *k_out, void *v_out, void *hip_stream);
+/*
+ * Its gradient (without rows and v).
+ *   q, k                  in   device, the forward's inputs (params->q, k)
+ *   dq_out, dk_out        in   device (params->q_out, k_out)
+ *   dq, dk                out  device, strides dq_strides, dk_strides; may be dq_out and dk_out, or
+ *                              q and k, with the same strides
+ *   dq_weight, dk_weight  out  device, fp32 [D], summed over all rows in a fixed order
+ *   workspace                  device scratch of mosaic_bsa_qk_norm_rope_workspace_bytes(..) bytes
+ * dk_out and dk may both be NULL (k, k_weight, dk_weight are then not read or written).
+ */
+size_t mosaic_bsa_qk_norm_rope_workspace_bytes(const mosaic_bsa_heads_params *params);
+int mosaic_bsa_qk_norm_rope_bwd(const mosaic_bsa_heads_params *params,
+                                const mosaic_bsa_rotation *rotation, const int32_t *positions,
+                                const void *q, const void *k, const float *q_weight,
+                                const float *k_weight, const void *dq_out, const void *dk_out,
+                                const mosaic_bsa_strides *dq_strides,
+                                const mosaic_bsa_strides *dk_strides, void *dq, void *dk,
+                                float *dq_weight, float *dk_weight, void *workspace,
+                                size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Attention inside a sliding window, with first tokens that stay visible.
+ *
+ * Sequence b has k_lens[b] keys (token j of it is row j of k and v) and q_lens[b] queries,
+ * which stand at its end: query i is at position p = k_lens[b] - q_lens[b] + i.  It sees key j
+ * where
+ *   0 <= j < k_lens[b]  and  j <= p + window_right  and  (j >= p - window_left or j < n_sink)
+ * (a negative window_left or window_right: no bound on that side; window_right = 0 is causal).
+ * A query that sees no key, and the rows i >= q_lens[b], give zeros and a log-sum-exp of
+ * -infinity; their gradients are zeros, as are those of keys that no query sees.
+ */
+typedef struct {
+    int32_t batch, heads, kv_heads;    /* kv_heads: 0 = heads; divides heads */
+    int32_t q_tokens, k_tokens;        /* rows of q and out; of k and v */
+    int32_t head_dim;                  /* 32, 64 or 128 */
+    int32_t dtype;                     /* MOSAIC_BSA_F32 or _BF16 */
+    int32_t window_left, window_right;
+    int32_t n_sink;                    /* first tokens that stay visible */
+    int32_t ring;                      /* 0, or forward only: k and v are a ring cache of
+                                          k_tokens = n_sink + ring rows; token j < n_sink is row
+                                          j, token j >= n_sink row n_sink + (j - n_sink) % ring,
+                                          where the newest token with that row is held.
+                                          k_lens is required and may exceed k_tokens;
+                                          0 <= window_left <= ring - q_tokens */
+    float softmax_scale;               /* <= 0 selects 1/sqrt(head_dim) */
+    mosaic_bsa_strides q, k, v, out, dout, dq, dk, dv;
+} mosaic_bsa_window_params;
+
+/* Bytes of workspace for op MOSAIC_BSA_OP_FWD or _BWD; 0 if none or params is invalid. */
+size_t mosaic_bsa_window_workspace_bytes(const mosaic_bsa_window_params *params, int op);
+
+/*
+ *   q, k, v          in   device; bases and strides multiples of 16 bytes
+ *   q_lens, k_lens   in   device, int32 [batch], or NULL: q_tokens, k_tokens.  Values are held
+ *                         to [0, q_tokens] and [0, k_tokens] (k_lens: >= 0 with a ring)
+ *   out              out  device, must not alias an input
+ *   lse              out  device, fp32 [batch, heads, q_tokens], natural log; may be NULL
+ *   workspace             mosaic_bsa_window_workspace_bytes(.., OP_FWD) bytes (may be 0)
+ * Rows of k and v that no query of the call sees may hold anything; everything else must be
+ * finite.  Single tokens and short chunks split the keys over workgroups and join the parts
+ * in a fixed order: the same call gives the same bits.
+ */
+int mosaic_bsa_window_fwd(const mosaic_bsa_window_params *params, const void *q, const void *k,
+                          const void *v, const int32_t *q_lens, const int32_t *k_lens, void *out,
+                          float *lse, void *workspace, size_t workspace_bytes, void *hip_stream);
+/*
+ *   out, lse         in   device, as written by the forward
+ *   dout             in   device
+ *   dq, dk, dv       out  device (dk, dv summed over the query heads that share a key/value
+ *                         head), must not alias an input or each other
+ *   workspace             mosaic_bsa_window_workspace_bytes(.., OP_BWD) bytes
+ * Every sum runs in a fixed order (no floating-point atomics).
+ */
+int mosaic_bsa_window_bwd(const mosaic_bsa_window_params *params, const void *q, const void *k,
+                          const void *v, const void *out, const float *lse, const void *dout,
+                          const int32_t *q_lens, const int32_t *k_lens, void *dq, void *dk,
+                          void *dv, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /*
  * Checker for selections that were not produced by mosaic_bsa_select: the

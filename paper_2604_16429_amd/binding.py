@@ -20,6 +20,11 @@ F32, BF16 = 0, 1
 OP_SELECT, OP_FWD, OP_BWD = 0, 1, 2
 
 
+ROTATE_HALVES, ROTATE_PAIRS = 0, 1
+SCALE_NONE, SCALE_LINEAR, SCALE_BASE, SCALE_RAMP = 0, 1, 2, 3
+MAX_PAIRS = 64
+
+
 class BsaError(RuntimeError):
     def __init__(self, code: int, text: str):
         super().__init__(f"mosaic_bsa error {code}: {text}")
@@ -68,6 +73,180 @@ class Params:
         return self.n_tokens // self.block_tokens
 
 
+class _CStrides(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("head", ctypes.c_int64), ("token", ctypes.c_int64)]
+
+
+class _CRotation(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("axes", ctypes.c_int32),
+                ("layout", ctypes.c_int32), ("magnitude", ctypes.c_float),
+                ("turns", ctypes.c_uint64 * MAX_PAIRS)]
+
+
+class _CHeadsParams(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in
+                 ("batch", "tokens", "heads", "kv_heads", "head_dim", "dtype", "cache_tokens",
+                  "position_batch")] + [("norm_eps", ctypes.c_float)] +
+                [(n, _CStrides) for n in ("q", "k", "v", "q_out", "k_out", "v_out")])
+
+
+class _CWindowParams(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in
+                 ("batch", "heads", "kv_heads", "q_tokens", "k_tokens", "head_dim", "dtype",
+                  "window_left", "window_right", "n_sink", "ring")] +
+                [("softmax_scale", ctypes.c_float)] +
+                [(n, _CStrides) for n in ("q", "k", "v", "out", "dout", "dq", "dk", "dv")])
+
+
+class Rotation:
+    """A mosaic_bsa_rotation, filled by mosaic_bsa_rotation_init (see there): the frequencies
+    of a rotation of heads by their positions, made once and used by every call.  inv_freq:
+    frequencies in radians per position that replace theta and the scaling."""
+
+    def __init__(self, rotary_dim: int, axes: int = 1, layout: int = ROTATE_HALVES,
+                 theta: float = 10000.0, scaling: int = SCALE_NONE, factor: float = 1.0,
+                 original_tokens: float = 0.0, beta_fast: float = 0.0, beta_slow: float = 0.0,
+                 inv_freq=None):
+        freq = None
+        if inv_freq is not None:
+            values = [float(x) for x in inv_freq]
+            if axes in (1, 2) and len(values) != rotary_dim // axes // 2:
+                raise ValueError(f"inv_freq needs {rotary_dim // axes // 2} values")
+            freq = (ctypes.c_double * max(1, len(values)))(*values)
+        self.c = _CRotation()
+        self.axes = axes
+        _check(load_library().mosaic_bsa_rotation_init(
+            rotary_dim, axes, layout, theta, scaling, factor, original_tokens, beta_fast,
+            beta_slow, freq, ctypes.byref(self.c)))
+        self.ref = ctypes.byref(self.c)
+
+
+class _StridedParams:
+    """Parameters whose C struct also carries the tensors' strides: the struct is made once and
+    a stride is written into it when it differs from the last call's."""
+
+    _C = None
+    _SCALARS = ()
+
+    def _c(self):
+        c = self.__dict__.get("_struct")
+        if c is None:
+            c = self._struct = self._C()
+            self._ref = ctypes.byref(c)
+            self._last = {}
+        for name in self._SCALARS:
+            value = getattr(self, name)
+            if self._last.get(name) != value:
+                setattr(c, name, value)
+                self._last[name] = value
+        return c
+
+    def _tensor(self, field, t, heads, tokens):
+        """Device pointer of a [batch, heads, tokens, head_dim] tensor, whose strides go into
+        `field`; integers and None are taken as they are (contiguous)."""
+        last = self._last
+        if t is None or isinstance(t, int):
+            if last.get(field) is not None:
+                setattr(self._struct, field, _CStrides())
+                last[field] = None
+            return t
+        shape = (self.batch, heads, tokens, self.head_dim)
+        if t.shape != shape:
+            raise ValueError(f"{field}: shape {tuple(t.shape)} instead of {shape}")
+        if t.dtype is not _named_dtype(self.dtype) or not t.is_cuda:
+            raise ValueError(f"{field}: {t.dtype} on {t.device} instead of the parameters' dtype "
+                             "on a GPU")
+        strides = t.stride()
+        seen = (strides, shape)
+        if last.get(field) != seen:
+            if strides[3] != 1:
+                raise ValueError(f"{field}: channels must be consecutive")
+            if strides[2] == 0 and tokens > 1:
+                raise ValueError(f"{field}: tokens share memory")
+            # a dimension of one entry may carry any stride: the contiguous one is taken
+            token = strides[2] if tokens > 1 else self.head_dim
+            head = strides[1] if heads > 1 else token * tokens
+            batch = strides[0] if self.batch > 1 else head * heads
+            setattr(self._struct, field, _CStrides(batch, head, token))
+            last[field] = seen
+        return t.data_ptr()
+
+
+_TORCH_DTYPES = {}
+
+
+def _named_dtype(name):
+    if not _TORCH_DTYPES:
+        import torch
+        _TORCH_DTYPES.update({F32: torch.float32, BF16: torch.bfloat16,
+                              "float32": torch.float32, "int32": torch.int32})
+    return _TORCH_DTYPES.get(name)
+
+
+def _vector(name, t, size, dtype_name):
+    """Pointer of a contiguous device tensor of `size` values of torch dtype `dtype_name`."""
+    if t is None or isinstance(t, int):
+        return t
+    if (t.numel() != size or t.dtype is not _named_dtype(dtype_name) or not t.is_cuda or
+            not t.is_contiguous()):
+        raise ValueError(f"{name}: {size} contiguous {dtype_name} values on a GPU expected")
+    return t.data_ptr()
+
+
+@dataclasses.dataclass
+class HeadsParams(_StridedParams):
+    """Mirror of the C struct mosaic_bsa_heads_params (the strides come from the tensors)."""
+    batch: int
+    tokens: int
+    heads: int
+    head_dim: int
+    dtype: int = BF16
+    kv_heads: int = 0
+    cache_tokens: int = 0
+    norm_eps: float = 1e-6
+
+    _C = _CHeadsParams
+    _SCALARS = ("batch", "tokens", "heads", "head_dim", "dtype", "kv_heads", "cache_tokens",
+                "norm_eps")
+
+    def _positions(self, rotation, t):
+        per = 0
+        if t is not None and not isinstance(t, int):
+            n, axes = self.tokens, rotation.axes
+            if t.dtype is not _named_dtype("int32") or not t.is_cuda or not t.is_contiguous():
+                raise ValueError("positions: contiguous int32 on a GPU expected")
+            if t.shape == (self.batch, n, axes) or (axes == 1 and t.shape == (self.batch, n)):
+                per = n * axes
+            elif t.shape != (n, axes) and not (axes == 1 and t.shape == (n,)):
+                raise ValueError(f"positions: shape {tuple(t.shape)}")
+            t = t.data_ptr()
+        if self._last.get("position_batch") != per:
+            self._struct.position_batch = per
+            self._last["position_batch"] = per
+        return t
+
+
+@dataclasses.dataclass
+class WindowParams(_StridedParams):
+    """Mirror of the C struct mosaic_bsa_window_params (the strides come from the tensors)."""
+    batch: int
+    heads: int
+    q_tokens: int
+    k_tokens: int
+    head_dim: int
+    dtype: int = BF16
+    kv_heads: int = 0
+    window_left: int = -1
+    window_right: int = 0
+    n_sink: int = 0
+    ring: int = 0
+    softmax_scale: float = 0.0
+
+    _C = _CWindowParams
+    _SCALARS = ("batch", "heads", "q_tokens", "k_tokens", "head_dim", "dtype", "kv_heads",
+                "window_left", "window_right", "n_sink", "ring", "softmax_scale")
+
+
 def library_path() -> str:
     return _LIB_PATH
 
@@ -107,6 +286,28 @@ def load_library() -> ctypes.CDLL:
         lib.mosaic_bsa_check_selection.argtypes = [pp, vp, ctypes.c_int32, vp, vp]
         lib.mosaic_bsa_probe_mfma.restype = i32
         lib.mosaic_bsa_probe_mfma.argtypes = [vp, ctypes.c_int32, ctypes.c_int32, vp]
+        dbl, st = ctypes.c_double, ctypes.POINTER(_CStrides)
+        hp, rp = ctypes.POINTER(_CHeadsParams), ctypes.POINTER(_CRotation)
+        wp = ctypes.POINTER(_CWindowParams)
+        lib.mosaic_bsa_rotation_init.restype = i32
+        lib.mosaic_bsa_rotation_init.argtypes = (
+            [ctypes.c_int32] * 3 + [dbl, ctypes.c_int32] + [dbl] * 4 + [ctypes.POINTER(dbl), rp])
+        lib.mosaic_bsa_rope_fwd.restype = i32
+        lib.mosaic_bsa_rope_fwd.argtypes = [hp, rp] + [vp] * 9
+        lib.mosaic_bsa_rope_bwd.restype = i32
+        lib.mosaic_bsa_rope_bwd.argtypes = [hp, rp] + [vp] * 6
+        lib.mosaic_bsa_qk_norm_rope_fwd.restype = i32
+        lib.mosaic_bsa_qk_norm_rope_fwd.argtypes = [hp, rp] + [vp] * 11
+        lib.mosaic_bsa_qk_norm_rope_workspace_bytes.restype = sz
+        lib.mosaic_bsa_qk_norm_rope_workspace_bytes.argtypes = [hp]
+        lib.mosaic_bsa_qk_norm_rope_bwd.restype = i32
+        lib.mosaic_bsa_qk_norm_rope_bwd.argtypes = [hp, rp] + [vp] * 7 + [st, st] + [vp] * 5 + [sz, vp]
+        lib.mosaic_bsa_window_workspace_bytes.restype = sz
+        lib.mosaic_bsa_window_workspace_bytes.argtypes = [wp, i32]
+        lib.mosaic_bsa_window_fwd.restype = i32
+        lib.mosaic_bsa_window_fwd.argtypes = [wp] + [vp] * 8 + [sz, vp]
+        lib.mosaic_bsa_window_bwd.restype = i32
+        lib.mosaic_bsa_window_bwd.argtypes = [wp] + [vp] * 12 + [sz, vp]
         lib.mosaic_bsa_strerror.restype = ctypes.c_char_p
         lib.mosaic_bsa_strerror.argtypes = [i32]
         _lib = lib
@@ -232,3 +433,113 @@ def mosaic_bsa_check_selection(params: Params, sel_idx, own_block_allowed: bool,
     _check(load_library().mosaic_bsa_check_selection(
         ctypes.byref(cp), _ptr(sel_idx), 1 if own_block_allowed else 0, _ptr(n_bad),
         _stream(stream)))
+
+
+# ---- rotation, head norms and windowed attention: tensors of shape [batch, heads, tokens,
+# head_dim] with any strides of the first three dimensions
+
+def mosaic_bsa_rotation_init(rotary_dim: int, axes: int = 1, layout: int = ROTATE_HALVES,
+                             **kw) -> Rotation:
+    """The C entry point's name for Rotation(...)."""
+    return Rotation(rotary_dim, axes, layout, **kw)
+
+
+def _kv(params) -> int:
+    return params.kv_heads or params.heads
+
+
+def _heads_forward(params, rotation, positions, q, k, q_out, k_out, v, v_out, rows):
+    params._c()
+    kv, n = _kv(params), params.tokens
+    m = n if rows is None else params.cache_tokens
+    pos = params._positions(rotation, positions)
+    tensor = params._tensor
+    return (pos, tensor("q", q, params.heads, n), tensor("k", k, kv, n), tensor("v", v, kv, n),
+            _vector("rows", rows, params.batch * n, "int32"),
+            tensor("q_out", q_out, params.heads, n), tensor("k_out", k_out, kv, m),
+            tensor("v_out", v_out, kv, m))
+
+
+def mosaic_bsa_rope_fwd(params: HeadsParams, rotation: Rotation, positions, q, k, q_out, k_out,
+                        v=None, v_out=None, rows=None, stream=None) -> None:
+    pos, q, k, v, rows, q_out, k_out, v_out = _heads_forward(
+        params, rotation, positions, q, k, q_out, k_out, v, v_out, rows)
+    _check(load_library().mosaic_bsa_rope_fwd(params._ref, rotation.ref, pos, q, k, v, rows, q_out,
+                                              k_out, v_out, _stream(stream)))
+
+
+def mosaic_bsa_rope_bwd(params: HeadsParams, rotation: Rotation, positions, dq_out, dk_out, dq, dk,
+                        stream=None) -> None:
+    params._c()
+    kv, n, tensor = _kv(params), params.tokens, params._tensor
+    pos = params._positions(rotation, positions)
+    dq_out, dk_out = tensor("q_out", dq_out, params.heads, n), tensor("k_out", dk_out, kv, n)
+    dq, dk = tensor("q", dq, params.heads, n), tensor("k", dk, kv, n)
+    _check(load_library().mosaic_bsa_rope_bwd(params._ref, rotation.ref, pos, dq_out, dk_out, dq,
+                                              dk, _stream(stream)))
+
+
+def mosaic_bsa_qk_norm_rope_fwd(params: HeadsParams, rotation: Rotation, positions, q, k, q_weight,
+                                k_weight, q_out, k_out, v=None, v_out=None, rows=None,
+                                stream=None) -> None:
+    pos, q, k, v, rows, q_out, k_out, v_out = _heads_forward(
+        params, rotation, positions, q, k, q_out, k_out, v, v_out, rows)
+    d = params.head_dim
+    _check(load_library().mosaic_bsa_qk_norm_rope_fwd(
+        params._ref, rotation.ref, pos, q, k, v, _vector("q_weight", q_weight, d, "float32"),
+        _vector("k_weight", k_weight, d, "float32"), rows, q_out, k_out, v_out, _stream(stream)))
+
+
+def mosaic_bsa_qk_norm_rope_workspace_bytes(params: HeadsParams) -> int:
+    params._c()
+    return int(load_library().mosaic_bsa_qk_norm_rope_workspace_bytes(params._ref))
+
+
+def mosaic_bsa_qk_norm_rope_bwd(params: HeadsParams, rotation: Rotation, positions, q, k, q_weight,
+                                k_weight, dq_out, dk_out, dq, dk, dq_weight, dk_weight, workspace,
+                                stream=None, workspace_bytes=None) -> None:
+    c = params._c()
+    kv, n, d, tensor = _kv(params), params.tokens, params.head_dim, params._tensor
+    pos = params._positions(rotation, positions)
+    q, k = tensor("q", q, params.heads, n), tensor("k", k, kv, n)
+    dq_out, dk_out = tensor("q_out", dq_out, params.heads, n), tensor("k_out", dk_out, kv, n)
+    # the strides of dq and dk are arguments of their own: the fields of v and v_out hold them
+    dq, dk = tensor("v", dq, params.heads, n), tensor("v_out", dk, kv, n)
+    wb = _nbytes(workspace) if workspace_bytes is None else workspace_bytes
+    _check(load_library().mosaic_bsa_qk_norm_rope_bwd(
+        params._ref, rotation.ref, pos, q, k, _vector("q_weight", q_weight, d, "float32"),
+        _vector("k_weight", k_weight, d, "float32"), dq_out, dk_out, ctypes.byref(c.v),
+        ctypes.byref(c.v_out), dq, dk, _vector("dq_weight", dq_weight, d, "float32"),
+        _vector("dk_weight", dk_weight, d, "float32"), _ptr(workspace), wb, _stream(stream)))
+
+
+def mosaic_bsa_window_workspace_bytes(params: WindowParams, op: int) -> int:
+    params._c()
+    return int(load_library().mosaic_bsa_window_workspace_bytes(params._ref, int(op)))
+
+
+def mosaic_bsa_window_fwd(params: WindowParams, q, k, v, out, lse=None, q_lens=None, k_lens=None,
+                          workspace=None, stream=None, workspace_bytes=None) -> None:
+    params._c()
+    h, kv, nq, nk, tensor = params.heads, _kv(params), params.q_tokens, params.k_tokens, params._tensor
+    wb = _nbytes(workspace) if workspace_bytes is None else workspace_bytes
+    _check(load_library().mosaic_bsa_window_fwd(
+        params._ref, tensor("q", q, h, nq), tensor("k", k, kv, nk), tensor("v", v, kv, nk),
+        _vector("q_lens", q_lens, params.batch, "int32"),
+        _vector("k_lens", k_lens, params.batch, "int32"), tensor("out", out, h, nq),
+        _vector("lse", lse, params.batch * h * nq, "float32"), _ptr(workspace), wb,
+        _stream(stream)))
+
+
+def mosaic_bsa_window_bwd(params: WindowParams, q, k, v, out, lse, dout, dq, dk, dv,
+                          workspace=None, q_lens=None, k_lens=None, stream=None,
+                          workspace_bytes=None) -> None:
+    params._c()
+    h, kv, nq, nk, tensor = params.heads, _kv(params), params.q_tokens, params.k_tokens, params._tensor
+    wb = _nbytes(workspace) if workspace_bytes is None else workspace_bytes
+    _check(load_library().mosaic_bsa_window_bwd(
+        params._ref, tensor("q", q, h, nq), tensor("k", k, kv, nk), tensor("v", v, kv, nk),
+        tensor("out", out, h, nq), _vector("lse", lse, params.batch * h * nq, "float32"),
+        tensor("dout", dout, h, nq), _vector("q_lens", q_lens, params.batch, "int32"),
+        _vector("k_lens", k_lens, params.batch, "int32"), tensor("dq", dq, h, nq),
+        tensor("dk", dk, kv, nk), tensor("dv", dv, kv, nk), _ptr(workspace), wb, _stream(stream)))

@@ -553,6 +553,15 @@ extern "C" const char* mosaic_bsa_strerror(int code)
     case MOSAIC_BSA_ERR_ALIGN: return "tensor base pointers must be 16-byte aligned";
     case MOSAIC_BSA_ERR_LAUNCH: return "HIP kernel launch failed";
     case MOSAIC_BSA_ERR_OP: return "operation not available";
+    case MOSAIC_BSA_ERR_ROTATION:
+        return "invalid rotation: rotary_dim must be a multiple of 2 * axes in [0, head_dim], axes 1 "
+               "or 2, layout HALVES or PAIRS, frequencies finite, factor >= 1 (RAMP: original_tokens "
+               "> 0, beta_fast > beta_slow > 0)";
+    case MOSAIC_BSA_ERR_STRIDE:
+        return "a stride is negative or too large, or rows of an output share memory";
+    case MOSAIC_BSA_ERR_WINDOW:
+        return "invalid window: n_sink must not be negative; a ring is for the forward only, takes "
+               "k_lens and k_tokens = n_sink + ring, and needs 0 <= window_left <= ring - q_tokens";
     }
     return "unknown error code";
 }
