@@ -161,7 +161,8 @@ __global__ __launch_bounds__(256) void window_dq_kernel(
         for (int hh = 0; hh < KT / 32; ++hh) {
             const int s0 = slot0 + 32 * hh, j0 = s0 - keys.sinks + keys.lo;
             const bool plain = s0 >= keys.sinks;
-            if (s0 >= keys.count || (plain && (j0 > w_hi || j0 + 31 < w_lo))) continue;
+            if (s0 >= keys.count || (plain && (j0 > w_hi || (j0 + 31 < w_lo && j0 >= s.sinks))))
+                continue;
             const bool full = plain && all_valid && j0 >= all_lo && j0 + 31 <= all_hi;
             f32x16 st = splat(0.0f), dp = splat(neg_delta);
 #pragma unroll
@@ -171,12 +172,12 @@ __global__ __launch_bounds__(256) void window_dq_kernel(
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                float w = __builtin_amdgcn_exp2f(fmaf(st[r], c2, neg_l2));
+                float ds = __builtin_amdgcn_exp2f(fmaf(st[r], c2, neg_l2)) * dp[r];
                 if (!full) {
                     const int slot = s0 + 8 * (r >> 2) + 4 * half + (r & 3);
-                    w = slot < keys.count && see.sees(s, keys.token(slot)) ? w : 0.0f;
+                    ds = slot < keys.count && see.sees(s, keys.token(slot)) ? ds : 0.0f;
                 }
-                st[r] = w * dp[r];
+                st[r] = ds;
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -316,13 +317,15 @@ __global__ __launch_bounds__(256) void window_dkdv_kernel(
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int r = 4 * r4 + e;
-                    float w = __builtin_amdgcn_exp2f(fmaf(st[r], c2, -l[e]));
+                    float w = __builtin_amdgcn_exp2f(fmaf(st[r], c2, -l[e])), ds = w * dp[r];
                     if (!full) {
                         const int p = pos_s[32 * hh + 8 * r4 + 4 * half + e];
-                        w = j < kl && j <= p + s.right && (j >= p - s.left || j < s.sinks) ? w : 0.0f;
+                        const bool seen = j < kl && j <= p + s.right && (j >= p - s.left || j < s.sinks);
+                        w = seen ? w : 0.0f;
+                        ds = seen ? ds : 0.0f;         // (dp of an unseen key may be anything)
                     }
                     st[r] = w;
-                    dp[r] *= w;
+                    dp[r] = ds;
                 }
             }
 #pragma unroll

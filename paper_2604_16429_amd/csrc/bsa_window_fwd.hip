@@ -95,7 +95,8 @@ __global__ __launch_bounds__(256) void window_fwd_kernel(const T* __restrict__ q
         for (int hh = 0; hh < KT / 32; ++hh) {
             const int s0 = slot0 + 32 * hh, j0 = s0 - keys.sinks + keys.lo;
             const bool plain = s0 >= keys.sinks;       // all 32 slots are consecutive tokens
-            if (s0 >= keys.count || (plain && (j0 > w_hi || j0 + 31 < w_lo))) continue;
+            if (s0 >= keys.count || (plain && (j0 > w_hi || (j0 + 31 < w_lo && j0 >= s.sinks))))
+                continue;
             const bool full = plain && all_valid && j0 >= all_lo && j0 + 31 <= all_hi;
             f32x16 st = splat(0.0f);
 #pragma unroll
