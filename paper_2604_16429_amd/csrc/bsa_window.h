@@ -42,9 +42,17 @@ __device__ __forceinline__ void lengths(const Shape& s, int b, int& ql, int& kl)
 // tokens, then tokens lo, lo + 1, ...
 struct KeyList {
     int sinks, lo, count;
+    int row_lo, rows, ring;            // row of token lo; rows of the cache
     __device__ __forceinline__ int token(int slot) const
     {
         return slot < sinks ? slot : slot - sinks + lo;
+    }
+    // Row of k and v that holds it.  The tokens from lo on are at most `ring`, or none of
+    // them is past the first turn of the ring: there is one wrap at most.
+    __device__ __forceinline__ int row(int slot) const
+    {
+        const int r = slot - sinks + row_lo;
+        return slot < sinks ? slot : r >= rows ? r - ring : r;
     }
 };
 __device__ __forceinline__ KeyList key_list(const Shape& s, int first, int last, int kl)
@@ -54,13 +62,12 @@ __device__ __forceinline__ KeyList key_list(const Shape& s, int first, int last,
     l.lo = max(0, first - s.left);
     l.sinks = max(0, min(s.sinks, min(l.lo, hi + 1)));
     l.count = l.sinks + max(0, hi - l.lo + 1);
+    l.row_lo = l.lo;
+    l.rows = s.k_tokens;
+    l.ring = s.ring;
+    if (s.ring && l.lo >= s.sinks)
+        l.row_lo = s.sinks + (int)((uint32_t)(l.lo - s.sinks) % (uint32_t)s.ring);
     return l;
-}
-// Row of k and v that holds a token.
-__device__ __forceinline__ int cache_row(const Shape& s, int token)
-{
-    if (s.ring == 0 || token < s.sinks) return token;
-    return s.sinks + (int)((uint32_t)(token - s.sinks) % (uint32_t)s.ring);
 }
 
 // What one query sees: tokens lo .. hi and those below sinks, up to hi.
@@ -241,6 +248,19 @@ __device__ __forceinline__ void store_lane_row(T* p, const f32x16 (&acc)[D / 32]
                  acc[dt][4 * r + 2] * f, acc[dt][4 * r + 3] * f);
 }
 
+// Few rows: their keys are split over workgroups, each of which leaves what it has of a row
+// here, and join_rows adds the parts in their order.
+struct Parts {
+    float* acc;          // [slices][rows][splits][D]: sum of weight x value against the part's reference
+    float2* ml;          // [slices][rows][splits]: reference in base 2, sum of weights
+    int32_t splits;      // 1: none
+};
+__device__ __forceinline__ int64_t part_of(const Shape& s, const Parts& p, uint32_t slice, int row,
+                                           int split)
+{
+    return ((int64_t)slice * s.rows + row) * p.splits + split;
+}
+
 }  // namespace win
 
 // Host side: launches, called by the entry points after validation.
@@ -252,5 +272,11 @@ hipError_t launch_window_bwd(bool is_bf16, int D, const win::Shape& s, const voi
                              const void* v, const void* out, const float* lse, const void* dout,
                              void* dq, void* dk, void* dv, void* workspace, hipStream_t stream);
 size_t window_bwd_workspace(bool is_bf16, int D, const win::Shape& s);
+
+// Up to kStepRows rows of a slice (single tokens): a kernel of its own.
+constexpr int kStepRows = 32;
+hipError_t launch_window_step(bool is_bf16, int D, const win::Shape& s, const void* q, const void* k,
+                              const void* v, void* out, float* lse, const win::Parts& parts,
+                              hipStream_t stream);
 
 }  // namespace bsa

@@ -107,7 +107,7 @@ __global__ __launch_bounds__(256) void window_dq_kernel(
     const Sight see = sight(s, p0 + tok, kl, valid);
 
     const int t_first = row0 / s.group, t_last = min((row0 + 127) / s.group, ql - 1);
-    KeyList keys = {0, 0, 0};
+    KeyList keys = {};
     if (t_first <= t_last) keys = key_list(s, p0 + t_first, p0 + t_last, kl);
     const int w_first = (row0 + 32 * wave) / s.group, w_end = (row0 + 32 * wave + 31) / s.group;
     const int w_last = min(w_end, ql - 1);

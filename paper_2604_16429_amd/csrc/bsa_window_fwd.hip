@@ -19,7 +19,8 @@ __global__ __launch_bounds__(256) void window_fwd_kernel(const T* __restrict__ q
                                                          const T* __restrict__ v,
                                                          T* __restrict__ out,
                                                          float* __restrict__ lse, const Shape s,
-                                                         uint32_t row_tiles, uint32_t items)
+                                                         const Parts parts, uint32_t row_tiles,
+                                                         uint32_t items)
 {
     constexpr int KT = sizeof(T) == 2 ? 64 : 32;       // keys of a tile
     constexpr int KS = D / 16, DT = D / 32;
@@ -33,7 +34,9 @@ __global__ __launch_bounds__(256) void window_fwd_kernel(const T* __restrict__ q
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, half = lane >> 5;
 
-    const uint32_t item = item_of(blockIdx.x, items);
+    const uint32_t work = item_of(blockIdx.x, items);
+    const int split = (int)(work % (uint32_t)parts.splits);
+    const uint32_t item = work / (uint32_t)parts.splits;
     const uint32_t slice = item / row_tiles;
     const int row0 = (int)(item - slice * row_tiles) * 128;
     const int b = (int)(slice / (uint32_t)s.kv_heads), a = (int)(slice - (uint32_t)b * s.kv_heads);
@@ -48,7 +51,7 @@ __global__ __launch_bounds__(256) void window_fwd_kernel(const T* __restrict__ q
     const Sight see = sight(s, p0 + tok, kl, valid);
 
     const int t_first = row0 / s.group, t_last = min((row0 + 127) / s.group, ql - 1);
-    KeyList keys = {0, 0, 0};
+    KeyList keys = {};
     if (t_first <= t_last) keys = key_list(s, p0 + t_first, p0 + t_last, kl);
     // the same for this wavefront's rows alone
     const int w_first = (row0 + 32 * wave) / s.group, w_end = (row0 + 32 * wave + 31) / s.group;
@@ -77,20 +80,27 @@ __global__ __launch_bounds__(256) void window_fwd_kernel(const T* __restrict__ q
     auto fetch = [&](int slot0) {
         kt.fetch(tid, [&](int r) -> const T* {
             const int slot = slot0 + r;
-            return slot < keys.count ? kb + (int64_t)cache_row(s, keys.token(slot)) * s.k.token : nullptr;
+            return slot < keys.count ? kb + (int64_t)keys.row(slot) * s.k.token : nullptr;
         });
         vt.fetch(tid, [&](int r) -> const T* {
             const int slot = slot0 + r;
-            return slot < keys.count ? vb + (int64_t)cache_row(s, keys.token(slot)) * s.v.token : nullptr;
+            return slot < keys.count ? vb + (int64_t)keys.row(slot) * s.v.token : nullptr;
         });
     };
-    if (keys.count > 0) fetch(0);
-    for (int slot0 = 0; slot0 < keys.count; slot0 += KT) {
+    // this workgroup's slots
+    int slot_a = 0, slot_e = keys.count;
+    if (parts.splits > 1) {
+        const int per = ((keys.count + KT - 1) / KT + parts.splits - 1) / parts.splits * KT;
+        slot_a = split * per;
+        slot_e = min(keys.count, slot_a + per);
+    }
+    if (slot_a < slot_e) fetch(slot_a);
+    for (int slot0 = slot_a; slot0 < slot_e; slot0 += KT) {
         __syncthreads();                               // everyone is done with the tile before
         kt.put(k_lds, tid);
         vt.put(v_lds, tid);
         __syncthreads();
-        if (slot0 + KT < keys.count) fetch(slot0 + KT);
+        if (slot0 + KT < slot_e) fetch(slot0 + KT);
 #pragma unroll
         for (int hh = 0; hh < KT / 32; ++hh) {
             const int s0 = slot0 + 32 * hh, j0 = s0 - keys.sinks + keys.lo;
@@ -150,6 +160,12 @@ __global__ __launch_bounds__(256) void window_fwd_kernel(const T* __restrict__ q
 
     if (!exists) return;
     const float l = l_run + swap32(l_run);
+    if (parts.splits > 1) {
+        const int64_t part = part_of(s, parts, slice, row, split);
+        store_lane_row<float, D>(parts.acc + part * D, acc, 1.0f, half);
+        if (half == 0) parts.ml[part] = make_float2(m_ref, l);
+        return;
+    }
     T* o = out + (int64_t)b * s.out.batch + (int64_t)head * s.out.head + (int64_t)tok * s.out.token;
     // (a row that sees nothing: zeros)
     store_lane_row<T, D>(o, acc, l == 0.0f ? 0.0f : 1.0f / l, half);
@@ -158,34 +174,116 @@ __global__ __launch_bounds__(256) void window_fwd_kernel(const T* __restrict__ q
             l == 0.0f ? -INFINITY : (m_ref + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
+// The parts of a row, in their order: out = sum 2^(m - M) acc / sum 2^(m - M) l.  A thread has
+// four channels.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void window_join_kernel(T* __restrict__ out,
+                                                          float* __restrict__ lse, const Shape s,
+                                                          const Parts parts, int64_t quads)
+{
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= quads) return;
+    const int c = (int)(at % (D / 4)) * 4;
+    const int64_t all_row = at / (D / 4), slice = all_row / s.rows;
+    const int row = (int)(all_row - slice * s.rows);
+    const float2* ml = parts.ml + all_row * parts.splits;
+    const float* acc = parts.acc + all_row * parts.splits * D + c;
+    float top = kNoRef;
+    for (int i = 0; i < parts.splits; ++i) top = fmaxf(top, ml[i].x);
+    float l = 0.0f;
+    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int i = 0; i < parts.splits; ++i) {
+        const float f = __builtin_amdgcn_exp2f(ml[i].x - top);
+        const float4 x = *(const float4*)(acc + (int64_t)i * D);
+        l = fmaf(f, ml[i].y, l);
+        sum.x = fmaf(f, x.x, sum.x); sum.y = fmaf(f, x.y, sum.y);
+        sum.z = fmaf(f, x.z, sum.z); sum.w = fmaf(f, x.w, sum.w);
+    }
+    const int b = (int)(slice / s.kv_heads), a = (int)(slice - (int64_t)b * s.kv_heads);
+    const int tok = row / s.group, head = a * s.group + (row - tok * s.group);
+    const float f = l == 0.0f ? 0.0f : 1.0f / l;
+    put4(out + (int64_t)b * s.out.batch + (int64_t)head * s.out.head + (int64_t)tok * s.out.token + c,
+         sum.x * f, sum.y * f, sum.z * f, sum.w * f);
+    if (lse && c == 0)
+        lse[((int64_t)b * s.heads + head) * s.q_tokens + tok] =
+            l == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// Most keys that a tile of `rows` rows can see.
+int64_t most_keys(const Shape& s, int rows)
+{
+    const int64_t tokens = ((int64_t)rows + s.group - 1) / s.group + 1;
+    const int64_t span = (int64_t)s.left + min((int64_t)s.right, tokens) + tokens + s.sinks;
+    return s.ring ? min(span, (int64_t)s.ring + s.sinks) : min(span, (int64_t)s.k_tokens);
+}
+
+// Into how many parts the keys of a launch of few row tiles are split.
+int splits_of(const Shape& s)
+{
+    const bool step = s.rows <= kStepRows;
+    const int tile = step ? s.rows : 128;
+    const int64_t items = (int64_t)s.batch * s.kv_heads * ((s.rows + tile - 1) / tile);
+    const int64_t pieces = (most_keys(s, tile) + 127) / 128;
+    const int64_t want = (step ? 768 : 512) / items;
+    const int64_t n = min(min(want, pieces), (int64_t)64);
+    return n < 2 ? 1 : (int)n;
+}
+
+Parts parts_of(const Shape& s, int D, void* workspace)
+{
+    Parts p = {nullptr, nullptr, splits_of(s)};
+    if (p.splits > 1) {
+        const int64_t n = (int64_t)s.batch * s.kv_heads * s.rows * p.splits;
+        p.acc = (float*)workspace;
+        p.ml = (float2*)(p.acc + n * D);
+    }
+    return p;
+}
+
 template <typename T, int D>
 hipError_t launch(const Shape& s, const void* q, const void* k, const void* v, void* out,
-                  float* lse, hipStream_t stream)
+                  float* lse, void* workspace, hipStream_t stream)
 {
-    const uint32_t row_tiles = ((uint32_t)s.rows + 127) / 128;
-    const uint32_t items = row_tiles * (uint32_t)(s.batch * s.kv_heads);
-    window_fwd_kernel<T, D><<<items, 256, 0, stream>>>((const T*)q, (const T*)k, (const T*)v,
-                                                       (T*)out, lse, s, row_tiles, items);
+    const Parts parts = parts_of(s, D, workspace);
+    hipError_t e;
+    if (s.rows <= kStepRows) {
+        e = launch_window_step(sizeof(T) == 2, D, s, q, k, v, out, lse, parts, stream);
+    } else {
+        const uint32_t row_tiles = ((uint32_t)s.rows + 127) / 128;
+        const uint32_t items = row_tiles * (uint32_t)(s.batch * s.kv_heads * parts.splits);
+        window_fwd_kernel<T, D><<<items, 256, 0, stream>>>((const T*)q, (const T*)k, (const T*)v,
+                                                           (T*)out, lse, s, parts, row_tiles, items);
+        e = hipGetLastError();
+    }
+    if (e != hipSuccess || parts.splits == 1) return e;
+    const int64_t quads = (int64_t)s.batch * s.kv_heads * s.rows * (D / 4);
+    window_join_kernel<T, D><<<(unsigned)((quads + 255) / 256), 256, 0, stream>>>((T*)out, lse, s,
+                                                                                  parts, quads);
     return hipGetLastError();
 }
 
 }  // namespace win
 
-size_t window_fwd_workspace(bool, int, const win::Shape&) { return 0; }
+size_t window_fwd_workspace(bool, int D, const win::Shape& s)
+{
+    const int splits = win::splits_of(s);
+    return splits == 1 ? 0 : (size_t)s.batch * s.kv_heads * s.rows * splits * (D + 2) * sizeof(float);
+}
 
 hipError_t launch_window_fwd(bool is_bf16, int D, const win::Shape& s, const void* q, const void* k,
                              const void* v, void* out, float* lse, void* workspace,
                              hipStream_t stream)
 {
     using namespace win;
-    (void)workspace;
+#define BSA_WINDOW_FWD(T, D_) win::launch<T, D_>(s, q, k, v, out, lse, workspace, stream)
     if (is_bf16)
-        return D == 32   ? launch<uint16_t, 32>(s, q, k, v, out, lse, stream)
-               : D == 64 ? launch<uint16_t, 64>(s, q, k, v, out, lse, stream)
-                         : launch<uint16_t, 128>(s, q, k, v, out, lse, stream);
-    return D == 32   ? launch<float, 32>(s, q, k, v, out, lse, stream)
-           : D == 64 ? launch<float, 64>(s, q, k, v, out, lse, stream)
-                     : launch<float, 128>(s, q, k, v, out, lse, stream);
+        return D == 32   ? BSA_WINDOW_FWD(uint16_t, 32)
+               : D == 64 ? BSA_WINDOW_FWD(uint16_t, 64)
+                         : BSA_WINDOW_FWD(uint16_t, 128);
+    return D == 32   ? BSA_WINDOW_FWD(float, 32)
+           : D == 64 ? BSA_WINDOW_FWD(float, 64)
+                     : BSA_WINDOW_FWD(float, 128);
+#undef BSA_WINDOW_FWD
 }
 
 }  // namespace bsa
