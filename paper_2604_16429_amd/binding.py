@@ -122,43 +122,44 @@ class Rotation:
 
 
 class _StridedParams:
-    """Parameters whose C struct also carries the tensors' strides: the struct is made once and
-    a stride is written into it when it differs from the last call's."""
+    """Parameters whose C struct also carries the tensors' strides.  The struct is made when a
+    call first needs it and after a parameter was set; a tensor is looked at closely where its
+    type, shape or strides differ from those that its field had in the call before."""
 
     _C = None
     _SCALARS = ()
 
+    def __setattr__(self, name, value):
+        self.__dict__[name] = value
+        self.__dict__["_struct"] = None
+
     def _c(self):
-        c = self.__dict__.get("_struct")
+        c = self._struct
         if c is None:
-            c = self._struct = self._C()
-            self._ref = ctypes.byref(c)
-            self._last = {}
-        for name in self._SCALARS:
-            value = getattr(self, name)
-            if self._last.get(name) != value:
-                setattr(c, name, value)
-                self._last[name] = value
+            c = self._C()
+            for name in self._SCALARS:
+                setattr(c, name, getattr(self, name))
+            self.__dict__.update(_struct=c, _ref=ctypes.byref(c), _seen={})
         return c
 
     def _tensor(self, field, t, heads, tokens):
         """Device pointer of a [batch, heads, tokens, head_dim] tensor, whose strides go into
         `field`; integers and None are taken as they are (contiguous)."""
-        last = self._last
+        seen = self._seen
         if t is None or isinstance(t, int):
-            if last.get(field) is not None:
+            if seen.get(field) is not None:
                 setattr(self._struct, field, _CStrides())
-                last[field] = None
+                seen[field] = None
             return t
-        shape = (self.batch, heads, tokens, self.head_dim)
-        if t.shape != shape:
-            raise ValueError(f"{field}: shape {tuple(t.shape)} instead of {shape}")
-        if t.dtype is not _named_dtype(self.dtype) or not t.is_cuda:
-            raise ValueError(f"{field}: {t.dtype} on {t.device} instead of the parameters' dtype "
-                             "on a GPU")
-        strides = t.stride()
-        seen = (strides, shape)
-        if last.get(field) != seen:
+        shape, strides = t.shape, t.stride()
+        now = (shape, strides, tokens, heads, t.dtype, t.is_cuda)
+        if seen.get(field) != now:
+            wanted = (self.batch, heads, tokens, self.head_dim)
+            if shape != wanted:
+                raise ValueError(f"{field}: shape {tuple(shape)} instead of {wanted}")
+            if t.dtype is not _named_dtype(self.dtype) or not t.is_cuda:
+                raise ValueError(f"{field}: {t.dtype} on {t.device} instead of the parameters' "
+                                 "dtype on a GPU")
             if strides[3] != 1:
                 raise ValueError(f"{field}: channels must be consecutive")
             if strides[2] == 0 and tokens > 1:
@@ -168,7 +169,7 @@ class _StridedParams:
             head = strides[1] if heads > 1 else token * tokens
             batch = strides[0] if self.batch > 1 else head * heads
             setattr(self._struct, field, _CStrides(batch, head, token))
-            last[field] = seen
+            seen[field] = now
         return t.data_ptr()
 
 
@@ -220,9 +221,9 @@ class HeadsParams(_StridedParams):
             elif t.shape != (n, axes) and not (axes == 1 and t.shape == (n,)):
                 raise ValueError(f"positions: shape {tuple(t.shape)}")
             t = t.data_ptr()
-        if self._last.get("position_batch") != per:
+        if self._seen.get("position_batch") != per:
             self._struct.position_batch = per
-            self._last["position_batch"] = per
+            self._seen["position_batch"] = per
         return t
 
 

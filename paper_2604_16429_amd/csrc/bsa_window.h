@@ -148,18 +148,18 @@ __device__ __forceinline__ f32x16 splat(float x)
 
 // A tile of ROWS token rows of D channels in LDS, 16-byte chunks swizzled by the row: row
 // fragments take the same chunk of 8 consecutive rows, transposing reads a pair of chunks of
-// 4 rows.  Filled through registers by 256 threads, so that the next tile's loads are in
+// 4 rows.  Filled through registers by THREADS threads, so that the next tile's loads are in
 // flight while this one is worked on.
-template <typename T, int D, int ROWS>
+template <typename T, int D, int ROWS, int THREADS = 256>
 struct Tile {
     static constexpr int ROW_BYTES = D * sizeof(T);
     static constexpr int CHUNKS = ROW_BYTES / 16;
     static constexpr int BYTES = ROWS * ROW_BYTES;
-    static constexpr int PER_THREAD = ROWS * CHUNKS / 256;
-    static_assert(PER_THREAD >= 1 && ROWS * CHUNKS % 256 == 0, "whole chunks for every thread");
+    static constexpr int PER_THREAD = ROWS * CHUNKS / THREADS;
+    static_assert(PER_THREAD >= 1 && ROWS * CHUNKS % THREADS == 0, "whole chunks for every thread");
     using Frag = typename Mma<T>::Frag;
 
-    uint4 held[PER_THREAD];
+    i32x4 held[PER_THREAD];
 
     static __device__ __forceinline__ int place(int row, int chunk)
     {
@@ -172,17 +172,17 @@ struct Tile {
     {
 #pragma unroll
         for (int i = 0; i < PER_THREAD; ++i) {
-            const int at = tid + 256 * i, row = at / CHUNKS, chunk = at % CHUNKS;
+            const int at = tid + THREADS * i, row = at / CHUNKS, chunk = at % CHUNKS;
             const T* p = base(row);
-            held[i] = p ? *(const uint4*)((const char*)p + 16 * chunk) : make_uint4(0, 0, 0, 0);
+            held[i] = p ? *(const i32x4*)((const char*)p + 16 * chunk) : i32x4{0, 0, 0, 0};
         }
     }
     __device__ __forceinline__ void put(unsigned char* lds, int tid) const
     {
 #pragma unroll
         for (int i = 0; i < PER_THREAD; ++i) {
-            const int at = tid + 256 * i;
-            *(uint4*)(lds + place(at / CHUNKS, at % CHUNKS)) = held[i];
+            const int at = tid + THREADS * i;
+            *(i32x4*)(lds + place(at / CHUNKS, at % CHUNKS)) = held[i];
         }
     }
     // rows row0 .. row0 + 31 as rows of an operand, channels 16 ks ..

@@ -1,17 +1,17 @@
-// Windowed attention backward, any shape the entry point takes, on the matrix cores.
+// Windowed attention backward.
 //
 // With P = exp(scale q.k - lse) recomputed and delta = dO . O for each query,
 //   dV_j = sum_i P_ij dO_i    dS_ij = P_ij (dO_i . v_j - delta_i)
 //   dQ_i = scale sum_j dS_ij k_j    dK_j = scale sum_i dS_ij q_i
-// Three launches: delta and lse in base 2 by row; dQ, which walks the keys of 128 rows as the
-// forward does; dK and dV, where a workgroup owns 128 keys (32 to a wavefront, their K and V rows in
-// registers) and walks the rows that see them, all heads of the group in one sequence, so that
-// every sum has one fixed order and no atomics.
+// Launches: delta and lse in base 2 by row; dQ, which walks the keys of 128 rows as the forward
+// does; dK and dV, where a wavefront owns 32 keys and walks the queries that see them, in tiles
+// of consecutive tokens of one head, the heads of the group one after the other.  Every sum has
+// one fixed order and no atomics.
 //
-// A sink is seen by every later query, the keys behind it by window ones: the tiles that hold
-// sinks would be walked for the whole sequence by one workgroup.  Their rows beyond the window
-// are cut into chunks with a workgroup each; the parts meet in fp32 in the workspace and are
-// added in the order of the chunks by a fourth launch.
+// A sink is seen by every later query, the keys behind it by window ones: a workgroup that owns
+// sinks would walk the whole sequence.  What lies beyond the window of a tile that holds sinks is
+// cut into chunks of queries, each with a workgroup of its own that leaves fp32 sums for 32 keys
+// in the workspace; the tile's own workgroup adds them in the order of the chunks before it rounds.
 #include "bsa_window.h"
 
 #include "bsa_launch.h"
@@ -20,15 +20,63 @@ namespace bsa {
 
 namespace win {
 
-constexpr int kKeys = 128;          // keys of a dK/dV workgroup
+constexpr int kKeys = 128;             // keys of a workgroup whose wavefronts share tiles
 constexpr float kNoWeight = 3.0e38f;   // lse of a row without keys: its weights are 0
 
-// What the sinks' far rows are cut into.
+// Sums of the queries beyond the window of the tiles that hold sinks: [slices][groups][chunks][2]
+// [32][D] floats, dK (without the scale) and dV of groups of 32 keys.
 struct Far {
-    int32_t tiles, chunks;          // key tiles that hold sinks (0: no far rows), chunks of each
+    float* sums;
+    int32_t groups, chunks;            // groups of keys that hold sinks (0: no such queries)
+    int32_t near_keys;                 // a group's tile is this many keys: 32 or kKeys
 };
 
-__host__ __device__ inline int64_t part_floats(int D) { return (int64_t)2 * kKeys * D; }
+// Query tokens a .. e - 1 of a sequence that see keys J .. J + n - 1 inside the window.
+struct Span {
+    int a, e;
+};
+__device__ __forceinline__ Span near_span(const Shape& s, int J, int n, int p0, int ql, int kl)
+{
+    Span t;
+    t.a = max(0, J - s.right - p0);
+    t.e = J < kl ? min(ql, J + n + s.left - p0) : 0;
+    return t;
+}
+// ... and beyond it (sinks): chunk `chunk` of those.
+__device__ __forceinline__ Span far_span(const Shape& s, int J, int n, int p0, int ql, int kl,
+                                         int chunk, int chunks)
+{
+    Span t;
+    const int a = max(max(0, J - s.right - p0), J + n + s.left - p0);
+    const int all = J < kl ? max(0, ql - a) : 0;
+    const int per = ((all + chunks - 1) / chunks + 31) / 32 * 32;
+    t.a = a + min(all, chunk * per);
+    t.e = a + min(all, (chunk + 1) * per);
+    return t;
+}
+// Whether some query of the sequence sees key j (what no query sees may hold anything).
+__device__ __forceinline__ bool is_seen(const Shape& s, int j, int p0, int ql, int kl)
+{
+    const int last = p0 + ql - 1;
+    return j < kl && max(p0, j - s.right) <= (j < s.sinks ? last : min(last, j + s.left));
+}
+
+// The queries of a tile that see this lane's key: offsets x of tokens t0 + x with (unsigned)(x -
+// first) <= span.
+struct Column {
+    int first;
+    uint32_t span;
+    __device__ __forceinline__ bool seen(int x) const { return (uint32_t)(x - first) <= span; }
+};
+__device__ __forceinline__ Column column(const Shape& s, int j, int kl, int pt0, int tokens)
+{
+    const int lo = max(0, j - s.right - pt0);
+    const int hi = j >= kl ? -1 : min(tokens - 1, j < s.sinks ? tokens : j + s.left - pt0);
+    Column c;
+    c.first = hi >= lo ? lo : 1 << 20;
+    c.span = hi >= lo ? (uint32_t)(hi - lo) : 0u;
+    return c;
+}
 
 template <typename T, int D>
 __global__ __launch_bounds__(256) void window_rows_kernel(const T* __restrict__ out,
@@ -69,8 +117,9 @@ __global__ __launch_bounds__(256) void window_rows_kernel(const T* __restrict__ 
         if (here && part == 0) {
             const float l =
                 valid ? lse[((int64_t)b * s.heads + head) * s.q_tokens + tok] : -INFINITY;
-            delta[at] = d;
-            lse2[at] = l == -INFINITY ? kNoWeight : l * kLog2e;
+            const int64_t to = ((int64_t)b * s.heads + head) * s.q_tokens + tok;
+            delta[to] = d;
+            lse2[to] = l == -INFINITY ? kNoWeight : l * kLog2e;
         }
     }
 }
@@ -130,8 +179,9 @@ __global__ __launch_bounds__(256) void window_dq_kernel(
             gf[ks] = valid ? M::load(g + 16 * ks + 8 * half) : Frag{};
         }
         if (valid) {
-            neg_l2 = -lse2[(int64_t)slice * s.rows + row];
-            neg_delta = -delta[(int64_t)slice * s.rows + row];
+            const int64_t from = ((int64_t)b * s.heads + head) * s.q_tokens + tok;
+            neg_l2 = -lse2[from];
+            neg_delta = -delta[from];
         }
     }
     const float c2 = s.scale * kLog2e;
@@ -194,67 +244,125 @@ __global__ __launch_bounds__(256) void window_dq_kernel(
                          acc, s.scale, half);
 }
 
-// Per slice: key tiles' rows inside the window, then far.tiles * far.chunks chunks of far rows.
+// Adds the far sums of a group of 32 keys to a wavefront's accumulators, in the order of the chunks.
+template <int D>
+__device__ __forceinline__ void add_far(const Far& far, int64_t slice, int group, int l32, int half,
+                                        f32x16 (&ak)[D / 32], f32x16 (&av)[D / 32], float k_sign)
+{
+    const float* p = far.sums + ((slice * far.groups + group) * far.chunks) * (int64_t)(64 * D) + l32 * D;
+    for (int c = 0; c < far.chunks; ++c, p += 64 * D) {
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const f32x4 x = *(const f32x4*)(p + 32 * dt + 8 * r + 4 * half);
+                const f32x4 y = *(const f32x4*)(p + 32 * D + 32 * dt + 8 * r + 4 * half);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    ak[dt][4 * r + e] = fmaf(k_sign, x[e], ak[dt][4 * r + e]);
+                    av[dt][4 * r + e] += y[e];
+                }
+            }
+    }
+}
+
+// The products of 32 keys (operands kf, vf) with 32 queries whose rows lie in LDS; `col`: which of
+// them see the lane's key.
+template <typename T, int D, class Tl>
+__device__ __forceinline__ void key_products(const unsigned char* q_lds, const unsigned char* g_lds,
+                                             const float* l2_s, const float* dl_s, int row0, int lane,
+                                             const typename Mma<T>::Frag (&kf)[D / 16],
+                                             const typename Mma<T>::Frag (&vf)[D / 16], float c2,
+                                             bool full, const Column& col, f32x16 (&ak)[D / 32],
+                                             f32x16 (&av)[D / 32])
+{
+    using M = Mma<T>;
+    using Frag = typename M::Frag;
+    const int half = lane >> 5;
+    f32x16 st = splat(0.0f), dp;
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+        const f32x4 x = *(const f32x4*)(dl_s + 8 * r4 + 4 * half);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) dp[4 * r4 + e] = -x[e];
+    }
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+        st = M::mul(Tl::row_frag(q_lds, row0, ks, lane), kf[ks], st);
+        dp = M::mul(Tl::row_frag(g_lds, row0, ks, lane), vf[ks], dp);
+    }
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+        const f32x4 l = *(const f32x4*)(l2_s + 8 * r4 + 4 * half);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int r = 4 * r4 + e;
+            float w = __builtin_amdgcn_exp2f(fmaf(st[r], c2, -l[e]));
+            if (!full) w = col.seen(8 * r4 + 4 * half + e) ? w : 0.0f;
+            st[r] = w;
+            dp[r] *= w;
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const Frag pw = M::pack(st, h), ds = M::pack(dp, h);
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt) {
+            av[dt] = M::mul(Tl::trans_frag(g_lds, row0 + 16 * h, dt, lane), pw, av[dt]);
+            ak[dt] = M::mul(Tl::trans_frag(q_lds, row0 + 16 * h, dt, lane), ds, ak[dt]);
+        }
+    }
+}
+
+// K and V of a wavefront's 32 keys as operands; zeros where no query sees a key.
+template <typename T, int D>
+__device__ __forceinline__ void load_keys(const T* k, const T* v, const Shape& s, int64_t b, int64_t a,
+                                          int j, bool here, int half,
+                                          typename Mma<T>::Frag (&kf)[D / 16],
+                                          typename Mma<T>::Frag (&vf)[D / 16])
+{
+    using Frag = typename Mma<T>::Frag;
+    const T* kp = k + b * s.k.batch + a * s.k.head + (int64_t)j * s.k.token + 8 * half;
+    const T* vp = v + b * s.v.batch + a * s.v.head + (int64_t)j * s.v.token + 8 * half;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+        kf[ks] = here ? Mma<T>::load(kp + 16 * ks) : Frag{};
+        vf[ks] = here ? Mma<T>::load(vp + 16 * ks) : Frag{};
+    }
+}
+
+// dK and dV of 128 keys, any type and head dim: four wavefronts share the tiles.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void window_dkdv_kernel(
     const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
     const T* __restrict__ dout, const float* __restrict__ delta, const float* __restrict__ lse2,
-    T* __restrict__ dk, T* __restrict__ dv, float* __restrict__ parts, const Shape s, const Far far,
-    uint32_t key_tiles, uint32_t items)
+    T* __restrict__ dk, T* __restrict__ dv, const Shape s, const Far far, uint32_t key_tiles,
+    uint32_t items)
 {
-    constexpr int RT = sizeof(T) == 2 ? 64 : 32;        // rows of a tile
+    constexpr int RT = sizeof(T) == 2 ? 64 : 32;        // tokens of a tile
     constexpr int KS = D / 16, DT = D / 32;
     using Tl = Tile<T, D, RT>;
-    using M = Mma<T>;
-    using Frag = typename M::Frag;
+    using Frag = typename Mma<T>::Frag;
     __shared__ __attribute__((aligned(1024))) unsigned char q_lds[Tl::BYTES];
     __shared__ __attribute__((aligned(1024))) unsigned char g_lds[Tl::BYTES];
     __shared__ float l2_s[RT], dl_s[RT];
-    __shared__ int pos_s[RT];
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, half = lane >> 5;
 
-    const uint32_t per_slice = key_tiles + (uint32_t)(far.tiles * far.chunks);
     const uint32_t item = item_of(blockIdx.x, items);
-    const uint32_t slice = item / per_slice, in_slice = item - slice * per_slice;
-    const bool is_far = in_slice >= key_tiles;
-    const int key_tile = is_far ? (int)(in_slice - key_tiles) / far.chunks : (int)in_slice;
-    const int chunk = is_far ? (int)(in_slice - key_tiles) - key_tile * far.chunks : 0;
+    const uint32_t slice = item / key_tiles;
+    const int key_tile = (int)(item - slice * key_tiles);
     const int b = (int)(slice / (uint32_t)s.kv_heads), a = (int)(slice - (uint32_t)b * s.kv_heads);
     int ql, kl;
     lengths(s, b, ql, kl);
     const int p0 = kl - ql;
-    const int J = key_tile * kKeys;
-    const int jw = J + 32 * wave, j = jw + l32;         // this wavefront's keys, this lane's
-
-    // rows that see the tile: query tokens t_a .. t_b
-    int t_a = max(0, J - s.right - p0), t_b = min(ql - 1, J + kKeys - 1 + s.left - p0);
-    if (J >= kl) t_b = -1;
-    int row_a = t_a * s.group, row_e = (t_b + 1) * s.group;
-    if (is_far) {
-        t_a = max(t_a, J + kKeys + s.left - p0);
-        const int rows = J < kl ? max(0, ql - t_a) * s.group : 0;
-        const int per = ((rows + far.chunks - 1) / far.chunks + RT - 1) / RT * RT;
-        row_a = t_a * s.group + chunk * per;
-        row_e = min(t_a * s.group + rows, row_a + per);
-    }
-
-    const T* qb = q + (int64_t)b * s.q.batch + (int64_t)a * s.group * s.q.head;
-    const T* gb = dout + (int64_t)b * s.dout.batch + (int64_t)a * s.group * s.dout.head;
+    const int J = key_tile * kKeys, jw = J + 32 * wave, j = jw + l32;
+    const Span span = near_span(s, J, kKeys, p0, ql, kl);
 
     Frag kf[KS], vf[KS];
-    {
-        const bool here = j < kl;
-        const T* kp = k + (int64_t)b * s.k.batch + (int64_t)a * s.k.head + (int64_t)j * s.k.token;
-        const T* vp = v + (int64_t)b * s.v.batch + (int64_t)a * s.v.head + (int64_t)j * s.v.token;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            kf[ks] = here ? M::load(kp + 16 * ks + 8 * half) : Frag{};
-            vf[ks] = here ? M::load(vp + 16 * ks + 8 * half) : Frag{};
-        }
-    }
+    load_keys<T, D>(k, v, s, b, a, j, is_seen(s, j, p0, ql, kl), half, kf, vf);
     const float c2 = s.scale * kLog2e;
     f32x16 ak[DT], av[DT];
 #pragma unroll
@@ -262,91 +370,48 @@ __global__ __launch_bounds__(256) void window_dkdv_kernel(
 
     Tl qt, gt;
     float l2_held = 0.0f, dl_held = 0.0f;
-    int pos_held = 0;
-    auto fetch = [&](int r0) {
-        qt.fetch(tid, [&](int r) -> const T* {
-            const int row = r0 + r, tok = row / s.group;
-            return row < row_e ? qb + (int64_t)(row - tok * s.group) * s.q.head + (int64_t)tok * s.q.token
-                               : nullptr;
-        });
-        gt.fetch(tid, [&](int r) -> const T* {
-            const int row = r0 + r, tok = row / s.group;
-            return row < row_e
-                       ? gb + (int64_t)(row - tok * s.group) * s.dout.head + (int64_t)tok * s.dout.token
-                       : nullptr;
-        });
+    auto fetch = [&](int head, int t0) {
+        const T* qb = q + (int64_t)b * s.q.batch + (int64_t)head * s.q.head + (int64_t)t0 * s.q.token;
+        const T* gb = dout + (int64_t)b * s.dout.batch + (int64_t)head * s.dout.head +
+                      (int64_t)t0 * s.dout.token;
+        const int n = span.e - t0;
+        qt.fetch(tid, [&](int x) -> const T* { return x < n ? qb + (int64_t)x * s.q.token : nullptr; });
+        gt.fetch(tid, [&](int x) -> const T* { return x < n ? gb + (int64_t)x * s.dout.token : nullptr; });
         if (tid < RT) {
-            const int row = r0 + tid;
-            const bool here = row < row_e;
-            l2_held = here ? lse2[(int64_t)slice * s.rows + row] : kNoWeight;
-            dl_held = here ? delta[(int64_t)slice * s.rows + row] : 0.0f;
-            pos_held = here ? p0 + row / s.group : INT32_MIN;      // (sees nothing)
+            const int64_t at = ((int64_t)b * s.heads + head) * s.q_tokens + t0 + tid;
+            l2_held = tid < n ? lse2[at] : kNoWeight;
+            dl_held = tid < n ? delta[at] : 0.0f;
         }
     };
-    if (row_a < row_e) fetch(row_a);
-    for (int r0 = row_a; r0 < row_e; r0 += RT) {
+    const int tiles = span.e > span.a ? (span.e - span.a + RT - 1) / RT : 0;
+    const int all = tiles * s.group;
+    if (all > 0) fetch(a * s.group, span.a);
+    int head = a * s.group, t0 = span.a;
+    for (int it = 0; it < all; ++it) {
         __syncthreads();
         qt.put(q_lds, tid);
         gt.put(g_lds, tid);
-        if (tid < RT) { l2_s[tid] = l2_held; dl_s[tid] = dl_held; pos_s[tid] = pos_held; }
+        if (tid < RT) { l2_s[tid] = l2_held; dl_s[tid] = dl_held; }
         __syncthreads();
-        if (r0 + RT < row_e) fetch(r0 + RT);
+        int next_head = head, next_t0 = t0 + RT;
+        if (next_t0 >= span.e) { ++next_head; next_t0 = span.a; }
+        if (it + 1 < all) fetch(next_head, next_t0);
 #pragma unroll
         for (int hh = 0; hh < RT / 32; ++hh) {
-            const int ra = r0 + 32 * hh, re = min(ra + 32, row_e);
-            if (ra >= re) continue;
-            const int pa = p0 + ra / s.group, pb = p0 + (re - 1) / s.group;
-            if (jw >= kl || jw > pb + s.right || (jw + 31 < pa - s.left && jw >= s.sinks)) continue;
-            const bool full = ra + 32 == re && jw + 31 < kl && jw + 31 <= pa + s.right &&
-                              (jw >= pb - s.left || jw + 31 < s.sinks);
-            f32x16 st = splat(0.0f), dp;
-#pragma unroll
-            for (int r4 = 0; r4 < 4; ++r4) {
-                const f32x4 x = *(const f32x4*)(dl_s + 32 * hh + 8 * r4 + 4 * half);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) dp[4 * r4 + e] = -x[e];
-            }
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                st = M::mul(Tl::row_frag(q_lds, 32 * hh, ks, lane), kf[ks], st);
-                dp = M::mul(Tl::row_frag(g_lds, 32 * hh, ks, lane), vf[ks], dp);
-            }
-#pragma unroll
-            for (int r4 = 0; r4 < 4; ++r4) {
-                const f32x4 l = *(const f32x4*)(l2_s + 32 * hh + 8 * r4 + 4 * half);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int r = 4 * r4 + e;
-                    float w = __builtin_amdgcn_exp2f(fmaf(st[r], c2, -l[e])), ds = w * dp[r];
-                    if (!full) {
-                        const int p = pos_s[32 * hh + 8 * r4 + 4 * half + e];
-                        const bool seen = j < kl && j <= p + s.right && (j >= p - s.left || j < s.sinks);
-                        w = seen ? w : 0.0f;
-                        ds = seen ? ds : 0.0f;         // (dp of an unseen key may be anything)
-                    }
-                    st[r] = w;
-                    dp[r] = ds;
-                }
-            }
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const Frag pw = M::pack(st, h), ds = M::pack(dp, h);
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt) {
-                    av[dt] = M::mul(Tl::trans_frag(g_lds, 32 * hh + 16 * h, dt, lane), pw, av[dt]);
-                    ak[dt] = M::mul(Tl::trans_frag(q_lds, 32 * hh + 16 * h, dt, lane), ds, ak[dt]);
-                }
-            }
+            const int ta = t0 + 32 * hh, n = min(32, span.e - ta), pa = p0 + ta;
+            if (n <= 0 || jw >= kl || jw > pa + n - 1 + s.right ||
+                (jw + 31 < pa - s.left && jw >= s.sinks))
+                continue;
+            const bool full = n == 32 && jw + 31 < kl && jw + 31 <= pa + s.right &&
+                              (jw >= pa + 31 - s.left || jw + 31 < s.sinks);
+            key_products<T, D, Tl>(q_lds, g_lds, l2_s + 32 * hh, dl_s + 32 * hh, 32 * hh, lane, kf, vf, c2,
+                                   full, column(s, j, kl, pa, n), ak, av);
         }
+        head = next_head;
+        t0 = next_t0;
     }
-
-    if (key_tile < far.tiles) {
-        // one of the parts that are added up: [chunks + 1][2][keys][D]
-        float* p = parts + (((int64_t)slice * far.tiles + key_tile) * (far.chunks + 1) +
-                            (is_far ? chunk + 1 : 0)) * part_floats(D) + (32 * wave + l32) * D;
-        store_lane_row<float, D>(p, ak, s.scale, half);
-        store_lane_row<float, D>(p + kKeys * D, av, 1.0f, half);
-    } else if (j < s.k_tokens) {
+    if (jw / 32 < far.groups) add_far<D>(far, slice, jw / 32, l32, half, ak, av, 1.0f);
+    if (j < s.k_tokens) {
         store_lane_row<T, D>(dk + (int64_t)b * s.dk.batch + (int64_t)a * s.dk.head +
                                  (int64_t)j * s.dk.token, ak, s.scale, half);
         store_lane_row<T, D>(dv + (int64_t)b * s.dv.batch + (int64_t)a * s.dv.head +
@@ -354,34 +419,118 @@ __global__ __launch_bounds__(256) void window_dkdv_kernel(
     }
 }
 
-// The tiles that hold sinks: parts in order of the chunks.  A thread has four channels.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void window_sinks_kernel(const float* __restrict__ parts,
-                                                           T* __restrict__ dk, T* __restrict__ dv,
-                                                           const Shape s, const Far far,
-                                                           int64_t quads)
+// dK and dV of 32 keys: four wavefronts own the same keys and take the tiles of queries in turn,
+// with tiles of their own and no barrier between them; their sums are added in the order of the
+// wavefronts.  FAR: the queries beyond the window of the tile that holds the keys, one chunk to a
+// workgroup, sums to the workspace; else all inside the window.
+template <typename T, int D, bool FAR>
+__global__ __launch_bounds__(256) void window_dkdv_narrow_kernel(
+    const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
+    const T* __restrict__ dout, const float* __restrict__ delta, const float* __restrict__ lse2,
+    T* __restrict__ dk, T* __restrict__ dv, const Shape s, const Far far, uint32_t key_groups,
+    uint32_t items)
 {
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (at >= quads) return;
-    const int c = (int)(at % (D / 4)) * 4;
-    int64_t rest = at / (D / 4);
-    const int key = (int)(rest % kKeys);
-    rest /= kKeys;
-    const int is_v = (int)(rest & 1);
-    const int64_t tile_at = rest >> 1, slice = tile_at / far.tiles;
-    const int j = (int)(tile_at - slice * far.tiles) * kKeys + key;
-    if (j >= s.k_tokens) return;
-    const float* p = parts + tile_at * (far.chunks + 1) * part_floats(D) +
-                     ((int64_t)is_v * kKeys + key) * D + c;
-    float4 sum = *(const float4*)p;
-    for (int i = 1; i <= far.chunks; ++i) {
-        const float4 x = *(const float4*)(p + i * part_floats(D));
-        sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
+    constexpr int RT = 32, KS = D / 16, DT = D / 32;
+    using Tl = Tile<T, D, RT, 64>;
+    using Frag = typename Mma<T>::Frag;
+    __shared__ __attribute__((aligned(1024))) unsigned char tiles_s[4][2][Tl::BYTES];
+    __shared__ float l2_s[4][RT], dl_s[4][RT];
+    static_assert(2 * DT * 16 * 64 * 4 <= (int)sizeof(tiles_s), "a wavefront's sums fit the tiles");
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l32 = lane & 31, half = lane >> 5;
+
+    const uint32_t chunks = FAR ? (uint32_t)far.chunks : 1u;
+    const uint32_t work = item_of(blockIdx.x, items);
+    const int chunk = (int)(work % chunks);
+    const uint32_t item = work / chunks;
+    const uint32_t slice = item / key_groups;
+    const int group = (int)(item - slice * key_groups);
+    const int b = (int)(slice / (uint32_t)s.kv_heads), a = (int)(slice - (uint32_t)b * s.kv_heads);
+    int ql, kl;
+    lengths(s, b, ql, kl);
+    const int p0 = kl - ql;
+    const int jw = 32 * group, j = jw + l32;
+    const Span span = FAR ? far_span(s, jw / far.near_keys * far.near_keys, far.near_keys, p0, ql, kl,
+                                     chunk, (int)chunks)
+                          : near_span(s, jw, 32, p0, ql, kl);
+
+    Frag kf[KS], vf[KS];
+    load_keys<T, D>(k, v, s, b, a, j, is_seen(s, j, p0, ql, kl), half, kf, vf);
+    const float c2 = s.scale * kLog2e;
+    f32x16 ak[DT], av[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) ak[dt] = av[dt] = splat(0.0f);
+
+    Tl qt, gt;
+    float row_held = 0.0f;                              // lse in lanes 0 .. 31, delta in the others
+    const int tiles = span.e > span.a ? (span.e - span.a + RT - 1) / RT : 0;
+    const int all = tiles * s.group;
+    auto fetch = [&](int it) {
+        const int hd = it / tiles, head = a * s.group + hd, t0 = span.a + (it - hd * tiles) * RT;
+        const T* qb = q + (int64_t)b * s.q.batch + (int64_t)head * s.q.head + (int64_t)t0 * s.q.token;
+        const T* gb = dout + (int64_t)b * s.dout.batch + (int64_t)head * s.dout.head +
+                      (int64_t)t0 * s.dout.token;
+        const int n = span.e - t0;
+        qt.fetch(lane, [&](int x) -> const T* { return x < n ? qb + (int64_t)x * s.q.token : nullptr; });
+        gt.fetch(lane, [&](int x) -> const T* { return x < n ? gb + (int64_t)x * s.dout.token : nullptr; });
+        const int64_t at = ((int64_t)b * s.heads + head) * s.q_tokens + t0 + l32;
+        row_held = l32 < n ? (half ? delta[at] : lse2[at]) : half ? 0.0f : kNoWeight;
+    };
+    if (wave < all) fetch(wave);
+    for (int it = wave; it < all; it += 4) {
+        lane_exchange();
+        qt.put(tiles_s[wave][0], lane);
+        gt.put(tiles_s[wave][1], lane);
+        (half ? dl_s : l2_s)[wave][l32] = row_held;
+        lane_exchange();
+        if (it + 4 < all) fetch(it + 4);
+        const int t0 = span.a + it % tiles * RT, n = min(RT, span.e - t0), pa = p0 + t0;
+        const bool full = n == 32 && jw + 31 < kl && jw + 31 <= pa + s.right &&
+                          (jw >= pa + 31 - s.left || jw + 31 < s.sinks);
+        key_products<T, D, Tl>(tiles_s[wave][0], tiles_s[wave][1], l2_s[wave], dl_s[wave], 0, lane, kf, vf,
+                               c2, full, column(s, j, kl, pa, n), ak, av);
     }
-    const int b = (int)(slice / s.kv_heads), a = (int)(slice - (int64_t)b * s.kv_heads);
-    T* y = is_v ? dv + (int64_t)b * s.dv.batch + (int64_t)a * s.dv.head + (int64_t)j * s.dv.token
-                : dk + (int64_t)b * s.dk.batch + (int64_t)a * s.dk.head + (int64_t)j * s.dk.token;
-    store4(y + c, sum);
+    // the other wavefronts' sums, in their order
+    float* const region = (float*)&tiles_s[0][0][0] + lane;
+    for (int w = 1; w < 4; ++w) {
+        __syncthreads();
+        if (wave == w) {
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    region[(dt * 16 + r) * 64] = ak[dt][r];
+                    region[((DT + dt) * 16 + r) * 64] = av[dt][r];
+                }
+        }
+        __syncthreads();
+        if (wave == 0) {
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    ak[dt][r] += region[(dt * 16 + r) * 64];
+                    av[dt][r] += region[((DT + dt) * 16 + r) * 64];
+                }
+        }
+    }
+    if (wave != 0) return;
+    if constexpr (FAR) {
+        float* p = far.sums + (((int64_t)slice * far.groups + group) * far.chunks + chunk) * (64 * D) +
+                   l32 * D;
+        store_lane_row<float, D>(p, ak, 1.0f, half);
+        store_lane_row<float, D>(p + 32 * D, av, 1.0f, half);
+    } else {
+        if (group < far.groups) add_far<D>(far, slice, group, l32, half, ak, av, 1.0f);
+        if (j < s.k_tokens) {
+            store_lane_row<T, D>(dk + (int64_t)b * s.dk.batch + (int64_t)a * s.dk.head +
+                                     (int64_t)j * s.dk.token, ak, s.scale, half);
+            store_lane_row<T, D>(dv + (int64_t)b * s.dv.batch + (int64_t)a * s.dv.head +
+                                     (int64_t)j * s.dv.token, av, 1.0f, half);
+        }
+    }
 }
 
 size_t rounded(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -391,70 +540,82 @@ size_t row_bytes(const Shape& s)
     return rounded((size_t)s.batch * s.kv_heads * s.rows * sizeof(float));
 }
 
+// Launches of few workgroups of 128 keys give every 32 keys a workgroup of their own.
+bool is_narrow(const Shape& s)
+{
+    return (int64_t)s.batch * s.kv_heads * ((s.k_tokens + kKeys - 1) / kKeys) < 256;
+}
+
 Far far_of(const Shape& s)
 {
-    Far f = {0, 0};
+    Far f = {nullptr, 0, 0, is_narrow(s) ? 32 : kKeys};
     // queries beyond the window of a sink exist where the window is shorter than the sequence
     if (s.sinks == 0 || s.left >= s.k_tokens) return f;
-    f.tiles = (min(s.sinks, s.k_tokens) + kKeys - 1) / kKeys;
-    f.chunks = max(1, min(64, s.rows / 1024));
+    f.groups = (s.sinks + 31) / 32;
+    // a workgroup per CU and a half, of at least 8 tiles of 32 queries for each wavefront
+    const int64_t slices = (int64_t)s.batch * s.kv_heads;
+    const int64_t want = max((int64_t)1, 384 / (slices * f.groups)), most = max(1, s.rows / 1024);
+    f.chunks = (int)min(min(want, most), (int64_t)32);
     return f;
 }
 
-size_t parts_bytes(const Shape& s, int D)
+size_t far_bytes(const Shape& s, int D)
 {
     const Far f = far_of(s);
-    if (f.tiles == 0) return 0;
-    return rounded((size_t)s.batch * s.kv_heads * f.tiles * (f.chunks + 1) * part_floats(D) *
-                   sizeof(float));
+    return rounded((size_t)s.batch * s.kv_heads * f.groups * f.chunks * 64 * D * sizeof(float));
 }
 
 template <typename T, int D>
-hipError_t launch_bwd(const Shape& s, const void* q, const void* k, const void* v, const void* out,
-                      const float* lse, const void* dout, void* dq, void* dk, void* dv,
+hipError_t launch_bwd(const Shape& s, const void* q_, const void* k_, const void* v_, const void* out_,
+                      const float* lse, const void* dout_, void* dq_, void* dk_, void* dv_,
                       void* workspace, hipStream_t stream)
 {
+    const T *q = (const T*)q_, *k = (const T*)k_, *v = (const T*)v_, *out = (const T*)out_,
+            *dout = (const T*)dout_;
+    T *dq = (T*)dq_, *dk = (T*)dk_, *dv = (T*)dv_;
     const int64_t slices = (int64_t)s.batch * s.kv_heads;
     float* delta = (float*)workspace;
     float* lse2 = (float*)((char*)workspace + row_bytes(s));
-    float* parts = (float*)((char*)workspace + 2 * row_bytes(s));
-    const Far far = far_of(s);
+    Far far = far_of(s);
+    far.sums = (float*)((char*)workspace + 2 * row_bytes(s));
 
     const int64_t all_rows = slices * s.rows;
     const int rows_per = 256 / (D * (int)sizeof(T) / 16);
     const int64_t row_groups = (all_rows + rows_per - 1) / rows_per;
     window_rows_kernel<T, D><<<(unsigned)min(row_groups, (int64_t)1 << 20), 256, 0, stream>>>(
-        (const T*)out, (const T*)dout, lse, delta, lse2, s, all_rows);
+        out, dout, lse, delta, lse2, s, all_rows);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
 
     const uint32_t row_tiles = ((uint32_t)s.rows + 127) / 128;
     const uint32_t q_items = row_tiles * (uint32_t)slices;
-    window_dq_kernel<T, D><<<q_items, 256, 0, stream>>>((const T*)q, (const T*)k, (const T*)v,
-                                                       (const T*)dout, delta, lse2, (T*)dq, s,
-                                                       row_tiles, q_items);
+    window_dq_kernel<T, D><<<q_items, 256, 0, stream>>>(q, k, v, dout, delta, lse2, dq, s, row_tiles,
+                                                       q_items);
     if ((e = hipGetLastError()) != hipSuccess) return e;
 
-    const uint32_t key_tiles = ((uint32_t)s.k_tokens + kKeys - 1) / kKeys;
-    const uint32_t k_items = (uint32_t)slices * (key_tiles + (uint32_t)(far.tiles * far.chunks));
-    window_dkdv_kernel<T, D><<<k_items, 256, 0, stream>>>(
-        (const T*)q, (const T*)k, (const T*)v, (const T*)dout, delta, lse2, (T*)dk, (T*)dv, parts, s,
-        far, key_tiles, k_items);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    if (far.tiles) {
-        const int64_t quads = slices * far.tiles * 2 * kKeys * (D / 4);
-        window_sinks_kernel<T, D><<<(unsigned)((quads + 255) / 256), 256, 0, stream>>>(
-            parts, (T*)dk, (T*)dv, s, far, quads);
-        e = hipGetLastError();
+    if (far.groups) {
+        const uint32_t n = (uint32_t)slices * (uint32_t)(far.groups * far.chunks);
+        window_dkdv_narrow_kernel<T, D, true><<<n, 256, 0, stream>>>(
+            q, k, v, dout, delta, lse2, dk, dv, s, far, (uint32_t)far.groups, n);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
     }
-    return e;
+    const uint32_t per = is_narrow(s) ? 32 : kKeys;
+    const uint32_t key_tiles = ((uint32_t)s.k_tokens + per - 1) / per;
+    const uint32_t k_items = (uint32_t)slices * key_tiles;
+    if (is_narrow(s))
+        window_dkdv_narrow_kernel<T, D, false><<<k_items, 256, 0, stream>>>(
+            q, k, v, dout, delta, lse2, dk, dv, s, far, key_tiles, k_items);
+    else
+        window_dkdv_kernel<T, D><<<k_items, 256, 0, stream>>>(q, k, v, dout, delta, lse2, dk, dv, s, far,
+                                                             key_tiles, k_items);
+    return hipGetLastError();
 }
 
 }  // namespace win
 
 size_t window_bwd_workspace(bool, int D, const win::Shape& s)
 {
-    return 2 * win::row_bytes(s) + win::parts_bytes(s, D);
+    return 2 * win::row_bytes(s) + win::far_bytes(s, D);
 }
 
 hipError_t launch_window_bwd(bool is_bf16, int D, const win::Shape& s, const void* q, const void* k,
