@@ -31,11 +31,18 @@ struct Shape {
     mosaic_bsa_strides q, k, v, out, dout, dq, dk, dv;    // elements
 };
 
-// Lengths of sequence b, held to what the tensors have.
+// Lengths of sequence b, held to what the tensors have; b is the same for all lanes, and so
+// are the results, in scalar registers with everything that follows from them (a load that a
+// kernel's stores might alias would leave them in vector registers).
+__device__ __forceinline__ int query_length(const Shape& s, int b)
+{
+    return s.q_lens ? min(max(s.q_lens[b], 0), s.q_tokens) : s.q_tokens;
+}
 __device__ __forceinline__ void lengths(const Shape& s, int b, int& ql, int& kl)
 {
-    ql = s.q_lens ? min(max(s.q_lens[b], 0), s.q_tokens) : s.q_tokens;
+    ql = __builtin_amdgcn_readfirstlane(query_length(s, b));
     kl = s.k_lens ? min(max(s.k_lens[b], 0), s.ring ? kUnbounded : s.k_tokens) : s.k_tokens;
+    kl = __builtin_amdgcn_readfirstlane(kl);
 }
 
 // The keys that queries at positions first .. last see, as slots 0 .. count - 1: `sinks` first

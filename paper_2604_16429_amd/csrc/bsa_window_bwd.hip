@@ -12,71 +12,13 @@
 // sinks would walk the whole sequence.  What lies beyond the window of a tile that holds sinks is
 // cut into chunks of queries, each with a workgroup of its own that leaves fp32 sums for 32 keys
 // in the workspace; the tile's own workgroup adds them in the order of the chunks before it rounds.
-#include "bsa_window.h"
+#include "bsa_window_bwd.h"
 
 #include "bsa_launch.h"
 
 namespace bsa {
 
 namespace win {
-
-constexpr int kKeys = 128;             // keys of a workgroup whose wavefronts share tiles
-constexpr float kNoWeight = 3.0e38f;   // lse of a row without keys: its weights are 0
-
-// Sums of the queries beyond the window of the tiles that hold sinks: [slices][groups][chunks][2]
-// [32][D] floats, dK (without the scale) and dV of groups of 32 keys.
-struct Far {
-    float* sums;
-    int32_t groups, chunks;            // groups of keys that hold sinks (0: no such queries)
-    int32_t near_keys;                 // a group's tile is this many keys: 32 or kKeys
-};
-
-// Query tokens a .. e - 1 of a sequence that see keys J .. J + n - 1 inside the window.
-struct Span {
-    int a, e;
-};
-__device__ __forceinline__ Span near_span(const Shape& s, int J, int n, int p0, int ql, int kl)
-{
-    Span t;
-    t.a = max(0, J - s.right - p0);
-    t.e = J < kl ? min(ql, J + n + s.left - p0) : 0;
-    return t;
-}
-// ... and beyond it (sinks): chunk `chunk` of those.
-__device__ __forceinline__ Span far_span(const Shape& s, int J, int n, int p0, int ql, int kl,
-                                         int chunk, int chunks)
-{
-    Span t;
-    const int a = max(max(0, J - s.right - p0), J + n + s.left - p0);
-    const int all = J < kl ? max(0, ql - a) : 0;
-    const int per = ((all + chunks - 1) / chunks + 31) / 32 * 32;
-    t.a = a + min(all, chunk * per);
-    t.e = a + min(all, (chunk + 1) * per);
-    return t;
-}
-// Whether some query of the sequence sees key j (what no query sees may hold anything).
-__device__ __forceinline__ bool is_seen(const Shape& s, int j, int p0, int ql, int kl)
-{
-    const int last = p0 + ql - 1;
-    return j < kl && max(p0, j - s.right) <= (j < s.sinks ? last : min(last, j + s.left));
-}
-
-// The queries of a tile that see this lane's key: offsets x of tokens t0 + x with (unsigned)(x -
-// first) <= span.
-struct Column {
-    int first;
-    uint32_t span;
-    __device__ __forceinline__ bool seen(int x) const { return (uint32_t)(x - first) <= span; }
-};
-__device__ __forceinline__ Column column(const Shape& s, int j, int kl, int pt0, int tokens)
-{
-    const int lo = max(0, j - s.right - pt0);
-    const int hi = j >= kl ? -1 : min(tokens - 1, j < s.sinks ? tokens : j + s.left - pt0);
-    Column c;
-    c.first = hi >= lo ? lo : 1 << 20;
-    c.span = hi >= lo ? (uint32_t)(hi - lo) : 0u;
-    return c;
-}
 
 template <typename T, int D>
 __global__ __launch_bounds__(256) void window_rows_kernel(const T* __restrict__ out,
@@ -97,9 +39,7 @@ __global__ __launch_bounds__(256) void window_rows_kernel(const T* __restrict__ 
         const int row = here ? (int)(at - slice * s.rows) : 0;
         const int b = (int)(slice / s.kv_heads), a = (int)(slice - (int64_t)b * s.kv_heads);
         const int tok = row / s.group, head = a * s.group + (row - tok * s.group);
-        int ql, kl;
-        lengths(s, b, ql, kl);
-        const bool valid = here && tok < ql;
+        const bool valid = here && tok < query_length(s, b);
         float d = 0.0f;
         if (valid) {
             const T* o = out + (int64_t)b * s.out.batch + (int64_t)head * s.out.head +
@@ -242,28 +182,6 @@ __global__ __launch_bounds__(256) void window_dq_kernel(
     store_lane_row<T, D>(dq + (int64_t)b * s.dq.batch + (int64_t)head * s.dq.head +
                              (int64_t)tok * s.dq.token,
                          acc, s.scale, half);
-}
-
-// Adds the far sums of a group of 32 keys to a wavefront's accumulators, in the order of the chunks.
-template <int D>
-__device__ __forceinline__ void add_far(const Far& far, int64_t slice, int group, int l32, int half,
-                                        f32x16 (&ak)[D / 32], f32x16 (&av)[D / 32], float k_sign)
-{
-    const float* p = far.sums + ((slice * far.groups + group) * far.chunks) * (int64_t)(64 * D) + l32 * D;
-    for (int c = 0; c < far.chunks; ++c, p += 64 * D) {
-#pragma unroll
-        for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const f32x4 x = *(const f32x4*)(p + 32 * dt + 8 * r + 4 * half);
-                const f32x4 y = *(const f32x4*)(p + 32 * D + 32 * dt + 8 * r + 4 * half);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    ak[dt][4 * r + e] = fmaf(k_sign, x[e], ak[dt][4 * r + e]);
-                    av[dt][4 * r + e] += y[e];
-                }
-            }
-    }
 }
 
 // The products of 32 keys (operands kf, vf) with 32 queries whose rows lie in LDS; `col`: which of
@@ -605,6 +523,8 @@ hipError_t launch_bwd(const Shape& s, const void* q_, const void* k_, const void
     if (is_narrow(s))
         window_dkdv_narrow_kernel<T, D, false><<<k_items, 256, 0, stream>>>(
             q, k, v, dout, delta, lse2, dk, dv, s, far, key_tiles, k_items);
+    else if (window_bwd_mfma_supported(sizeof(T) == 2, D, s))
+        return launch_window_dkdv_mfma(D, s, q, k, v, dout, delta, lse2, dk, dv, far, stream);
     else
         window_dkdv_kernel<T, D><<<k_items, 256, 0, stream>>>(q, k, v, dout, delta, lse2, dk, dv, s, far,
                                                              key_tiles, k_items);

@@ -1,0 +1,372 @@
+// Windowed attention backward, bf16, head dims 64 and 128: dK and dV of large launches (see
+// bsa_window_bwd.hip for the formulas and the other kernels).
+//
+// A workgroup of four wavefronts owns 128 keys, 32 to each, and walks the queries that see them
+// inside the window, head by head, in tiles of 64 (head dim 128: 32) tokens that are gathered
+// straight into LDS, double buffered, one barrier a tile.  Matrix instructions bound it; per 32
+// queries x 32 keys there are as many LDS bytes to read as the matrix unit takes time, and
+// vector work of about half that time.  So the order of everything in a tile is written out:
+// fragments are read several matrix instructions before their use, and the exponentials and
+// products of the weights stand behind matrix instructions, two to a slot, where nothing waits
+// for the instruction in front of it.  Where the window's border crosses a tile, the products of
+// S start from -infinity for what is hidden, so that the order is the same; a wavefront skips
+// tiles that none of its keys is seen from.
+// At head dim 128 the two accumulators take half of the registers, so V lies in LDS.
+#include "bsa_window_bwd.h"
+
+namespace bsa {
+
+namespace win {
+
+__device__ __forceinline__ int swz(int row, int chunk)
+{
+    return chunk ^ (((row & 3) << 1) | ((row >> 2) & 1));
+}
+
+// Tiles of ROWS token rows of one head, gathered into LDS by NW wavefronts: slab wave + NW i is 1 KiB,
+// lane l of it fills chunk l and fetches the channels that the swizzle puts there.
+template <int D, int ROWS, int NW>
+struct Gather {
+    static constexpr int ROW_BYTES = 2 * D, LPR = ROW_BYTES / 16, RPS = 1024 / ROW_BYTES;
+    static constexpr int BYTES = ROWS * ROW_BYTES, MINE = BYTES / 1024 / NW;
+    static_assert(RPS * NW % 8 == 0, "the slabs of a lane share its swizzled chunk");
+    // the first n <= ROWS rows from `first` on, of `stride` bytes; rows from n on repeat the last
+    static __device__ __forceinline__ void gather(const uint16_t* first, uint32_t stride, int n,
+                                                  uint32_t lds, int wave, int lane)
+    {
+        const i32x4 rsrc = buffer_desc(first, (uint32_t)(n - 1) * stride + ROW_BYTES);
+        const int x = RPS * wave + lane / LPR;
+        const uint32_t chunk = (uint32_t)swz(x, lane % LPR) * 16;
+        if (n == ROWS) {
+            const uint32_t voff = (uint32_t)x * stride + chunk;
+#pragma unroll
+            for (int i = 0; i < MINE; ++i)
+                load_lds_16(rsrc, voff, (uint32_t)(RPS * NW * i) * stride,
+                            lds + (uint32_t)(wave + NW * i) * 1024u);
+        } else {
+#pragma unroll
+            for (int i = 0; i < MINE; ++i)
+                load_lds_16(rsrc, (uint32_t)min(x + RPS * NW * i, n - 1) * stride + chunk, 0,
+                            lds + (uint32_t)(wave + NW * i) * 1024u);
+        }
+    }
+};
+
+__device__ __forceinline__ bf16x8 operand(const uint32_t (&w)[8], int h)
+{
+    return __builtin_bit_cast(bf16x8, make_uint4(w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]));
+}
+
+// D = 64: tiles of 64 tokens, V in registers.  D = 128: tiles of 32, V in LDS.
+template <int D>
+__global__ __launch_bounds__(256, 2) void window_dkdv_mfma_kernel(
+    const uint16_t* __restrict__ q, const uint16_t* __restrict__ k, const uint16_t* __restrict__ v,
+    const uint16_t* __restrict__ dout, const float* __restrict__ delta,
+    const float* __restrict__ lse2, uint16_t* __restrict__ dk, uint16_t* __restrict__ dv,
+    const Shape s, const Far far, uint32_t key_tiles, uint32_t items)
+{
+    constexpr int KS = D / 16, DT = D / 32, RT = D == 64 ? 64 : 32, ROW = 2 * D, TILE = RT * ROW;
+    constexpr int VB = D == 64 ? 16 : 32 * ROW;         // (no V in LDS at head dim 64)
+    using G = Gather<D, RT, 4>;
+    // [buffer][Q, dO]; the buffers alternate by bit 14 of the address
+    __shared__ __attribute__((aligned(32768))) unsigned char tiles_s[2][2][TILE];
+    __shared__ __attribute__((aligned(1024))) float rows_s[2][2][64];    // [buffer][lse, delta]
+    __shared__ __attribute__((aligned(1024))) unsigned char v_s[4][VB];
+
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int l32 = lane & 31, half = lane >> 5;
+
+    const uint32_t item = item_of(blockIdx.x, items);
+    const uint32_t slice = item / key_tiles;
+    const int key_tile = (int)(item - slice * key_tiles);
+    const int b = (int)(slice / (uint32_t)s.kv_heads), a = (int)(slice - (uint32_t)b * s.kv_heads);
+    int ql, kl;
+    lengths(s, b, ql, kl);
+    const int p0 = kl - ql;
+    const int J = key_tile * kKeys, jw = J + 32 * wave, j = jw + l32;
+    const Span span = near_span(s, J, kKeys, p0, ql, kl);
+    const int tiles = span.e > span.a ? (span.e - span.a + RT - 1) / RT : 0;
+    const int all = tiles * s.group;
+
+    auto issue = [&](int head, int t0, int buf) {
+        const int n = min(RT, span.e - t0);
+        G::gather(q + (int64_t)b * s.q.batch + (int64_t)head * s.q.head + (int64_t)t0 * s.q.token,
+                  (uint32_t)s.q.token * 2u, n, lds_address(tiles_s[buf][0]), wave, lane);
+        G::gather(dout + (int64_t)b * s.dout.batch + (int64_t)head * s.dout.head +
+                      (int64_t)t0 * s.dout.token,
+                  (uint32_t)s.dout.token * 2u, n, lds_address(tiles_s[buf][1]), wave, lane);
+        const int64_t at = ((int64_t)b * s.heads + head) * s.q_tokens + t0;
+        const uint32_t off = (uint32_t)min(lane, n - 1) * 4u;
+        if (wave == 0) load_lds_4(buffer_desc(lse2 + at, (uint32_t)n * 4u), off, 0, lds_address(rows_s[buf][0]));
+        if (wave == 3) load_lds_4(buffer_desc(delta + at, (uint32_t)n * 4u), off, 0, lds_address(rows_s[buf][1]));
+    };
+    int head = a * s.group, t0 = span.a;
+    if (all > 0) issue(head, t0, 0);
+
+    // K as operand; -V likewise, or to LDS.  The sign makes delta - dP of a product that starts
+    // from delta, so that -dS costs one product; it goes into the scale of dK.
+    bf16x8 kf[KS], vf[D == 64 ? KS : 1];
+    {
+        const bool here = is_seen(s, j, p0, ql, kl);
+        const uint16_t* kp = k + (int64_t)b * s.k.batch + (int64_t)a * s.k.head + (int64_t)j * s.k.token + 8 * half;
+        const uint16_t* vp = v + (int64_t)b * s.v.batch + (int64_t)a * s.v.head + (int64_t)j * s.v.token + 8 * half;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            kf[ks] = here ? *(const bf16x8*)(kp + 16 * ks) : bf16x8{};
+            const bf16x8 x = negated(here ? *(const bf16x8*)(vp + 16 * ks) : bf16x8{});
+            if constexpr (D == 64) vf[ks] = x;
+            else *(bf16x8*)(v_s[wave] + l32 * ROW + swz(l32, 2 * ks + half) * 16) = x;
+        }
+    }
+    const float c2 = s.scale * kLog2e;
+    f32x16 ak[DT], av[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) ak[dt] = av[dt] = splat(0.0f);
+
+    // addresses of this lane's fragments in the buffer that is read next
+    uint32_t row_at[4], v_at[4], tr_at[2], val_at;
+    {
+        const uint32_t base = lds_address(tiles_s), vbase = lds_address(v_s[wave]);
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+            const uint32_t at = (uint32_t)(l32 * ROW + swz(l32, 2 * ks + half) * 16);
+            row_at[ks] = base + at;
+            v_at[ks] = vbase + at;
+        }
+        const int s16 = lane & 15, gq4 = lane >> 4, r = 4 * (gq4 >> 1) + (s16 >> 2);
+#pragma unroll
+        for (int dt = 0; dt < 2; ++dt) {
+            const int col = 16 * (gq4 & 1) + 4 * (s16 & 3) + 32 * dt;
+            tr_at[dt] = base + (uint32_t)(r * ROW + swz(r, col >> 3) * 16 + (col & 7) * 2);
+        }
+        val_at = lds_address(rows_s) + 16u * (uint32_t)half;
+    }
+    auto row_frag = [&](int is_g, int row0, int ks) {
+        return lds_read<bf16x8>(row_at[ks & 3], is_g * TILE + row0 * ROW + (ks >> 2) * 128);
+    };
+    auto trans_frag = [&](int is_g, int row0, int dt) {
+        bf16x4 part[2];
+#pragma unroll
+        for (int rd = 0; rd < 2; ++rd)
+            part[rd] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+                (__attribute__((address_space(3))) bf16x4*)(uintptr_t)(
+                    tr_at[dt & 1] + (uint32_t)(is_g * TILE + (row0 + 8 * rd) * ROW + (dt >> 1) * 128)));
+        return __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+
+    // What S starts from: 0, and -infinity where the lane's key does not see the query, which
+    // makes the weight 0.
+    auto start_of = [&](bool full, const Column& col) {
+        f32x16 st = splat(0.0f);
+        if (!full) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                st[e] = col.seen(8 * (e >> 2) + (e & 3) + 4 * half) ? 0.0f : -INFINITY;
+        }
+        return st;
+    };
+    // One tile, D = 64: S, dP of tokens 0..31, then of 32..63 with the weights of the first half
+    // behind them, dV, dK of the first half with the weights of the second, dV, dK of the second.
+    auto tile64 = [&](f32x16 (&st)[2]) {
+        constexpr int W = 8;                            // fragments read ahead
+        auto read_frag = [&](int i) -> bf16x8 {
+            const int u = i & 3;
+            if (i < 16) return row_frag((i >> 2) & 1, 32 * (i >> 3), u);
+            return trans_frag(1 - ((i >> 2) & 1), 32 * ((i - 16) >> 3) + 16 * (u >> 1), u & 1);
+        };
+        bf16x8 f[W];
+        f32x16 dp[2];
+        f32x4 l4[4];
+        uint32_t pw[2][8], dw[2][8];
+        float fm[2][2], ex[2][2];
+        auto read_delta = [&](int qt) {
+#pragma unroll
+            for (int r4 = 0; r4 < 4; ++r4) {
+                const f32x4 d4 = lds_read<f32x4>(val_at, 256 + 128 * qt + 32 * r4);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) dp[qt][4 * r4 + r] = d4[r];
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = read_frag(i);
+        read_delta(0);
+#pragma unroll
+        for (int i = 4; i < W; ++i) f[i] = read_frag(i);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            const int u = i & 3;
+            const bf16x8 x = f[i % W];
+            if (i < 16) {
+                const int qt = i >> 3;
+                if ((i & 4) == 0)
+                    st[qt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, kf[u], st[qt], 0, 0, 0);
+                else
+                    dp[qt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, vf[D == 64 ? u : 0], dp[qt], 0, 0, 0);
+            } else {
+                const int qt = (i - 16) >> 3, h = u >> 1, dt = u & 1;
+                if ((i & 4) == 0)
+                    av[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, operand(pw[qt], h), av[dt], 0, 0, 0);
+                else
+                    ak[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, operand(dw[qt], h), ak[dt], 0, 0, 0);
+            }
+            if (i + W < 32) f[i % W] = read_frag(i + W);
+            // lse of the queries whose weights come next, delta of the second half
+            if (i >= 3 && i < 7) l4[i - 3] = lds_read<f32x4>(val_at, 32 * (i - 3));
+            if (i == 7) read_delta(1);
+            if (i >= 10 && i < 18 && (i & 1) == 0)
+                l4[(i - 10) >> 1] = lds_read<f32x4>(val_at, 128 + 32 * ((i - 10) >> 1));
+            // two weights to a slot: exponentials, the fma of the next two, products and packs of
+            // the two before
+            if (i >= 7 && i < 23) {
+                const int qt = (i - 7) >> 3, e = 2 * ((i - 7) & 7);
+                fm[(i + 1) & 1][0] = fmaf(st[qt][e], c2, -l4[e >> 2][e & 3]);
+                fm[(i + 1) & 1][1] = fmaf(st[qt][e + 1], c2, -l4[e >> 2][(e & 3) + 1]);
+                asm volatile("" : "+v"(fm[(i + 1) & 1][0]), "+v"(fm[(i + 1) & 1][1]));
+            }
+            if (i >= 8 && i < 24) {
+                ex[i & 1][0] = __builtin_amdgcn_exp2f(fm[i & 1][0]);
+                ex[i & 1][1] = __builtin_amdgcn_exp2f(fm[i & 1][1]);
+                asm volatile("" : "+v"(ex[i & 1][0]), "+v"(ex[i & 1][1]));
+            }
+            if (i >= 9 && i < 25) {
+                const int qt = (i - 9) >> 3, e = 2 * ((i - 9) & 7), o = (i - 1) & 1;
+                pw[qt][e >> 1] = pack_bf16(ex[o][0], ex[o][1]);
+                dw[qt][e >> 1] = pack_bf16(ex[o][0] * dp[qt][e], ex[o][1] * dp[qt][e + 1]);
+                asm volatile("" : "+v"(pw[qt][e >> 1]), "+v"(dw[qt][e >> 1]));
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // One tile, D = 128: S, dP, dV, dK; exponentials behind dP, products behind dV.
+    auto tile128 = [&](f32x16 st) {
+        constexpr int W = 6;
+        // 0-7 Q rows (S), 8-23 dO rows and V in turn (dP), 24-31 dO transposed (dV), 32-39 Q (dK)
+        auto read_frag = [&](int i) -> bf16x8 {
+            if (i < 8) return row_frag(0, 0, i);
+            if (i < 24) {
+                const int ks = (i - 8) >> 1;
+                if (i & 1) return lds_read<bf16x8>(v_at[ks & 3], (ks >> 2) * 128);
+                return row_frag(1, 0, ks);
+            }
+            return trans_frag(i < 32, 16 * ((i >> 2) & 1), i & 3);
+        };
+        bf16x8 f[W];
+        f32x16 dp;
+        f32x4 l4[2];
+        uint32_t pw[8], dw[8];
+        float fm[2][2];
+#pragma unroll
+        for (int i = 0; i < W; ++i) f[i] = read_frag(i);
+        __builtin_amdgcn_sched_barrier(0);
+        auto ask = [&](int i) {
+            if (i + W < 40) f[i % W] = read_frag(i + W);
+        };
+#pragma unroll
+        for (int t = 0; t < 32; ++t) {
+            const int i = t & 7, h = i >> 2, dt = i & 3;
+            if (t < 8) {
+                st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % W], kf[i % KS], st, 0, 0, 0);
+                ask(i);
+            } else if (t < 16) {
+                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[(8 + 2 * i) % W], f[(9 + 2 * i) % W], dp, 0, 0, 0);
+                ask(8 + 2 * i);
+                ask(9 + 2 * i);
+            } else if (t < 24) {
+                av[dt % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[(24 + i) % W], operand(pw, h), av[dt % DT], 0, 0, 0);
+                ask(24 + i);
+            } else {
+                ak[dt % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[(32 + i) % W], operand(dw, h), ak[dt % DT], 0, 0, 0);
+                ask(32 + i);
+            }
+            if (t >= 2 && t < 6) {
+                const f32x4 d4 = lds_read<f32x4>(val_at, 256 + 32 * (t - 2));
+#pragma unroll
+                for (int r = 0; r < 4; ++r) dp[4 * (t - 2) + r] = d4[r];
+            }
+            if (t == 6 || t == 7) l4[t - 6] = lds_read<f32x4>(val_at, 32 * (t - 6));
+            if (t >= 10 && t < 18) {
+                const int e = 2 * (t - 10);
+                st[e] = __builtin_amdgcn_exp2f(fm[t & 1][0]);
+                st[e + 1] = __builtin_amdgcn_exp2f(fm[t & 1][1]);
+                pw[e >> 1] = pack_bf16(st[e], st[e + 1]);
+                asm volatile("" : "+v"(pw[e >> 1]));
+            }
+            if (t >= 9 && t < 17) {
+                const int e = 2 * (t - 9);
+                fm[(t + 1) & 1][0] = fmaf(st[e], c2, -l4[(e >> 2) & 1][e & 3]);
+                fm[(t + 1) & 1][1] = fmaf(st[e + 1], c2, -l4[(e >> 2) & 1][(e & 3) + 1]);
+                asm volatile("" : "+v"(fm[(t + 1) & 1][0]), "+v"(fm[(t + 1) & 1][1]));
+            }
+            if (t == 10 || t == 12) l4[(t - 10) >> 1] = lds_read<f32x4>(val_at, 64 + 16 * (t - 10));
+            if (t >= 18 && t < 26) {
+                const int e = 2 * (t - 18);
+                dw[e >> 1] = pack_bf16(st[e] * dp[e], st[e + 1] * dp[e + 1]);
+                asm volatile("" : "+v"(dw[e >> 1]));
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+
+    for (int it = 0; it < all; ++it) {
+        // tile `it` has landed and everyone is done with the other buffer
+        wait_gathers();
+        __syncthreads();
+        int next_head = head, next_t0 = t0 + RT;
+        if (next_t0 >= span.e) { ++next_head; next_t0 = span.a; }
+        if (it + 1 < all) issue(next_head, next_t0, (it + 1) & 1);
+        const int n = min(RT, span.e - t0), pa = p0 + t0;
+        const bool any = jw < kl && jw <= pa + n - 1 + s.right && (jw + 31 >= pa - s.left || jw < s.sinks);
+        const bool full = n == RT && jw + 31 < kl && jw + 31 <= pa + s.right &&
+                          (jw >= pa + RT - 1 - s.left || jw + 31 < s.sinks);
+        if (any) {
+            if constexpr (D == 64) {
+                f32x16 st[2] = {start_of(full, column(s, j, kl, pa, n)),
+                                start_of(full, column(s, j, kl, pa + 32, n - 32))};
+                tile64(st);
+            } else {
+                tile128(start_of(full, column(s, j, kl, pa, n)));
+            }
+        }
+        head = next_head;
+        t0 = next_t0;
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) row_at[ks] ^= 16384u;
+        tr_at[0] ^= 16384u; tr_at[1] ^= 16384u;
+        val_at ^= 512u;
+    }
+    if (jw / 32 < far.groups) add_far<D>(far, slice, jw / 32, l32, half, ak, av, -1.0f);
+    if (j < s.k_tokens) {
+        store_lane_row<uint16_t, D>(dk + (int64_t)b * s.dk.batch + (int64_t)a * s.dk.head +
+                                        (int64_t)j * s.dk.token, ak, -s.scale, half);
+        store_lane_row<uint16_t, D>(dv + (int64_t)b * s.dv.batch + (int64_t)a * s.dv.head +
+                                        (int64_t)j * s.dv.token, av, 1.0f, half);
+    }
+}
+
+}  // namespace win
+
+bool window_bwd_mfma_supported(bool is_bf16, int D, const win::Shape& s)
+{
+    // 64 rows of a tile are reached by 32-bit offsets
+    const int64_t most = (int64_t)1 << 24;
+    return is_bf16 && (D == 64 || D == 128) && s.q.token < most && s.dout.token < most;
+}
+
+hipError_t launch_window_dkdv_mfma(int D, const win::Shape& s, const void* q, const void* k,
+                                   const void* v, const void* dout, const float* delta,
+                                   const float* lse2, void* dk, void* dv, const win::Far& far,
+                                   hipStream_t stream)
+{
+    using namespace win;
+    const uint32_t key_tiles = ((uint32_t)s.k_tokens + kKeys - 1) / kKeys;
+    const uint32_t items = (uint32_t)(s.batch * s.kv_heads) * key_tiles;
+    auto kernel = D == 64 ? window_dkdv_mfma_kernel<64> : window_dkdv_mfma_kernel<128>;
+    kernel<<<items, 256, 0, stream>>>((const uint16_t*)q, (const uint16_t*)k, (const uint16_t*)v,
+                                      (const uint16_t*)dout, delta, lse2, (uint16_t*)dk, (uint16_t*)dv,
+                                      s, far, key_tiles, items);
+    return hipGetLastError();
+}
+
+}  // namespace bsa

@@ -259,3 +259,15 @@ def test_rows_far_into_a_long_cache():
             r = attention(q[0, i].double(), k64, v64, see, 1.0 / math.sqrt(D))
             d = (out[0, i].cpu().double() - r["out"]).abs()
             assert bool((d <= r["out_tol"](BF16)).all())
+
+
+@DTYPES
+@pytest.mark.parametrize("D", [32, 64, 128])
+@pytest.mark.parametrize("h,kv,left,right,sinks", [(4, 1, 100, 0, 4), (3, 1, 70, 50, 33), (1, 1, 300, 0, 200)])
+def test_many_key_tiles(dtype, D, h, kv, left, right, sinks):
+    """Batches that fill the chip: 128 keys to a workgroup in the backward."""
+    n = 389
+    B = 64 // kv + 1
+    run(dtype, B, h, kv, n, n, D, left, right, sinks, train=True, seed=D + left,
+        q_lens=[n - (i * 37) % n if i % 3 else n for i in range(B)],
+        k_lens=[n - (i * 23) % 350 if i % 2 else n for i in range(B)])
