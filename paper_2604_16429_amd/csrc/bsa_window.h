@@ -50,11 +50,7 @@ __device__ __forceinline__ void lengths(const Shape& s, int b, int& ql, int& kl)
 struct KeyList {
     int sinks, lo, count;
     int row_lo, rows, ring;            // row of token lo; rows of the cache
-    __device__ __forceinline__ int token(int slot) const
-    {
-        return slot < sinks ? slot : slot - sinks + lo;
-    }
-    // Row of k and v that holds it.  The tokens from lo on are at most `ring`, or none of
+    // Row of k and v that holds a slot's token.  The tokens from lo on are at most `ring`, or none of
     // them is past the first turn of the ring: there is one wrap at most.
     __device__ __forceinline__ int row(int slot) const
     {
@@ -77,19 +73,50 @@ __device__ __forceinline__ KeyList key_list(const Shape& s, int first, int last,
     return l;
 }
 
-// What one query sees: tokens lo .. hi and those below sinks, up to hi.
+// What one query sees, in slots of a key list that holds all of it: slots below `sinks` and
+// those with (unsigned)(slot - first) <= span.
 struct Sight {
-    int lo, hi;
-    __device__ __forceinline__ bool sees(const Shape& s, int j) const
+    int sinks, first;
+    uint32_t span;
+    __device__ __forceinline__ bool sees(int slot) const
     {
-        return j <= hi && (j >= lo || j < s.sinks);
+        return slot < sinks || (uint32_t)(slot - first) <= span;
     }
 };
-__device__ __forceinline__ Sight sight(const Shape& s, int p, int kl, bool valid)
+__device__ __forceinline__ Sight sight(const Shape& s, const KeyList& keys, int p, int kl, bool valid)
 {
+    const int hi = valid ? min(kl - 1, p + s.right) : -1, lo = max(0, p - s.left);
     Sight v;
-    v.hi = valid ? min(kl - 1, p + s.right) : -1;
-    v.lo = p - s.left;
+    v.sinks = min(s.sinks, hi + 1);
+    v.first = hi >= lo ? lo - keys.lo + keys.sinks : 1 << 30;
+    v.span = hi >= lo ? (uint32_t)(hi - lo) : 0u;
+    return v;
+}
+
+// What rows r0 .. r0 + n - 1 of a slice see: some of them slots below `sinks` and any_a .. any_e, all
+// of them all_a .. all_e.
+struct RowsSight {
+    int sinks, any_a, any_e, all_a, all_e;
+    __device__ __forceinline__ bool any(int slot, int n) const
+    {
+        return slot < sinks || (slot <= any_e && slot + n - 1 >= any_a);
+    }
+    __device__ __forceinline__ bool all(int slot, int n) const
+    {
+        return slot >= all_a && slot + n - 1 <= all_e;
+    }
+};
+__device__ __forceinline__ RowsSight rows_sight(const Shape& s, const KeyList& keys, int r0, int n,
+                                                int p0, int ql, int kl)
+{
+    const int first = r0 / s.group, end = (r0 + n - 1) / s.group, last = min(end, ql - 1);
+    const int shift = keys.sinks - keys.lo;
+    RowsSight v;
+    v.any_a = max(0, p0 + first - s.left) + shift;
+    v.any_e = first < ql ? min(kl - 1, p0 + last + s.right) + shift : -1;
+    v.sinks = first < ql ? min(s.sinks, p0 + last + s.right + 1) : 0;
+    v.all_a = max(0, p0 + end - s.left) + shift;
+    v.all_e = end < ql && r0 + n <= s.rows ? min(kl - 1, p0 + first + s.right) + shift : -1;
     return v;
 }
 

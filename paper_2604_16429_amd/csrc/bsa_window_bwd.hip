@@ -3,8 +3,8 @@
 // With P = exp(scale q.k - lse) recomputed and delta = dO . O for each query,
 //   dV_j = sum_i P_ij dO_i    dS_ij = P_ij (dO_i . v_j - delta_i)
 //   dQ_i = scale sum_j dS_ij k_j    dK_j = scale sum_i dS_ij q_i
-// Launches: delta and lse in base 2 by row; dQ, which walks the keys of 128 rows as the forward
-// does; dK and dV, where a wavefront owns 32 keys and walks the queries that see them, in tiles
+// Launches: dQ, which walks the keys of 128 rows as the forward does and leaves delta and lse in base
+// 2 of each row; dK and dV, where a wavefront owns 32 keys and walks the queries that see them, in tiles
 // of consecutive tokens of one head, the heads of the group one after the other.  Every sum has
 // one fixed order and no atomics.
 //
@@ -21,54 +21,11 @@ namespace bsa {
 namespace win {
 
 template <typename T, int D>
-__global__ __launch_bounds__(256) void window_rows_kernel(const T* __restrict__ out,
-                                                          const T* __restrict__ dout,
-                                                          const float* __restrict__ lse,
-                                                          float* __restrict__ delta,
-                                                          float* __restrict__ lse2, const Shape s,
-                                                          int64_t all_rows)
-{
-    constexpr int LANES = D * sizeof(T) / 16, V = 16 / sizeof(T);
-    const int part = threadIdx.x % LANES;
-    const int64_t step = (int64_t)gridDim.x * (256 / LANES);
-    // (the bound is the same for all lanes of a wavefront, which meet in the sums)
-    for (int64_t at0 = (int64_t)blockIdx.x * (256 / LANES); at0 < all_rows; at0 += step) {
-        const int64_t at = at0 + threadIdx.x / LANES;
-        const bool here = at < all_rows;
-        const int64_t slice = here ? at / s.rows : 0;
-        const int row = here ? (int)(at - slice * s.rows) : 0;
-        const int b = (int)(slice / s.kv_heads), a = (int)(slice - (int64_t)b * s.kv_heads);
-        const int tok = row / s.group, head = a * s.group + (row - tok * s.group);
-        const bool valid = here && tok < query_length(s, b);
-        float d = 0.0f;
-        if (valid) {
-            const T* o = out + (int64_t)b * s.out.batch + (int64_t)head * s.out.head +
-                         (int64_t)tok * s.out.token + V * part;
-            const T* g = dout + (int64_t)b * s.dout.batch + (int64_t)head * s.dout.head +
-                         (int64_t)tok * s.dout.token + V * part;
-#pragma unroll
-            for (int i = 0; i < V; i += 4) {
-                const float4 x = load4(o + i), y = load4(g + i);
-                d += x.x * y.x + x.y * y.y + x.z * y.z + x.w * y.w;
-            }
-        }
-#pragma unroll
-        for (int o = 1; o < LANES; o <<= 1) d += __shfl_xor(d, o);
-        if (here && part == 0) {
-            const float l =
-                valid ? lse[((int64_t)b * s.heads + head) * s.q_tokens + tok] : -INFINITY;
-            const int64_t to = ((int64_t)b * s.heads + head) * s.q_tokens + tok;
-            delta[to] = d;
-            lse2[to] = l == -INFINITY ? kNoWeight : l * kLog2e;
-        }
-    }
-}
-
-template <typename T, int D>
 __global__ __launch_bounds__(256) void window_dq_kernel(
     const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
-    const T* __restrict__ dout, const float* __restrict__ delta, const float* __restrict__ lse2,
-    T* __restrict__ dq, const Shape s, uint32_t row_tiles, uint32_t items)
+    const T* __restrict__ out, const float* __restrict__ lse, const T* __restrict__ dout,
+    float* __restrict__ delta, float* __restrict__ lse2, T* __restrict__ dq, const Shape s,
+    uint32_t row_tiles, uint32_t items)
 {
     constexpr int KT = sizeof(T) == 2 ? 64 : 32;
     constexpr int KS = D / 16, DT = D / 32;
@@ -93,16 +50,12 @@ __global__ __launch_bounds__(256) void window_dq_kernel(
     const int row = row0 + 32 * wave + l32;
     const int tok = row / s.group, head = a * s.group + (row - tok * s.group);
     const bool exists = row < s.rows, valid = exists && tok < ql;
-    const Sight see = sight(s, p0 + tok, kl, valid);
 
     const int t_first = row0 / s.group, t_last = min((row0 + 127) / s.group, ql - 1);
     KeyList keys = {};
     if (t_first <= t_last) keys = key_list(s, p0 + t_first, p0 + t_last, kl);
-    const int w_first = (row0 + 32 * wave) / s.group, w_end = (row0 + 32 * wave + 31) / s.group;
-    const int w_last = min(w_end, ql - 1);
-    const int w_lo = p0 + w_first - s.left, w_hi = min(kl - 1, p0 + w_last + s.right);
-    const int all_lo = p0 + w_end - s.left, all_hi = min(kl - 1, p0 + w_first + s.right);
-    const bool all_valid = w_end < ql && row0 + 32 * wave + 31 < s.rows;
+    const Sight see = sight(s, keys, p0 + tok, kl, valid);
+    const RowsSight rows = rows_sight(s, keys, row0 + 32 * wave, 32, p0, ql, kl);
 
     const T* kb = k + (int64_t)b * s.k.batch + (int64_t)a * s.k.head;
     const T* vb = v + (int64_t)b * s.v.batch + (int64_t)a * s.v.head;
@@ -113,15 +66,27 @@ __global__ __launch_bounds__(256) void window_dq_kernel(
         const T* p = q + (int64_t)b * s.q.batch + (int64_t)head * s.q.head + (int64_t)tok * s.q.token;
         const T* g = dout + (int64_t)b * s.dout.batch + (int64_t)head * s.dout.head +
                      (int64_t)tok * s.dout.token;
+        const T* o = out + (int64_t)b * s.out.batch + (int64_t)head * s.out.head +
+                     (int64_t)tok * s.out.token;
+        float d = 0.0f;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             qf[ks] = valid ? M::load(p + 16 * ks + 8 * half) : Frag{};
             gf[ks] = valid ? M::load(g + 16 * ks + 8 * half) : Frag{};
+            const Frag of = valid ? M::load(o + 16 * ks + 8 * half) : Frag{};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) d = fmaf((float)gf[ks][i], (float)of[i], d);
         }
+        d += swap32(d);
         if (valid) {
-            const int64_t from = ((int64_t)b * s.heads + head) * s.q_tokens + tok;
-            neg_l2 = -lse2[from];
-            neg_delta = -delta[from];
+            const int64_t at = ((int64_t)b * s.heads + head) * s.q_tokens + tok;
+            const float l = lse[at], l2 = l == -INFINITY ? kNoWeight : l * kLog2e;
+            if (half == 0) {
+                delta[at] = d;
+                lse2[at] = l2;
+            }
+            neg_l2 = -l2;
+            neg_delta = -d;
         }
     }
     const float c2 = s.scale * kLog2e;
@@ -133,11 +98,11 @@ __global__ __launch_bounds__(256) void window_dq_kernel(
     auto fetch = [&](int slot0) {
         kt.fetch(tid, [&](int r) -> const T* {
             const int slot = slot0 + r;
-            return slot < keys.count ? kb + (int64_t)keys.token(slot) * s.k.token : nullptr;
+            return slot < keys.count ? kb + (int64_t)keys.row(slot) * s.k.token : nullptr;
         });
         vt.fetch(tid, [&](int r) -> const T* {
             const int slot = slot0 + r;
-            return slot < keys.count ? vb + (int64_t)keys.token(slot) * s.v.token : nullptr;
+            return slot < keys.count ? vb + (int64_t)keys.row(slot) * s.v.token : nullptr;
         });
     };
     if (keys.count > 0) fetch(0);
@@ -149,11 +114,9 @@ __global__ __launch_bounds__(256) void window_dq_kernel(
         if (slot0 + KT < keys.count) fetch(slot0 + KT);
 #pragma unroll
         for (int hh = 0; hh < KT / 32; ++hh) {
-            const int s0 = slot0 + 32 * hh, j0 = s0 - keys.sinks + keys.lo;
-            const bool plain = s0 >= keys.sinks;
-            if (s0 >= keys.count || (plain && (j0 > w_hi || (j0 + 31 < w_lo && j0 >= s.sinks))))
-                continue;
-            const bool full = plain && all_valid && j0 >= all_lo && j0 + 31 <= all_hi;
+            const int s0 = slot0 + 32 * hh;
+            if (s0 >= keys.count || !rows.any(s0, 32)) continue;
+            const bool full = rows.all(s0, 32);
             f32x16 st = splat(0.0f), dp = splat(neg_delta);
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
@@ -165,7 +128,7 @@ __global__ __launch_bounds__(256) void window_dq_kernel(
                 float ds = __builtin_amdgcn_exp2f(fmaf(st[r], c2, neg_l2)) * dp[r];
                 if (!full) {
                     const int slot = s0 + 8 * (r >> 2) + 4 * half + (r & 3);
-                    ds = slot < keys.count && see.sees(s, keys.token(slot)) ? ds : 0.0f;
+                    ds = see.sees(slot) ? ds : 0.0f;
                 }
                 st[r] = ds;
             }
@@ -497,19 +460,17 @@ hipError_t launch_bwd(const Shape& s, const void* q_, const void* k_, const void
     Far far = far_of(s);
     far.sums = (float*)((char*)workspace + 2 * row_bytes(s));
 
-    const int64_t all_rows = slices * s.rows;
-    const int rows_per = 256 / (D * (int)sizeof(T) / 16);
-    const int64_t row_groups = (all_rows + rows_per - 1) / rows_per;
-    window_rows_kernel<T, D><<<(unsigned)min(row_groups, (int64_t)1 << 20), 256, 0, stream>>>(
-        out, dout, lse, delta, lse2, s, all_rows);
-    hipError_t e = hipGetLastError();
+    hipError_t e;
+    if (window_bwd_mfma_supported(sizeof(T) == 2, D, s)) {
+        e = launch_window_dq_mfma(D, s, q, k, v, out, lse, dout, delta, lse2, dq, stream);
+    } else {
+        const uint32_t row_tiles = ((uint32_t)s.rows + 127) / 128;
+        const uint32_t q_items = row_tiles * (uint32_t)slices;
+        window_dq_kernel<T, D><<<q_items, 256, 0, stream>>>(q, k, v, out, lse, dout, delta, lse2, dq, s,
+                                                           row_tiles, q_items);
+        e = hipGetLastError();
+    }
     if (e != hipSuccess) return e;
-
-    const uint32_t row_tiles = ((uint32_t)s.rows + 127) / 128;
-    const uint32_t q_items = row_tiles * (uint32_t)slices;
-    window_dq_kernel<T, D><<<q_items, 256, 0, stream>>>(q, k, v, dout, delta, lse2, dq, s, row_tiles,
-                                                       q_items);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
 
     if (far.groups) {
         const uint32_t n = (uint32_t)slices * (uint32_t)(far.groups * far.chunks);

@@ -1,7 +1,7 @@
-// Windowed attention backward, bf16, head dims 64 and 128: dK and dV of large launches (see
-// bsa_window_bwd.hip for the formulas and the other kernels).
+// Windowed attention backward, bf16, head dims 64 and 128 (see bsa_window_bwd.hip for the formulas
+// and the other kernels): dQ, and dK and dV of large launches.
 //
-// A workgroup of four wavefronts owns 128 keys, 32 to each, and walks the queries that see them
+// dK and dV: a workgroup of four wavefronts owns 128 keys, 32 to each, and walks the queries that see them
 // inside the window, head by head, in tiles of 64 (head dim 128: 32) tokens that are gathered
 // straight into LDS, double buffered, one barrier a tile.  Matrix instructions bound it; per 32
 // queries x 32 keys there are as many LDS bytes to read as the matrix unit takes time, and
@@ -13,49 +13,11 @@
 // tiles that none of its keys is seen from.
 // At head dim 128 the two accumulators take half of the registers, so V lies in LDS.
 #include "bsa_window_bwd.h"
+#include "bsa_window_mfma.h"
 
 namespace bsa {
 
 namespace win {
-
-__device__ __forceinline__ int swz(int row, int chunk)
-{
-    return chunk ^ (((row & 3) << 1) | ((row >> 2) & 1));
-}
-
-// Tiles of ROWS token rows of one head, gathered into LDS by NW wavefronts: slab wave + NW i is 1 KiB,
-// lane l of it fills chunk l and fetches the channels that the swizzle puts there.
-template <int D, int ROWS, int NW>
-struct Gather {
-    static constexpr int ROW_BYTES = 2 * D, LPR = ROW_BYTES / 16, RPS = 1024 / ROW_BYTES;
-    static constexpr int BYTES = ROWS * ROW_BYTES, MINE = BYTES / 1024 / NW;
-    static_assert(RPS * NW % 8 == 0, "the slabs of a lane share its swizzled chunk");
-    // the first n <= ROWS rows from `first` on, of `stride` bytes; rows from n on repeat the last
-    static __device__ __forceinline__ void gather(const uint16_t* first, uint32_t stride, int n,
-                                                  uint32_t lds, int wave, int lane)
-    {
-        const i32x4 rsrc = buffer_desc(first, (uint32_t)(n - 1) * stride + ROW_BYTES);
-        const int x = RPS * wave + lane / LPR;
-        const uint32_t chunk = (uint32_t)swz(x, lane % LPR) * 16;
-        if (n == ROWS) {
-            const uint32_t voff = (uint32_t)x * stride + chunk;
-#pragma unroll
-            for (int i = 0; i < MINE; ++i)
-                load_lds_16(rsrc, voff, (uint32_t)(RPS * NW * i) * stride,
-                            lds + (uint32_t)(wave + NW * i) * 1024u);
-        } else {
-#pragma unroll
-            for (int i = 0; i < MINE; ++i)
-                load_lds_16(rsrc, (uint32_t)min(x + RPS * NW * i, n - 1) * stride + chunk, 0,
-                            lds + (uint32_t)(wave + NW * i) * 1024u);
-        }
-    }
-};
-
-__device__ __forceinline__ bf16x8 operand(const uint32_t (&w)[8], int h)
-{
-    return __builtin_bit_cast(bf16x8, make_uint4(w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]));
-}
 
 // D = 64: tiles of 64 tokens, V in registers.  D = 128: tiles of 32, V in LDS.
 template <int D>
@@ -345,13 +307,225 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_mfma_kernel(
     }
 }
 
+// dQ of 128 rows: four wavefronts of 32 share tiles of 64 keys, double buffered.  It also leaves
+// delta = dO . O and lse in base 2 for the kernels of dK and dV.
+template <int D>
+__global__ __launch_bounds__(256, 2) void window_dq_mfma_kernel(
+    const uint16_t* __restrict__ q, const uint16_t* __restrict__ k, const uint16_t* __restrict__ v,
+    const uint16_t* __restrict__ out, const float* __restrict__ lse,
+    const uint16_t* __restrict__ dout, float* __restrict__ delta, float* __restrict__ lse2,
+    uint16_t* __restrict__ dq, const Shape s, uint32_t row_tiles, uint32_t items)
+{
+    constexpr int KS = D / 16, DT = D / 32, ROW = 2 * D, TILE = 64 * ROW;
+    using G = KeyGather<D, 64, 4>;
+    // [buffer][K, V]
+    __shared__ __attribute__((aligned(4 * TILE))) unsigned char tiles_s[2][2][TILE];
+
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int l32 = lane & 31, half = lane >> 5;
+
+    const uint32_t item = item_of(blockIdx.x, items);
+    const uint32_t slice = item / row_tiles;
+    const int row0 = (int)(item - slice * row_tiles) * 128;
+    const int b = (int)(slice / (uint32_t)s.kv_heads), a = (int)(slice - (uint32_t)b * s.kv_heads);
+    int ql, kl;
+    lengths(s, b, ql, kl);
+    const int p0 = kl - ql;
+    const int t_first = row0 / s.group, t_last = min((row0 + 127) / s.group, ql - 1);
+    KeyList keys = {};
+    if (t_first <= t_last) keys = key_list(s, p0 + t_first, p0 + t_last, kl);
+    const int tiles = (keys.count + 63) / 64;
+
+    const uint32_t k_stride = (uint32_t)s.k.token * 2u, v_stride = (uint32_t)s.v.token * 2u;
+    const i32x4 k_rsrc = buffer_desc(k + (int64_t)b * s.k.batch + (int64_t)a * s.k.head,
+                                     (uint32_t)(s.k_tokens - 1) * k_stride + ROW);
+    const i32x4 v_rsrc = buffer_desc(v + (int64_t)b * s.v.batch + (int64_t)a * s.v.head,
+                                     (uint32_t)(s.k_tokens - 1) * v_stride + ROW);
+    auto issue = [&](int c) {
+        G::gather(k_rsrc, k_stride, keys, 64 * c, lds_address(tiles_s[c & 1][0]), wave, lane);
+        G::gather(v_rsrc, v_stride, keys, 64 * c, lds_address(tiles_s[c & 1][1]), wave, lane);
+    };
+    if (tiles > 0) issue(0);
+
+    const int row = row0 + 32 * wave + l32;
+    const int tok = row / s.group, head = a * s.group + (row - tok * s.group);
+    const bool valid = row < s.rows && tok < ql;
+    const Sight see = sight(s, keys, p0 + tok, kl, valid);
+    const RowsSight rows = rows_sight(s, keys, row0 + 32 * wave, 32, p0, ql, kl);
+    bf16x8 qf[KS], gf[KS];
+    float neg_l2 = -kNoWeight, neg_delta = 0.0f;
+    {
+        const uint16_t* qp = q + (int64_t)b * s.q.batch + (int64_t)head * s.q.head + (int64_t)tok * s.q.token + 8 * half;
+        const uint16_t* gp = dout + (int64_t)b * s.dout.batch + (int64_t)head * s.dout.head +
+                             (int64_t)tok * s.dout.token + 8 * half;
+        const uint16_t* op = out + (int64_t)b * s.out.batch + (int64_t)head * s.out.head +
+                             (int64_t)tok * s.out.token + 8 * half;
+        float d = 0.0f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            qf[ks] = valid ? *(const bf16x8*)(qp + 16 * ks) : bf16x8{};
+            gf[ks] = valid ? *(const bf16x8*)(gp + 16 * ks) : bf16x8{};
+            const bf16x8 o = valid ? *(const bf16x8*)(op + 16 * ks) : bf16x8{};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) d = fmaf((float)gf[ks][i], (float)o[i], d);
+        }
+        d += swap32(d);
+        if (valid) {
+            const int64_t at = ((int64_t)b * s.heads + head) * s.q_tokens + tok;
+            const float l = lse[at], l2 = l == -INFINITY ? kNoWeight : l * kLog2e;
+            if (half == 0) {
+                delta[at] = d;
+                lse2[at] = l2;
+            }
+            neg_l2 = -l2;
+            neg_delta = -d;
+        }
+    }
+    const float c2 = s.scale * kLog2e;
+    // dP^T starts from -delta, which leaves one product for dS^T = P^T (dP^T - delta)
+    const f32x16 neg_dl = splat(neg_delta);
+    f32x16 acc[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) acc[dt] = splat(0.0f);
+
+    uint32_t row_at[4], tr_at[2];
+    {
+        const uint32_t base = lds_address(tiles_s);
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) row_at[ks] = base + (uint32_t)(l32 * ROW + swz(l32, 2 * ks + half) * 16);
+        const int s16 = lane & 15, gq4 = lane >> 4, r = 4 * (gq4 >> 1) + (s16 >> 2);
+#pragma unroll
+        for (int dt = 0; dt < 2; ++dt) {
+            const int col = 16 * (gq4 & 1) + 4 * (s16 & 3) + 32 * dt;
+            tr_at[dt] = base + (uint32_t)(r * ROW + swz(r, col >> 3) * 16 + (col & 7) * 2);
+        }
+    }
+    auto row_frag = [&](int is_v, int r0, int ks) {
+        return lds_read<bf16x8>(row_at[ks & 3], is_v * TILE + r0 * ROW + (ks >> 2) * 128);
+    };
+    auto trans_frag = [&](int r0, int dt) {
+        bf16x4 part[2];
+#pragma unroll
+        for (int rd = 0; rd < 2; ++rd)
+            part[rd] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+                (__attribute__((address_space(3))) bf16x4*)(uintptr_t)(
+                    tr_at[dt & 1] + (uint32_t)((r0 + 8 * rd) * ROW + (dt >> 1) * 128)));
+        return __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+
+    // One tile of 64 keys: S^T and dP^T of both halves, then dQ^T += K^T dS^T of both; behind dP of a
+    // half go its exponentials, behind what follows the products.  Fragments are read W ahead.
+    auto tile = [&](f32x16 (&st)[2]) {
+        constexpr int W = 8, N = KS, ALL = 4 * N + 4 * DT;       // matrix instructions
+        auto read_frag = [&](int i) -> bf16x8 {
+            if (i < 4 * N) return row_frag((i / N) & 1, 32 * (i / (2 * N)), i % N);
+            const int u = i - 4 * N;
+            return trans_frag(32 * (u / (2 * DT)) + 16 * ((u / DT) & 1), u % DT);
+        };
+        bf16x8 f[W];
+        f32x16 dp[2];
+        uint32_t w[2][8];
+        float fm[2][2];
+#pragma unroll
+        for (int i = 0; i < W; ++i) f[i] = read_frag(i);
+        __builtin_amdgcn_sched_barrier(0);
+        // two weights to a slot at head dim 128, four at 64: the fma from slot F on, exponentials a
+        // slot later, products from slot X on
+        constexpr int PER = 16 / N, F = N + 1, X = 2 * N + 2;
+#pragma unroll
+        for (int t = 0; t < ALL; ++t) {
+            if (t < 4 * N) {
+                const int hh = t / (2 * N), u = t % N;
+                if ((t / N) & 1)
+                    dp[hh] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[t % W], gf[u], u == 0 ? neg_dl : dp[hh], 0, 0, 0);
+                else
+                    st[hh] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[t % W], qf[u], st[hh], 0, 0, 0);
+            } else {
+                const int u = t - 4 * N, hh = u / (2 * DT), h = (u / DT) & 1, dt = u % DT;
+                acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[t % W], operand(w[hh], h), acc[dt], 0, 0, 0);
+            }
+            if (t + W < ALL) f[t % W] = read_frag(t + W);
+#pragma unroll
+            for (int p = 0; p < PER; p += 2) {
+                {
+                    const int hh = t >= F + 2 * N ? 1 : 0, e = PER * (t - F - 2 * N * hh - 1) + p;
+                    if (e >= 0 && e < 16 && t > F) {
+                        st[hh][e] = __builtin_amdgcn_exp2f(PER == 2 ? fm[t & 1][0] : st[hh][e]);
+                        st[hh][e + 1] = __builtin_amdgcn_exp2f(PER == 2 ? fm[t & 1][1] : st[hh][e + 1]);
+                        asm volatile("" : "+v"(st[hh][e]), "+v"(st[hh][e + 1]));
+                    }
+                }
+                {
+                    const int hh = t >= F + 2 * N ? 1 : 0, e = PER * (t - F - 2 * N * hh) + p;
+                    if (e >= 0 && e < 16) {
+                        const float f0 = fmaf(st[hh][e], c2, neg_l2), f1 = fmaf(st[hh][e + 1], c2, neg_l2);
+                        if (PER == 2) {
+                            fm[(t + 1) & 1][0] = f0;
+                            fm[(t + 1) & 1][1] = f1;
+                            asm volatile("" : "+v"(fm[(t + 1) & 1][0]), "+v"(fm[(t + 1) & 1][1]));
+                        } else {
+                            st[hh][e] = f0;
+                            st[hh][e + 1] = f1;
+                            asm volatile("" : "+v"(st[hh][e]), "+v"(st[hh][e + 1]));
+                        }
+                    }
+                }
+                {
+                    const int hh = t >= X + 2 * N ? 1 : 0, e = PER * (t - X - 2 * N * hh) + p;
+                    if (e >= 0 && e < 16) {
+                        w[hh][e >> 1] = pack_bf16(st[hh][e] * dp[hh][e], st[hh][e + 1] * dp[hh][e + 1]);
+                        asm volatile("" : "+v"(w[hh][e >> 1]));
+                    }
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    for (int c = 0; c < tiles; ++c) {
+        // tile c has landed and everyone is done with the other buffer
+        wait_gathers();
+        __syncthreads();
+        if (c + 1 < tiles) issue(c + 1);
+        if (rows.any(64 * c, 64)) {
+            f32x16 st[2] = {splat(0.0f), splat(0.0f)};
+            if (!rows.all(64 * c, 64)) {
+                st[0] = start_of(see, 64 * c, half);
+                st[1] = start_of(see, 64 * c + 32, half);
+            }
+            tile(st);
+        }
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) row_at[ks] ^= 2u * TILE;
+        tr_at[0] ^= 2u * TILE; tr_at[1] ^= 2u * TILE;
+    }
+    __syncthreads();                                    // the tiles are used up
+    store_wave_rows<D>(dq + (int64_t)b * s.dq.batch + (int64_t)a * s.group * s.dq.head, s.dq, s,
+                       row0 + 32 * wave, acc, s.scale, &tiles_s[0][0][0] + 4096 * wave, lane);
+}
+
 }  // namespace win
 
 bool window_bwd_mfma_supported(bool is_bf16, int D, const win::Shape& s)
 {
     // 64 rows of a tile are reached by 32-bit offsets
     const int64_t most = (int64_t)1 << 24;
-    return is_bf16 && (D == 64 || D == 128) && s.q.token < most && s.dout.token < most;
+    return is_bf16 && (D == 64 || D == 128) && s.q.token < most && s.dout.token < most &&
+           win::slices_fit(s);
+}
+
+hipError_t launch_window_dq_mfma(int D, const win::Shape& s, const void* q, const void* k,
+                                 const void* v, const void* out, const float* lse, const void* dout,
+                                 float* delta, float* lse2, void* dq, hipStream_t stream)
+{
+    using namespace win;
+    const uint32_t row_tiles = ((uint32_t)s.rows + 127) / 128;
+    const uint32_t items = row_tiles * (uint32_t)(s.batch * s.kv_heads);
+    auto kernel = D == 64 ? window_dq_mfma_kernel<64> : window_dq_mfma_kernel<128>;
+    kernel<<<items, 256, 0, stream>>>((const uint16_t*)q, (const uint16_t*)k, (const uint16_t*)v,
+                                      (const uint16_t*)out, lse, (const uint16_t*)dout, delta, lse2,
+                                      (uint16_t*)dq, s, row_tiles, items);
+    return hipGetLastError();
 }
 
 hipError_t launch_window_dkdv_mfma(int D, const win::Shape& s, const void* q, const void* k,

@@ -48,17 +48,12 @@ __global__ __launch_bounds__(256) void window_fwd_kernel(const T* __restrict__ q
     const int row = row0 + 32 * wave + l32;
     const int tok = row / s.group, head = a * s.group + (row - tok * s.group);
     const bool exists = row < s.rows, valid = exists && tok < ql;
-    const Sight see = sight(s, p0 + tok, kl, valid);
 
     const int t_first = row0 / s.group, t_last = min((row0 + 127) / s.group, ql - 1);
     KeyList keys = {};
     if (t_first <= t_last) keys = key_list(s, p0 + t_first, p0 + t_last, kl);
-    // the same for this wavefront's rows alone
-    const int w_first = (row0 + 32 * wave) / s.group, w_end = (row0 + 32 * wave + 31) / s.group;
-    const int w_last = min(w_end, ql - 1);
-    const int w_lo = p0 + w_first - s.left, w_hi = min(kl - 1, p0 + w_last + s.right);
-    const int all_lo = p0 + w_end - s.left, all_hi = min(kl - 1, p0 + w_first + s.right);
-    const bool all_valid = w_end < ql && row0 + 32 * wave + 31 < s.rows;
+    const Sight see = sight(s, keys, p0 + tok, kl, valid);
+    const RowsSight rows = rows_sight(s, keys, row0 + 32 * wave, 32, p0, ql, kl);
 
     const T* kb = k + (int64_t)b * s.k.batch + (int64_t)a * s.k.head;
     const T* vb = v + (int64_t)b * s.v.batch + (int64_t)a * s.v.head;
@@ -103,11 +98,9 @@ __global__ __launch_bounds__(256) void window_fwd_kernel(const T* __restrict__ q
         if (slot0 + KT < slot_e) fetch(slot0 + KT);
 #pragma unroll
         for (int hh = 0; hh < KT / 32; ++hh) {
-            const int s0 = slot0 + 32 * hh, j0 = s0 - keys.sinks + keys.lo;
-            const bool plain = s0 >= keys.sinks;       // all 32 slots are consecutive tokens
-            if (s0 >= keys.count || (plain && (j0 > w_hi || (j0 + 31 < w_lo && j0 >= s.sinks))))
-                continue;
-            const bool full = plain && all_valid && j0 >= all_lo && j0 + 31 <= all_hi;
+            const int s0 = slot0 + 32 * hh;
+            if (s0 >= keys.count || !rows.any(s0, 32)) continue;
+            const bool full = rows.all(s0, 32);
             f32x16 st = splat(0.0f);
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks)
@@ -116,8 +109,7 @@ __global__ __launch_bounds__(256) void window_fwd_kernel(const T* __restrict__ q
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int slot = s0 + 8 * (r >> 2) + 4 * half + (r & 3);
-                    const bool seen = slot < keys.count && see.sees(s, keys.token(slot));
-                    st[r] = seen ? st[r] : -INFINITY;
+                    st[r] = see.sees(slot) ? st[r] : -INFINITY;
                 }
             }
             f32x16 w;

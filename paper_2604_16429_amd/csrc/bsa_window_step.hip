@@ -101,15 +101,14 @@ __global__ __launch_bounds__(64 * kStepWaves) void window_step_kernel(
     for (int nr = 0; nr < NR; ++nr) {
         const int row = 16 * nr + l16, tok = row / s.group;
         const bool valid = row < s.rows && tok < ql;
-        see[nr] = sight(s, p0 + tok, kl, valid);
+        see[nr] = sight(s, keys, p0 + tok, kl, valid);
         const T* p = q + (int64_t)b * s.q.batch +
                      (int64_t)(a * s.group + (row - tok * s.group)) * s.q.head + (int64_t)tok * s.q.token;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks)
             qf[nr][ks] = valid ? Mma<T>::load(p + 32 * ks + 8 * grp) : Frag{};
     }
-    // keys before `all_lo` or after `all_hi` are hidden from some row
-    const int all_lo = p0 + ql - 1 - s.left, all_hi = min(kl - 1, p0 + s.right);
+    const RowsSight rows = rows_sight(s, keys, 0, s.rows, p0, ql, kl);
 
     const float c2 = s.scale * kLog2e;
     f32x4 acc[NR][DT];
@@ -163,9 +162,7 @@ __global__ __launch_bounds__(64 * kStepWaves) void window_step_kernel(
         lane_exchange();
         if (slot0 + KT * W < slot_e) fetch(slot0 + KT * W);
 
-        const int j0 = slot0 - keys.sinks + keys.lo;
-        const bool full = slot0 >= keys.sinks && slot0 + KT <= slot_e && j0 >= all_lo &&
-                          j0 + KT - 1 <= all_hi;
+        const bool full = slot0 + KT <= slot_e && rows.all(slot0, KT);
         Frag p[NR];
 #pragma unroll
         for (int nr = 0; nr < NR; ++nr) {
@@ -175,7 +172,7 @@ __global__ __launch_bounds__(64 * kStepWaves) void window_step_kernel(
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const int slot = slot0 + 16 * kt + 4 * grp + r;
-                        const bool seen = slot < slot_e && see[nr].sees(s, keys.token(slot));
+                        const bool seen = slot < slot_e && see[nr].sees(slot);
                         st[nr][kt][r] = seen ? st[nr][kt][r] : -INFINITY;
                     }
             }
@@ -266,10 +263,6 @@ __global__ __launch_bounds__(64 * kStepWaves) void window_step_kernel(
             sum += *(const f32x4*)(lds + w * REGION + (row * D + c) * 4);
         }
         const int tok = row / s.group, head = a * s.group + (row - tok * s.group);
-        if (tok >= ql) {                               // not masked where all others see all keys
-            l = 0.0f;
-            sum = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        }
         if (parts.splits > 1) {
             const int64_t part = part_of(s, parts, slice, row, split);
             *(f32x4*)(parts.acc + part * D + c) = sum;
