@@ -307,6 +307,12 @@ hipError_t launch_window_bwd(bool is_bf16, int D, const win::Shape& s, const voi
                              void* dq, void* dk, void* dv, void* workspace, hipStream_t stream);
 size_t window_bwd_workspace(bool is_bf16, int D, const win::Shape& s);
 
+// bf16 at head dims 64 and 128 in slices that 32-bit offsets reach.
+bool window_fwd_mfma_supported(bool is_bf16, int D, const win::Shape& s);
+hipError_t launch_window_fwd_mfma(int D, const win::Shape& s, const void* q, const void* k,
+                                  const void* v, void* out, float* lse, const win::Parts& parts,
+                                  hipStream_t stream);
+
 // Up to kStepRows rows of a slice (single tokens): a kernel of its own.
 constexpr int kStepRows = 32;
 hipError_t launch_window_step(bool is_bf16, int D, const win::Shape& s, const void* q, const void* k,

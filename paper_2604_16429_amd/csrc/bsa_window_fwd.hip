@@ -240,6 +240,8 @@ hipError_t launch(const Shape& s, const void* q, const void* k, const void* v, v
     hipError_t e;
     if (s.rows <= kStepRows) {
         e = launch_window_step(sizeof(T) == 2, D, s, q, k, v, out, lse, parts, stream);
+    } else if (window_fwd_mfma_supported(sizeof(T) == 2, D, s)) {
+        e = launch_window_fwd_mfma(D, s, q, k, v, out, lse, parts, stream);
     } else {
         const uint32_t row_tiles = ((uint32_t)s.rows + 127) / 128;
         const uint32_t items = row_tiles * (uint32_t)(s.batch * s.kv_heads * parts.splits);
