@@ -142,35 +142,41 @@ class _StridedParams:
             self.__dict__.update(_struct=c, _ref=ctypes.byref(c), _seen={})
         return c
 
-    def _tensor(self, field, t, heads, tokens):
-        """Device pointer of a [batch, heads, tokens, head_dim] tensor, whose strides go into
-        `field`; integers and None are taken as they are (contiguous)."""
-        seen = self._seen
-        if t is None or isinstance(t, int):
-            if seen.get(field) is not None:
-                setattr(self._struct, field, _CStrides())
-                seen[field] = None
-            return t
-        shape, strides = t.shape, t.stride()
-        now = (shape, strides, tokens, heads, t.dtype, t.is_cuda)
-        if seen.get(field) != now:
-            wanted = (self.batch, heads, tokens, self.head_dim)
-            if shape != wanted:
-                raise ValueError(f"{field}: shape {tuple(shape)} instead of {wanted}")
-            if t.dtype is not _named_dtype(self.dtype) or not t.is_cuda:
-                raise ValueError(f"{field}: {t.dtype} on {t.device} instead of the parameters' "
-                                 "dtype on a GPU")
-            if strides[3] != 1:
-                raise ValueError(f"{field}: channels must be consecutive")
-            if strides[2] == 0 and tokens > 1:
-                raise ValueError(f"{field}: tokens share memory")
-            # a dimension of one entry may carry any stride: the contiguous one is taken
-            token = strides[2] if tokens > 1 else self.head_dim
-            head = strides[1] if heads > 1 else token * tokens
-            batch = strides[0] if self.batch > 1 else head * heads
-            setattr(self._struct, field, _CStrides(batch, head, token))
-            seen[field] = now
-        return t.data_ptr()
+    def _tensors(self, *args):
+        """Device pointers of [batch, heads, tokens, head_dim] tensors, given as (field of the
+        struct, tensor, heads, tokens) one after the other.  The strides go into the fields;
+        integers and None are taken as they are (contiguous)."""
+        seen, pointers = self._seen, []
+        for field, t, heads, tokens in args:
+            if t is None or isinstance(t, int):
+                if seen.get(field) is not None:
+                    setattr(self._struct, field, _CStrides())
+                    seen[field] = None
+                pointers.append(t)
+                continue
+            now = (t.shape, t.stride(), t.dtype, t.is_cuda, tokens)
+            if seen.get(field) != now:
+                self._look(field, t, heads, tokens)
+                seen[field] = now
+            pointers.append(t.data_ptr())
+        return pointers
+
+    def _look(self, field, t, heads, tokens):
+        wanted, strides = (self.batch, heads, tokens, self.head_dim), t.stride()
+        if t.shape != wanted:
+            raise ValueError(f"{field}: shape {tuple(t.shape)} instead of {wanted}")
+        if t.dtype is not _named_dtype(self.dtype) or not t.is_cuda:
+            raise ValueError(f"{field}: {t.dtype} on {t.device} instead of the parameters' dtype "
+                             "on a GPU")
+        if strides[3] != 1:
+            raise ValueError(f"{field}: channels must be consecutive")
+        if strides[2] == 0 and tokens > 1:
+            raise ValueError(f"{field}: tokens share memory")
+        # a dimension of one entry may carry any stride: the contiguous one is taken
+        token = strides[2] if tokens > 1 else self.head_dim
+        head = strides[1] if heads > 1 else token * tokens
+        batch = strides[0] if self.batch > 1 else head * heads
+        setattr(self._struct, field, _CStrides(batch, head, token))
 
 
 _TORCH_DTYPES = {}
@@ -330,11 +336,18 @@ def _stream(stream):
     if stream is None:
         # the handle of torch.cuda.current_stream() without its Stream object, which
         # took 3.1 us of a call (a forward with its one launch 8.5 us, without 5.6)
-        import torch
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        global _raw_stream
+        if _raw_stream is None:
+            import torch
+            torch.cuda.current_device()               # (initialises the device on first use)
+            _raw_stream = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+        return _raw_stream[0](_raw_stream[1]())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
+
+
+_raw_stream = None
 
 
 def _nbytes(t) -> int:
@@ -445,20 +458,20 @@ def mosaic_bsa_rotation_init(rotary_dim: int, axes: int = 1, layout: int = ROTAT
     return Rotation(rotary_dim, axes, layout, **kw)
 
 
-def _kv(params) -> int:
-    return params.kv_heads or params.heads
-
-
 def _heads_forward(params, rotation, positions, q, k, q_out, k_out, v, v_out, rows):
     params._c()
-    kv, n = _kv(params), params.tokens
+    h, kv, n = params.heads, params.kv_heads or params.heads, params.tokens
     m = n if rows is None else params.cache_tokens
-    pos = params._positions(rotation, positions)
-    tensor = params._tensor
-    return (pos, tensor("q", q, params.heads, n), tensor("k", k, kv, n), tensor("v", v, kv, n),
-            _vector("rows", rows, params.batch * n, "int32"),
-            tensor("q_out", q_out, params.heads, n), tensor("k_out", k_out, kv, m),
-            tensor("v_out", v_out, kv, m))
+    pos = None if positions is None else params._positions(rotation, positions)
+    rows = None if rows is None else _vector("rows", rows, params.batch * n, "int32")
+    if v is None and v_out is None:
+        q, k, q_out, k_out = params._tensors(("q", q, h, n), ("k", k, kv, n), ("q_out", q_out, h, n),
+                                             ("k_out", k_out, kv, m))
+    else:
+        q, k, q_out, k_out, v, v_out = params._tensors(
+            ("q", q, h, n), ("k", k, kv, n), ("q_out", q_out, h, n), ("k_out", k_out, kv, m),
+            ("v", v, kv, n), ("v_out", v_out, kv, m))
+    return pos, q, k, v, rows, q_out, k_out, v_out
 
 
 def mosaic_bsa_rope_fwd(params: HeadsParams, rotation: Rotation, positions, q, k, q_out, k_out,
@@ -472,10 +485,10 @@ def mosaic_bsa_rope_fwd(params: HeadsParams, rotation: Rotation, positions, q, k
 def mosaic_bsa_rope_bwd(params: HeadsParams, rotation: Rotation, positions, dq_out, dk_out, dq, dk,
                         stream=None) -> None:
     params._c()
-    kv, n, tensor = _kv(params), params.tokens, params._tensor
-    pos = params._positions(rotation, positions)
-    dq_out, dk_out = tensor("q_out", dq_out, params.heads, n), tensor("k_out", dk_out, kv, n)
-    dq, dk = tensor("q", dq, params.heads, n), tensor("k", dk, kv, n)
+    h, kv, n = params.heads, params.kv_heads or params.heads, params.tokens
+    pos = None if positions is None else params._positions(rotation, positions)
+    dq_out, dk_out, dq, dk = params._tensors(("q_out", dq_out, h, n), ("k_out", dk_out, kv, n),
+                                             ("q", dq, h, n), ("k", dk, kv, n))
     _check(load_library().mosaic_bsa_rope_bwd(params._ref, rotation.ref, pos, dq_out, dk_out, dq,
                                               dk, _stream(stream)))
 
@@ -500,12 +513,12 @@ def mosaic_bsa_qk_norm_rope_bwd(params: HeadsParams, rotation: Rotation, positio
                                 k_weight, dq_out, dk_out, dq, dk, dq_weight, dk_weight, workspace,
                                 stream=None, workspace_bytes=None) -> None:
     c = params._c()
-    kv, n, d, tensor = _kv(params), params.tokens, params.head_dim, params._tensor
-    pos = params._positions(rotation, positions)
-    q, k = tensor("q", q, params.heads, n), tensor("k", k, kv, n)
-    dq_out, dk_out = tensor("q_out", dq_out, params.heads, n), tensor("k_out", dk_out, kv, n)
+    h, kv, n, d = params.heads, params.kv_heads or params.heads, params.tokens, params.head_dim
+    pos = None if positions is None else params._positions(rotation, positions)
     # the strides of dq and dk are arguments of their own: the fields of v and v_out hold them
-    dq, dk = tensor("v", dq, params.heads, n), tensor("v_out", dk, kv, n)
+    q, k, dq_out, dk_out, dq, dk = params._tensors(
+        ("q", q, h, n), ("k", k, kv, n), ("q_out", dq_out, h, n), ("k_out", dk_out, kv, n),
+        ("v", dq, h, n), ("v_out", dk, kv, n))
     wb = _nbytes(workspace) if workspace_bytes is None else workspace_bytes
     _check(load_library().mosaic_bsa_qk_norm_rope_bwd(
         params._ref, rotation.ref, pos, q, k, _vector("q_weight", q_weight, d, "float32"),
@@ -522,12 +535,12 @@ def mosaic_bsa_window_workspace_bytes(params: WindowParams, op: int) -> int:
 def mosaic_bsa_window_fwd(params: WindowParams, q, k, v, out, lse=None, q_lens=None, k_lens=None,
                           workspace=None, stream=None, workspace_bytes=None) -> None:
     params._c()
-    h, kv, nq, nk, tensor = params.heads, _kv(params), params.q_tokens, params.k_tokens, params._tensor
+    h, kv, nq, nk = params.heads, params.kv_heads or params.heads, params.q_tokens, params.k_tokens
     wb = _nbytes(workspace) if workspace_bytes is None else workspace_bytes
+    q, k, v, out = params._tensors(("q", q, h, nq), ("k", k, kv, nk), ("v", v, kv, nk), ("out", out, h, nq))
     _check(load_library().mosaic_bsa_window_fwd(
-        params._ref, tensor("q", q, h, nq), tensor("k", k, kv, nk), tensor("v", v, kv, nk),
-        _vector("q_lens", q_lens, params.batch, "int32"),
-        _vector("k_lens", k_lens, params.batch, "int32"), tensor("out", out, h, nq),
+        params._ref, q, k, v, _vector("q_lens", q_lens, params.batch, "int32"),
+        _vector("k_lens", k_lens, params.batch, "int32"), out,
         _vector("lse", lse, params.batch * h * nq, "float32"), _ptr(workspace), wb,
         _stream(stream)))
 
@@ -536,11 +549,13 @@ def mosaic_bsa_window_bwd(params: WindowParams, q, k, v, out, lse, dout, dq, dk,
                           workspace=None, q_lens=None, k_lens=None, stream=None,
                           workspace_bytes=None) -> None:
     params._c()
-    h, kv, nq, nk, tensor = params.heads, _kv(params), params.q_tokens, params.k_tokens, params._tensor
+    h, kv, nq, nk = params.heads, params.kv_heads or params.heads, params.q_tokens, params.k_tokens
     wb = _nbytes(workspace) if workspace_bytes is None else workspace_bytes
+    q, k, v, out, dout, dq, dk, dv = params._tensors(
+        ("q", q, h, nq), ("k", k, kv, nk), ("v", v, kv, nk), ("out", out, h, nq),
+        ("dout", dout, h, nq), ("dq", dq, h, nq), ("dk", dk, kv, nk), ("dv", dv, kv, nk))
     _check(load_library().mosaic_bsa_window_bwd(
-        params._ref, tensor("q", q, h, nq), tensor("k", k, kv, nk), tensor("v", v, kv, nk),
-        tensor("out", out, h, nq), _vector("lse", lse, params.batch * h * nq, "float32"),
-        tensor("dout", dout, h, nq), _vector("q_lens", q_lens, params.batch, "int32"),
-        _vector("k_lens", k_lens, params.batch, "int32"), tensor("dq", dq, h, nq),
-        tensor("dk", dk, kv, nk), tensor("dv", dv, kv, nk), _ptr(workspace), wb, _stream(stream)))
+        params._ref, q, k, v, out, _vector("lse", lse, params.batch * h * nq, "float32"), dout,
+        _vector("q_lens", q_lens, params.batch, "int32"),
+        _vector("k_lens", k_lens, params.batch, "int32"), dq, dk, dv, _ptr(workspace), wb,
+        _stream(stream)))

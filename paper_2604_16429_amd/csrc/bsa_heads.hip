@@ -26,6 +26,9 @@ namespace bsa {
 
 namespace heads {
 
+typedef __attribute__((ext_vector_type(4))) int32_t i32x4;
+typedef __attribute__((ext_vector_type(2))) int32_t i32x2;
+
 // One of q, k, v: what a call reads (x; g: the gradient of the result) and writes.
 struct Segment {
     const void *x, *g;
@@ -49,38 +52,53 @@ struct Args {
     uint64_t turns[MOSAIC_BSA_MAX_PAIRS];
 };
 
-// V channels of a row
+// V channels of a row, as they lie in memory (32-bit words; V = 1 in bf16: one in a word).
 template <typename T, int V>
-__device__ __forceinline__ void load_chunk(const T* p, float (&e)[2 * V], int at)
-{
-    if constexpr (sizeof(T) == 4) {
-        if constexpr (V == 4) {
-            const float4 r = *(const float4*)p;
-            e[at] = r.x; e[at + 1] = r.y; e[at + 2] = r.z; e[at + 3] = r.w;
-        } else if constexpr (V == 2) {
-            const float2 r = *(const float2*)p;
-            e[at] = r.x; e[at + 1] = r.y;
-        } else {
-            e[at] = *p;
-        }
-    } else {
-        uint32_t u[V == 1 ? 1 : V / 2];
-        if constexpr (V == 8) {
-            const uint4 r = *(const uint4*)p;
-            u[0] = r.x; u[1] = r.y; u[2] = r.z; u[3] = r.w;
-        } else if constexpr (V == 4) {
-            const uint2 r = *(const uint2*)p;
-            u[0] = r.x; u[1] = r.y;
-        } else if constexpr (V == 2) {
-            u[0] = *(const uint32_t*)p;
-        } else {
-            u[0] = *p;
-        }
+struct Chunk {
+    static constexpr int WORDS = sizeof(T) * V < 4 ? 1 : (int)sizeof(T) * V / 4;
+    uint32_t w[WORDS];
+    __device__ __forceinline__ void load(const T* p)
+    {
+        if constexpr (WORDS == 4) {
+            const i32x4 r = *(const i32x4*)p;
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-            e[at + i] = __uint_as_float((i & 1) ? u[i / 2] & 0xffff0000u : u[i / 2] << 16);
+            for (int i = 0; i < 4; ++i) w[i] = (uint32_t)r[i];
+        } else if constexpr (WORDS == 2) {
+            const i32x2 r = *(const i32x2*)p;
+            w[0] = (uint32_t)r[0];
+            w[1] = (uint32_t)r[1];
+        } else if constexpr (sizeof(T) * V == 4) {
+            w[0] = *(const uint32_t*)p;
+        } else {
+            w[0] = *p;
+        }
     }
-}
+    __device__ __forceinline__ float value(int i) const
+    {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+        else return __uint_as_float((i & 1) ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+    }
+};
+// A lane's two chunks of a row; zeros where it has none.
+template <typename T, int V>
+struct Piece {
+    Chunk<T, V> a, b;
+    __device__ __forceinline__ void load(const T* p, int ch_a, int ch_b, bool has_a, bool has_b)
+    {
+#pragma unroll
+        for (int i = 0; i < Chunk<T, V>::WORDS; ++i) a.w[i] = b.w[i] = 0u;
+        if (has_a) a.load(p + ch_a);
+        if (has_b) b.load(p + ch_b);
+    }
+    __device__ __forceinline__ void values(float (&e)[2 * V]) const
+    {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            e[i] = a.value(i);
+            e[V + i] = b.value(i);
+        }
+    }
+};
 
 template <typename T, int V>
 __device__ __forceinline__ void store_chunk(T* p, const float (&e)[2 * V], int at)
@@ -118,21 +136,30 @@ __device__ __forceinline__ void cos_sin(uint32_t u, float& c, float& s)
 
 enum { kRotate, kNorm, kNormGrad };
 
-// Sum over the P (a power of two) lanes of a row.
-template <int P_MAX>
+template <int CTRL>
+__device__ __forceinline__ float add_lane(float x)
+{
+    return x + __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, 0xf,
+                                                                     0xf, true));
+}
+// Sum over the P (a power of two) lanes of a row: neighbours, pairs, then mirrored halves of 8 and 16
+// lanes, which data-parallel moves reach without LDS.
 __device__ __forceinline__ float row_sum(float x, int P)
 {
-#pragma unroll
-    for (int o = 1; o < P_MAX; o <<= 1)
-        if (o < P) x += __shfl_xor(x, o);
+    if (P > 1) x = add_lane<0xb1>(x);                  // lanes 1 0 3 2
+    if (P > 2) x = add_lane<0x4e>(x);                  // lanes 2 3 0 1
+    if (P > 4) x = add_lane<0x141>(x);                 // mirrored in 8
+    if (P > 8) x = add_lane<0x140>(x);                 // mirrored in 16
+    if (P > 16) x += __shfl_xor(x, 16);
+    if (P > 32) x += __shfl_xor(x, 32);
     return x;
 }
 
 template <typename T, int V, bool PAIRS, int MODE>
-__global__ __launch_bounds__(256) void heads_kernel(const Args a, const int D, const int P)
+__global__ __launch_bounds__(256, 3) void heads_kernel(const Args a, const int D, const int P)
 {
     constexpr int E = 2 * V;
-    constexpr int U = MODE == kNormGrad ? 2 : 4;     // heads in flight
+    constexpr int U = MODE == kNormGrad ? 1 : 2;     // heads at a time
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int unit = lane & (P - 1), slot = lane / P, per_wave = 64 / P;
     const bool active = unit < a.units, rotated = unit < a.rotated_units;
@@ -211,26 +238,27 @@ __global__ __launch_bounds__(256) void heads_kernel(const Args a, const int D, c
                     }
                 }
             }
-            for (int h = from; h < to; h += U) {
-                float e[U][E], d[MODE == kNormGrad ? U : 1][MODE == kNormGrad ? E : 1];
+            // The rows of the next U heads are asked for before these are worked on.
+            Piece<T, V> xn[U], gn[MODE == kNormGrad ? U : 1];
+            auto ask = [&](int h) {
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-#pragma unroll
-                    for (int i = 0; i < E; ++i) {
-                        e[u][i] = 0.0f;
-                        if constexpr (MODE == kNormGrad) d[u][i] = 0.0f;
-                    }
-                    if (h + u < to) {
-                        const T* p = x + (int64_t)(h + u) * sg.xs.head;
-                        if (here) load_chunk<T, V>(p + ch_a, e[u], 0);
-                        if (here && has_b) load_chunk<T, V>(p + ch_b, e[u], V);
-                        if constexpr (MODE == kNormGrad) {
-                            const T* r = g + (int64_t)(h + u) * sg.gs.head;
-                            if (here) load_chunk<T, V>(r + ch_a, d[u], 0);
-                            if (here && has_b) load_chunk<T, V>(r + ch_b, d[u], V);
-                        }
-                    }
+                    const bool there = here && h + u < to;
+                    xn[u].load(x + (int64_t)(h + u) * sg.xs.head, ch_a, ch_b, there, there && has_b);
+                    if constexpr (MODE == kNormGrad)
+                        gn[u].load(g + (int64_t)(h + u) * sg.gs.head, ch_a, ch_b, there, there && has_b);
                 }
+            };
+            ask(from);
+            for (int h = from; h < to; h += U) {
+                float e[U][E], d[MODE == kNormGrad ? U : 1][MODE == kNormGrad ? E : 1];
+                Piece<T, V> xc[U], gc[MODE == kNormGrad ? U : 1];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    xc[u] = xn[u];
+                    if constexpr (MODE == kNormGrad) gc[u] = gn[u];
+                }
+                if (h + U < to) ask(h + U);
                 auto turn = [&](float (&z)[E]) {
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
@@ -243,6 +271,8 @@ __global__ __launch_bounds__(256) void heads_kernel(const Args a, const int D, c
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     if (h + u >= to) break;
+                    xc[u].values(e[u]);
+                    if constexpr (MODE == kNormGrad) gc[u].values(d[u]);
                     if constexpr (MODE == kRotate) {
                         if (!copy) turn(e[u]);
                     } else {
@@ -250,7 +280,7 @@ __global__ __launch_bounds__(256) void heads_kernel(const Args a, const int D, c
                             float sq = 0.0f;
 #pragma unroll
                             for (int i = 0; i < E; ++i) sq = fmaf(e[u][i], e[u][i], sq);
-                            sq = row_sum<64>(sq, P);
+                            sq = row_sum(sq, P);
                             const float r = 1.0f / sqrtf(sq * (1.0f / (float)D) + a.eps);
                             if constexpr (MODE == kNorm) {
 #pragma unroll
@@ -266,7 +296,7 @@ __global__ __launch_bounds__(256) void heads_kernel(const Args a, const int D, c
                                     d[u][i] *= w[i];
                                     dot = fmaf(d[u][i], e[u][i], dot);
                                 }
-                                dot = row_sum<64>(dot, P) * (1.0f / (float)D);
+                                dot = row_sum(dot, P) * (1.0f / (float)D);
 #pragma unroll
                                 for (int i = 0; i < E; ++i)
                                     e[u][i] = r * fmaf(-dot, e[u][i], d[u][i]);
@@ -302,27 +332,37 @@ __global__ __launch_bounds__(256) void heads_kernel(const Args a, const int D, c
     }
 }
 
-// dw = sum of the workgroups' parts in a fixed order, in 64 bits.  One workgroup per 16
-// columns of the [workgroups][2 D] parts.
+// dw = sum of the workgroups' parts in a fixed order, in 64 bits.  One workgroup per four columns of
+// the [workgroups][2 D] parts.
 __global__ __launch_bounds__(256) void weight_grad_kernel(const float* __restrict__ partial,
                                                           int workgroups, int D, float* dqw,
                                                           float* dkw)
 {
-    __shared__ double sums[16][17];
-    const int col = blockIdx.x * 16 + (threadIdx.x & 15), part = threadIdx.x >> 4;
-    double s = 0.0;
-    for (int w = part; w < workgroups; w += 16) s += (double)partial[(int64_t)w * 2 * D + col];
-    sums[part][threadIdx.x & 15] = s;
-    __syncthreads();
-    if (part == 0) {
-        for (int i = 1; i < 16; ++i) s += sums[i][threadIdx.x & 15];
-        if (col < D) dqw[col] = (float)s;
-        else if (dkw) dkw[col - D] = (float)s;
+    __shared__ double sums[256][4];
+    const int col = blockIdx.x * 4, at = threadIdx.x;
+    double s[4] = {0.0, 0.0, 0.0, 0.0};
+    for (int w = at; w < workgroups; w += 256) {
+        const float4 x = *(const float4*)(partial + (int64_t)w * 2 * D + col);
+        s[0] += (double)x.x; s[1] += (double)x.y; s[2] += (double)x.z; s[3] += (double)x.w;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sums[at][i] = s[i];
+    for (int o = 128; o > 0; o >>= 1) {
+        __syncthreads();
+        if (at < o)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sums[at][i] += sums[at + o][i];
+    }
+    if (at == 0) {
+        float* to = col < D ? dqw + col : dkw ? dkw + (col - D) : nullptr;
+        if (to)
+            for (int i = 0; i < 4; ++i) to[i] = (float)sums[0][i];
     }
 }
 
-// workgroups whose parts the backward of the norm leaves
-constexpr int kGradWorkgroups = 1024;
+// Workgroups whose parts the backward of the norm leaves: three to a CU, as many as run at once with
+// the registers of its widest form (1,024: a round and a third).
+constexpr int kGradWorkgroups = 768;
 
 template <typename T, int V, bool PAIRS>
 hipError_t launch_mode(const Args& a, int mode, int D, int P, unsigned grid, hipStream_t stream)
@@ -414,10 +454,13 @@ int launch(Args& a, const mosaic_bsa_heads_params* p, const Checked& c,
     int P = 1;
     while (P < a.units) P <<= 1;
     a.all_heads = a.seg[0].heads + a.seg[1].heads + a.seg[2].heads;
-    // Heads of a token stay together, so that its angles are made once, until that leaves
-    // less than four wavefronts per SIMD.
+    // Heads of a token stay together, so that its angles are made once: all of them while that
+    // gives 8,192 workgroups, else 8 or more (a launch of one round of workgroups and a few ends with
+    // those few alone on the chip), and fewer where less than four wavefronts per SIMD would be left.
     const int64_t groups = ((int64_t)a.all_tokens + 4 * (64 / P) - 1) / (4 * (64 / P));
-    int64_t chunks = (1024 + groups - 1) / groups;
+    const int64_t even = (8192 + groups - 1) / groups, most = (a.all_heads + 7) / 8;
+    int64_t chunks = even < most ? even : most;
+    if (groups * chunks < 1024) chunks = (1024 + groups - 1) / groups;
     if (chunks > a.all_heads) chunks = a.all_heads;
     a.head_chunk = (int)((a.all_heads + chunks - 1) / chunks);
     a.chunks = (a.all_heads + a.head_chunk - 1) / a.head_chunk;
@@ -632,7 +675,7 @@ extern "C" int mosaic_bsa_qk_norm_rope_bwd(
     const int esz = c.is_bf16 ? 2 : 4;
     if (unaligned(q, esz) || (dk && unaligned(k, esz)) || unaligned(positions, 4) ||
         unaligned(q_weight, 4) || unaligned(k_weight, 4) || unaligned(dq_weight, 4) ||
-        unaligned(dk_weight, 4) || unaligned(workspace, 4))
+        unaligned(dk_weight, 4) || unaligned(workspace, 16))
         return MOSAIC_BSA_ERR_ALIGN;
     if (!workspace || workspace_bytes < mosaic_bsa_qk_norm_rope_workspace_bytes(params))
         return MOSAIC_BSA_ERR_WORKSPACE;
@@ -650,7 +693,7 @@ extern "C" int mosaic_bsa_qk_norm_rope_bwd(
     if (int rc = launch(a, params, c, rotation, kNormGrad, true, kGradWorkgroups, &used,
                         (hipStream_t)hip_stream))
         return rc;
-    weight_grad_kernel<<<2 * D / 16, 256, 0, (hipStream_t)hip_stream>>>(
+    weight_grad_kernel<<<2 * D / 4, 256, 0, (hipStream_t)hip_stream>>>(
         a.partial, (int)used, D, dq_weight, dk ? dk_weight : nullptr);
     return hipGetLastError() == hipSuccess ? MOSAIC_BSA_OK : MOSAIC_BSA_ERR_LAUNCH;
 }
