@@ -295,6 +295,24 @@ __device__ __forceinline__ int64_t part_of(const Shape& s, const Parts& p, uint3
     return ((int64_t)slice * s.rows + row) * p.splits + split;
 }
 
+// Most keys that `rows` consecutive rows of a slice can see.
+inline int64_t most_keys(const Shape& s, int rows)
+{
+    const int64_t tokens = ((int64_t)rows + s.group - 1) / s.group + 1;
+    const int64_t right = s.right < tokens ? s.right : tokens;
+    const int64_t span = (int64_t)s.left + right + tokens + s.sinks;
+    const int64_t all = s.ring ? (int64_t)s.ring + s.sinks : (int64_t)s.k_tokens;
+    return span < all ? span : all;
+}
+// Up to 16 rows and few keys: as many wavefronts to a workgroup as registers allow, and no parts,
+// whose joining is a launch more.
+constexpr int step_waves(int element, int D) { return element * D <= 128 ? 16 : element * D <= 256 ? 8 : 4; }
+inline bool is_wide_step(bool is_bf16, int D, const Shape& s)
+{
+    const int waves = step_waves(is_bf16 ? 2 : 4, D);
+    return s.rows <= 16 && waves > 4 && most_keys(s, s.rows) <= 128 * waves;
+}
+
 }  // namespace win
 
 // Host side: launches, called by the entry points after validation.
@@ -313,8 +331,7 @@ hipError_t launch_window_fwd_mfma(int D, const win::Shape& s, const void* q, con
                                   const void* v, void* out, float* lse, const win::Parts& parts,
                                   hipStream_t stream);
 
-// Up to kStepRows rows of a slice (single tokens): a kernel of its own.
-constexpr int kStepRows = 32;
+// Few rows: 16 (all of a slice) or 32 to a workgroup.
 hipError_t launch_window_step(bool is_bf16, int D, const win::Shape& s, const void* q, const void* k,
                               const void* v, void* out, float* lse, const win::Parts& parts,
                               hipStream_t stream);

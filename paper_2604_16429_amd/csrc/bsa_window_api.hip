@@ -53,6 +53,7 @@ int check_params(const mosaic_bsa_window_params* p, Checked* c)
     s.ring = p->ring;
     s.scale = p->softmax_scale > 0.0f ? p->softmax_scale : 1.0f / sqrtf((float)p->head_dim);
     s.q_lens = s.k_lens = nullptr;
+    s.q = s.k = s.v = s.out = s.dout = s.dq = s.dk = s.dv = mosaic_bsa_strides{0, 0, 0};
     return MOSAIC_BSA_OK;
 }
 

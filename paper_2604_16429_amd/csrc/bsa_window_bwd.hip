@@ -20,42 +20,75 @@ namespace bsa {
 
 namespace win {
 
+// Wavefronts of a workgroup whose tiles are the wavefronts' own: as many as registers leave room for.
 template <typename T, int D>
+constexpr int narrow_waves() { return D * (int)sizeof(T) <= 128 ? 8 : 4; }
+
+// A wavefront's values lane by lane through LDS: those of wavefronts 1 .. are added to wavefront 0's in
+// their order.  `lds` has room for one wavefront's.  All wavefronts call it.
+template <int NW, int COUNT>
+__device__ __forceinline__ void add_waves(unsigned char* lds, int wave, int lane, f32x16 (&x)[COUNT])
+{
+    float* const region = (float*)lds + lane;
+    for (int w = 1; w < NW; ++w) {
+        __syncthreads();
+        if (wave == w) {
+#pragma unroll
+            for (int c = 0; c < COUNT; ++c)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) region[(c * 16 + r) * 64] = x[c][r];
+        }
+        __syncthreads();
+        if (wave == 0) {
+#pragma unroll
+            for (int c = 0; c < COUNT; ++c)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) x[c][r] += region[(c * 16 + r) * 64];
+        }
+    }
+}
+
+// NARROW: the four wavefronts own the same 32 rows and take the tiles of keys in turn, with tiles of
+// their own and no barrier between them; else 32 rows each and the tiles are shared.
+template <typename T, int D, bool NARROW>
 __global__ __launch_bounds__(256) void window_dq_kernel(
     const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
     const T* __restrict__ out, const float* __restrict__ lse, const T* __restrict__ dout,
     float* __restrict__ delta, float* __restrict__ lse2, T* __restrict__ dq, const Shape s,
     uint32_t row_tiles, uint32_t items)
 {
-    constexpr int KT = sizeof(T) == 2 ? 64 : 32;
-    constexpr int KS = D / 16, DT = D / 32;
-    using Tl = Tile<T, D, KT>;
+    constexpr int KT = sizeof(T) == 2 && !NARROW ? 64 : 32, ROWS = NARROW ? 32 : 128;
+    constexpr int KS = D / 16, DT = D / 32, SETS = NARROW ? 4 : 1;
+    using Tl = Tile<T, D, KT, NARROW ? 64 : 256>;
     using M = Mma<T>;
     using Frag = typename M::Frag;
-    __shared__ __attribute__((aligned(1024))) unsigned char k_lds[Tl::BYTES];
-    __shared__ __attribute__((aligned(1024))) unsigned char v_lds[Tl::BYTES];
+    __shared__ __attribute__((aligned(1024))) unsigned char tiles_s[SETS][2][Tl::BYTES];
+    static_assert(!NARROW || DT * 16 * 64 * 4 <= (int)sizeof(tiles_s), "a wavefront's sums fit the tiles");
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, half = lane >> 5;
+    unsigned char* const k_lds = tiles_s[NARROW ? wave : 0][0];
+    unsigned char* const v_lds = tiles_s[NARROW ? wave : 0][1];
+    const int loader = NARROW ? lane : tid;
 
     const uint32_t item = item_of(blockIdx.x, items);
     const uint32_t slice = item / row_tiles;
-    const int row0 = (int)(item - slice * row_tiles) * 128;
+    const int row0 = (int)(item - slice * row_tiles) * ROWS;
     const int b = (int)(slice / (uint32_t)s.kv_heads), a = (int)(slice - (uint32_t)b * s.kv_heads);
     int ql, kl;
     lengths(s, b, ql, kl);
     const int p0 = kl - ql;
 
-    const int row = row0 + 32 * wave + l32;
+    const int wave_row = row0 + (NARROW ? 0 : 32 * wave), row = wave_row + l32;
     const int tok = row / s.group, head = a * s.group + (row - tok * s.group);
     const bool exists = row < s.rows, valid = exists && tok < ql;
 
-    const int t_first = row0 / s.group, t_last = min((row0 + 127) / s.group, ql - 1);
+    const int t_first = row0 / s.group, t_last = min((row0 + ROWS - 1) / s.group, ql - 1);
     KeyList keys = {};
     if (t_first <= t_last) keys = key_list(s, p0 + t_first, p0 + t_last, kl);
     const Sight see = sight(s, keys, p0 + tok, kl, valid);
-    const RowsSight rows = rows_sight(s, keys, row0 + 32 * wave, 32, p0, ql, kl);
+    const RowsSight rows = rows_sight(s, keys, wave_row, 32, p0, ql, kl);
 
     const T* kb = k + (int64_t)b * s.k.batch + (int64_t)a * s.k.head;
     const T* vb = v + (int64_t)b * s.v.batch + (int64_t)a * s.v.head;
@@ -81,7 +114,7 @@ __global__ __launch_bounds__(256) void window_dq_kernel(
         if (valid) {
             const int64_t at = ((int64_t)b * s.heads + head) * s.q_tokens + tok;
             const float l = lse[at], l2 = l == -INFINITY ? kNoWeight : l * kLog2e;
-            if (half == 0) {
+            if (half == 0 && (!NARROW || wave == 0)) {
                 delta[at] = d;
                 lse2[at] = l2;
             }
@@ -96,22 +129,25 @@ __global__ __launch_bounds__(256) void window_dq_kernel(
 
     Tl kt, vt;
     auto fetch = [&](int slot0) {
-        kt.fetch(tid, [&](int r) -> const T* {
+        kt.fetch(loader, [&](int r) -> const T* {
             const int slot = slot0 + r;
             return slot < keys.count ? kb + (int64_t)keys.row(slot) * s.k.token : nullptr;
         });
-        vt.fetch(tid, [&](int r) -> const T* {
+        vt.fetch(loader, [&](int r) -> const T* {
             const int slot = slot0 + r;
             return slot < keys.count ? vb + (int64_t)keys.row(slot) * s.v.token : nullptr;
         });
     };
-    if (keys.count > 0) fetch(0);
-    for (int slot0 = 0; slot0 < keys.count; slot0 += KT) {
-        __syncthreads();
-        kt.put(k_lds, tid);
-        vt.put(v_lds, tid);
-        __syncthreads();
-        if (slot0 + KT < keys.count) fetch(slot0 + KT);
+    const int first = NARROW ? KT * wave : 0, step = NARROW ? 4 * KT : KT;
+    if (first < keys.count) fetch(first);
+    for (int slot0 = first; slot0 < keys.count; slot0 += step) {
+        if constexpr (NARROW) lane_exchange();
+        else __syncthreads();
+        kt.put(k_lds, loader);
+        vt.put(v_lds, loader);
+        if constexpr (NARROW) lane_exchange();
+        else __syncthreads();
+        if (slot0 + step < keys.count) fetch(slot0 + step);
 #pragma unroll
         for (int hh = 0; hh < KT / 32; ++hh) {
             const int s0 = slot0 + 32 * hh;
@@ -140,6 +176,10 @@ __global__ __launch_bounds__(256) void window_dq_kernel(
                     acc[dt] = M::mul(Tl::trans_frag(k_lds, 32 * hh + 16 * h, dt, lane), ds, acc[dt]);
             }
         }
+    }
+    if constexpr (NARROW) {
+        add_waves<4>(&tiles_s[0][0][0], wave, lane, acc);
+        if (wave != 0) return;
     }
     if (!exists) return;
     store_lane_row<T, D>(dq + (int64_t)b * s.dq.batch + (int64_t)head * s.dq.head +
@@ -300,23 +340,23 @@ __global__ __launch_bounds__(256) void window_dkdv_kernel(
     }
 }
 
-// dK and dV of 32 keys: four wavefronts own the same keys and take the tiles of queries in turn,
+// dK and dV of 32 keys: the wavefronts own the same keys and take the tiles of queries in turn,
 // with tiles of their own and no barrier between them; their sums are added in the order of the
 // wavefronts.  FAR: the queries beyond the window of the tile that holds the keys, one chunk to a
 // workgroup, sums to the workspace; else all inside the window.
 template <typename T, int D, bool FAR>
-__global__ __launch_bounds__(256) void window_dkdv_narrow_kernel(
+__global__ __launch_bounds__((64 * narrow_waves<T, D>())) void window_dkdv_narrow_kernel(
     const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
     const T* __restrict__ dout, const float* __restrict__ delta, const float* __restrict__ lse2,
     T* __restrict__ dk, T* __restrict__ dv, const Shape s, const Far far, uint32_t key_groups,
     uint32_t items)
 {
-    constexpr int RT = 32, KS = D / 16, DT = D / 32;
+    constexpr int RT = 32, KS = D / 16, DT = D / 32, NW = narrow_waves<T, D>();
     using Tl = Tile<T, D, RT, 64>;
     using Frag = typename Mma<T>::Frag;
-    __shared__ __attribute__((aligned(1024))) unsigned char tiles_s[4][2][Tl::BYTES];
-    __shared__ float l2_s[4][RT], dl_s[4][RT];
-    static_assert(2 * DT * 16 * 64 * 4 <= (int)sizeof(tiles_s), "a wavefront's sums fit the tiles");
+    __shared__ __attribute__((aligned(1024))) unsigned char tiles_s[NW][2][Tl::BYTES];
+    __shared__ float l2_s[NW][RT], dl_s[NW][RT];
+    static_assert(DT * 16 * 64 * 4 <= (int)sizeof(tiles_s), "a wavefront's sums fit the tiles");
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -360,43 +400,21 @@ __global__ __launch_bounds__(256) void window_dkdv_narrow_kernel(
         row_held = l32 < n ? (half ? delta[at] : lse2[at]) : half ? 0.0f : kNoWeight;
     };
     if (wave < all) fetch(wave);
-    for (int it = wave; it < all; it += 4) {
+    for (int it = wave; it < all; it += NW) {
         lane_exchange();
         qt.put(tiles_s[wave][0], lane);
         gt.put(tiles_s[wave][1], lane);
         (half ? dl_s : l2_s)[wave][l32] = row_held;
         lane_exchange();
-        if (it + 4 < all) fetch(it + 4);
+        if (it + NW < all) fetch(it + NW);
         const int t0 = span.a + it % tiles * RT, n = min(RT, span.e - t0), pa = p0 + t0;
         const bool full = n == 32 && jw + 31 < kl && jw + 31 <= pa + s.right &&
                           (jw >= pa + 31 - s.left || jw + 31 < s.sinks);
         key_products<T, D, Tl>(tiles_s[wave][0], tiles_s[wave][1], l2_s[wave], dl_s[wave], 0, lane, kf, vf,
                                c2, full, column(s, j, kl, pa, n), ak, av);
     }
-    // the other wavefronts' sums, in their order
-    float* const region = (float*)&tiles_s[0][0][0] + lane;
-    for (int w = 1; w < 4; ++w) {
-        __syncthreads();
-        if (wave == w) {
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    region[(dt * 16 + r) * 64] = ak[dt][r];
-                    region[((DT + dt) * 16 + r) * 64] = av[dt][r];
-                }
-        }
-        __syncthreads();
-        if (wave == 0) {
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    ak[dt][r] += region[(dt * 16 + r) * 64];
-                    av[dt][r] += region[((DT + dt) * 16 + r) * 64];
-                }
-        }
-    }
+    add_waves<NW>(&tiles_s[0][0][0], wave, lane, ak);
+    add_waves<NW>(&tiles_s[0][0][0], wave, lane, av);
     if (wave != 0) return;
     if constexpr (FAR) {
         float* p = far.sums + (((int64_t)slice * far.groups + group) * far.chunks + chunk) * (64 * D) +
@@ -433,9 +451,9 @@ Far far_of(const Shape& s)
     // queries beyond the window of a sink exist where the window is shorter than the sequence
     if (s.sinks == 0 || s.left >= s.k_tokens) return f;
     f.groups = (s.sinks + 31) / 32;
-    // a workgroup per CU and a half, of at least 8 tiles of 32 queries for each wavefront
+    // a workgroup per CU and a half, of at least 8 tiles of 32 queries
     const int64_t slices = (int64_t)s.batch * s.kv_heads;
-    const int64_t want = max((int64_t)1, 384 / (slices * f.groups)), most = max(1, s.rows / 1024);
+    const int64_t want = max((int64_t)1, 384 / (slices * f.groups)), most = max(1, s.rows / 256);
     f.chunks = (int)min(min(want, most), (int64_t)32);
     return f;
 }
@@ -461,20 +479,23 @@ hipError_t launch_bwd(const Shape& s, const void* q_, const void* k_, const void
     far.sums = (float*)((char*)workspace + 2 * row_bytes(s));
 
     hipError_t e;
-    if (window_bwd_mfma_supported(sizeof(T) == 2, D, s)) {
+    // launches of fewer workgroups of 128 rows than CUs: 32 rows to each
+    const bool few_rows = slices * (((int64_t)s.rows + 127) / 128) < 256;
+    if (!few_rows && window_bwd_mfma_supported(sizeof(T) == 2, D, s)) {
         e = launch_window_dq_mfma(D, s, q, k, v, out, lse, dout, delta, lse2, dq, stream);
     } else {
-        const uint32_t row_tiles = ((uint32_t)s.rows + 127) / 128;
+        const uint32_t per = few_rows ? 32 : 128, row_tiles = ((uint32_t)s.rows + per - 1) / per;
         const uint32_t q_items = row_tiles * (uint32_t)slices;
-        window_dq_kernel<T, D><<<q_items, 256, 0, stream>>>(q, k, v, out, lse, dout, delta, lse2, dq, s,
-                                                           row_tiles, q_items);
+        auto kernel = few_rows ? window_dq_kernel<T, D, true> : window_dq_kernel<T, D, false>;
+        kernel<<<q_items, 256, 0, stream>>>(q, k, v, out, lse, dout, delta, lse2, dq, s, row_tiles,
+                                            q_items);
         e = hipGetLastError();
     }
     if (e != hipSuccess) return e;
 
     if (far.groups) {
         const uint32_t n = (uint32_t)slices * (uint32_t)(far.groups * far.chunks);
-        window_dkdv_narrow_kernel<T, D, true><<<n, 256, 0, stream>>>(
+        window_dkdv_narrow_kernel<T, D, true><<<n, 64 * narrow_waves<T, D>(), 0, stream>>>(
             q, k, v, dout, delta, lse2, dk, dv, s, far, (uint32_t)far.groups, n);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
@@ -482,7 +503,7 @@ hipError_t launch_bwd(const Shape& s, const void* q_, const void* k_, const void
     const uint32_t key_tiles = ((uint32_t)s.k_tokens + per - 1) / per;
     const uint32_t k_items = (uint32_t)slices * key_tiles;
     if (is_narrow(s))
-        window_dkdv_narrow_kernel<T, D, false><<<k_items, 256, 0, stream>>>(
+        window_dkdv_narrow_kernel<T, D, false><<<k_items, 64 * narrow_waves<T, D>(), 0, stream>>>(
             q, k, v, dout, delta, lse2, dk, dv, s, far, key_tiles, k_items);
     else if (window_bwd_mfma_supported(sizeof(T) == 2, D, s))
         return launch_window_dkdv_mfma(D, s, q, k, v, dout, delta, lse2, dk, dv, far, stream);

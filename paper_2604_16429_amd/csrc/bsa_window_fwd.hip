@@ -201,29 +201,31 @@ __global__ __launch_bounds__(256) void window_join_kernel(T* __restrict__ out,
             l == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-// Most keys that a tile of `rows` rows can see.
-int64_t most_keys(const Shape& s, int rows)
+// Launches of up to 32 rows, and of fewer workgroups of 128 rows than CUs in fp32 and at head dim 32,
+// give 32 rows a workgroup of their own, whose wavefronts share the keys out.  (Nothing here may
+// depend on strides, which the size of the workspace is asked for without.)
+bool is_step(bool is_bf16, int D, const Shape& s)
 {
-    const int64_t tokens = ((int64_t)rows + s.group - 1) / s.group + 1;
-    const int64_t span = (int64_t)s.left + min((int64_t)s.right, tokens) + tokens + s.sinks;
-    return s.ring ? min(span, (int64_t)s.ring + s.sinks) : min(span, (int64_t)s.k_tokens);
+    return s.rows <= 32 || ((!is_bf16 || D == 32) &&
+                            (int64_t)s.batch * s.kv_heads * ((s.rows + 127) / 128) < 256);
 }
 
-// Into how many parts the keys of a launch of few row tiles are split.
-int splits_of(const Shape& s)
+// Into how many parts the keys of a launch of few workgroups are split: for up to three workgroups of
+// 32 rows to a CU, two of 128 rows, 128 keys at least to each.
+int splits_of(bool is_bf16, int D, const Shape& s)
 {
-    const bool step = s.rows <= kStepRows;
-    const int tile = step ? s.rows : 128;
+    const bool step = is_step(is_bf16, D, s);
+    if (step && is_wide_step(is_bf16, D, s)) return 1;
+    const int tile = !step ? 128 : s.rows <= 16 ? s.rows : 32;
     const int64_t items = (int64_t)s.batch * s.kv_heads * ((s.rows + tile - 1) / tile);
     const int64_t pieces = (most_keys(s, tile) + 127) / 128;
-    const int64_t want = (step ? 768 : 512) / items;
-    const int64_t n = min(min(want, pieces), (int64_t)64);
+    const int64_t n = min(min((step ? 768 : 512) / items, pieces), (int64_t)64);
     return n < 2 ? 1 : (int)n;
 }
 
-Parts parts_of(const Shape& s, int D, void* workspace)
+Parts parts_of(bool is_bf16, int D, const Shape& s, void* workspace)
 {
-    Parts p = {nullptr, nullptr, splits_of(s)};
+    Parts p = {nullptr, nullptr, splits_of(is_bf16, D, s)};
     if (p.splits > 1) {
         const int64_t n = (int64_t)s.batch * s.kv_heads * s.rows * p.splits;
         p.acc = (float*)workspace;
@@ -236,9 +238,9 @@ template <typename T, int D>
 hipError_t launch(const Shape& s, const void* q, const void* k, const void* v, void* out,
                   float* lse, void* workspace, hipStream_t stream)
 {
-    const Parts parts = parts_of(s, D, workspace);
+    const Parts parts = parts_of(sizeof(T) == 2, D, s, workspace);
     hipError_t e;
-    if (s.rows <= kStepRows) {
+    if (is_step(sizeof(T) == 2, D, s)) {
         e = launch_window_step(sizeof(T) == 2, D, s, q, k, v, out, lse, parts, stream);
     } else if (window_fwd_mfma_supported(sizeof(T) == 2, D, s)) {
         e = launch_window_fwd_mfma(D, s, q, k, v, out, lse, parts, stream);
@@ -258,9 +260,9 @@ hipError_t launch(const Shape& s, const void* q, const void* k, const void* v, v
 
 }  // namespace win
 
-size_t window_fwd_workspace(bool, int D, const win::Shape& s)
+size_t window_fwd_workspace(bool is_bf16, int D, const win::Shape& s)
 {
-    const int splits = win::splits_of(s);
+    const int splits = win::splits_of(is_bf16, D, s);
     return splits == 1 ? 0 : (size_t)s.batch * s.kv_heads * s.rows * splits * (D + 2) * sizeof(float);
 }
 

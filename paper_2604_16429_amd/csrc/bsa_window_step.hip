@@ -1,8 +1,8 @@
-// Windowed attention forward for few rows (single tokens, and a few of them): at most 32 rows
-// (token, head of the group) of a (batch, key/value head) slice.
+// Windowed attention forward for few rows (single tokens, chunks, short sequences): a workgroup owns
+// 16 or 32 rows (token, head of the group) of a (batch, key/value head) slice.
 //
 // K and V are read once and used for a handful of rows, so memory bandwidth bounds it, or, where
-// the window is short, latency.  A workgroup has 4 wavefronts that take 32 keys each in turn and
+// the window is short, latency.  A workgroup has 4 wavefronts (or 8 or 16) that take 32 keys each in turn and
 // share nothing until the end: no barrier stands between a wavefront and its next loads, which
 // are in flight while it works on the keys before.  Rows fill 16-wide matrix instructions: S^T =
 // K Q^T, whose K operand is loaded from memory as the lanes hold it, and O^T += V^T P^T, where V goes
@@ -53,15 +53,13 @@ __device__ __forceinline__ float row_max16(float x)
     return fmaxf(x, swap32(x));
 }
 
-constexpr int kStepWaves = 4;
-
-// NR: 16-row tiles.
-template <typename T, int D, int NR>
-__global__ __launch_bounds__(64 * kStepWaves) void window_step_kernel(
+// NR: 16-row tiles.  W: wavefronts.
+template <typename T, int D, int NR, int W>
+__global__ __launch_bounds__(64 * W) void window_step_kernel(
     const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v, T* __restrict__ out,
-    float* __restrict__ lse, const Shape s, const Parts parts, uint32_t items)
+    float* __restrict__ lse, const Shape s, const Parts parts, uint32_t row_tiles, uint32_t items)
 {
-    constexpr int KS = D / 32, DT = D / 16, KT = 32, W = kStepWaves;
+    constexpr int KS = D / 32, DT = D / 16, KT = 32;
     constexpr int ROW = D * sizeof(T), CHUNKS = ROW / 16;
     constexpr int V_LOADS = KT * CHUNKS / 64;
     constexpr int ACC_BYTES = NR * 16 * D * 4;
@@ -78,14 +76,17 @@ __global__ __launch_bounds__(64 * kStepWaves) void window_step_kernel(
 
     const uint32_t work = item_of(blockIdx.x, items);
     const int split = (int)(work % (uint32_t)parts.splits);
-    const uint32_t slice = work / (uint32_t)parts.splits;
+    const uint32_t item = work / (uint32_t)parts.splits;
+    const uint32_t slice = item / row_tiles;
+    const int row0 = (int)(item - slice * row_tiles) * (16 * NR), row_n = min(16 * NR, s.rows - row0);
     const int b = (int)(slice / (uint32_t)s.kv_heads), a = (int)(slice - (uint32_t)b * s.kv_heads);
     int ql, kl;
     lengths(s, b, ql, kl);
     const int p0 = kl - ql;
 
+    const int t_first = row0 / s.group, t_last = min((row0 + row_n - 1) / s.group, ql - 1);
     KeyList keys = {};
-    if (ql > 0) keys = key_list(s, p0, p0 + ql - 1, kl);
+    if (t_first <= t_last) keys = key_list(s, p0 + t_first, p0 + t_last, kl);
     int slot_a = 0, slot_e = keys.count;
     if (parts.splits > 1) {
         const int per = ((keys.count + KT - 1) / KT + parts.splits - 1) / parts.splits * KT;
@@ -99,7 +100,7 @@ __global__ __launch_bounds__(64 * kStepWaves) void window_step_kernel(
     Sight see[NR];
 #pragma unroll
     for (int nr = 0; nr < NR; ++nr) {
-        const int row = 16 * nr + l16, tok = row / s.group;
+        const int row = row0 + 16 * nr + l16, tok = row / s.group;
         const bool valid = row < s.rows && tok < ql;
         see[nr] = sight(s, keys, p0 + tok, kl, valid);
         const T* p = q + (int64_t)b * s.q.batch +
@@ -108,7 +109,7 @@ __global__ __launch_bounds__(64 * kStepWaves) void window_step_kernel(
         for (int ks = 0; ks < KS; ++ks)
             qf[nr][ks] = valid ? Mma<T>::load(p + 32 * ks + 8 * grp) : Frag{};
     }
-    const RowsSight rows = rows_sight(s, keys, 0, s.rows, p0, ql, kl);
+    const RowsSight rows = rows_sight(s, keys, row0, row_n, p0, ql, kl);
 
     const float c2 = s.scale * kLog2e;
     f32x4 acc[NR][DT];
@@ -250,17 +251,17 @@ __global__ __launch_bounds__(64 * kStepWaves) void window_step_kernel(
             *(f32x4*)(mine + ((16 * nr + l16) * D + 16 * dt + 4 * grp) * 4) = acc[nr][dt] * f;
     }
     __syncthreads();
-    const int quads = s.rows * (D / 4);
+    const int quads = row_n * (D / 4);
     for (int at = tid; at < quads; at += 64 * W) {
-        const int row = at / (D / 4), c = at % (D / 4) * 4;
+        const int own = at / (D / 4), row = row0 + own, c = at % (D / 4) * 4;
         float top = kNoRef, l = 0.0f;
 #pragma unroll
-        for (int w = 0; w < W; ++w) top = fmaxf(top, m_s[w][row]);
+        for (int w = 0; w < W; ++w) top = fmaxf(top, m_s[w][own]);
         f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int w = 0; w < W; ++w) {
-            l = fmaf(__builtin_amdgcn_exp2f(m_s[w][row] - top), l_s[w][row], l);
-            sum += *(const f32x4*)(lds + w * REGION + (row * D + c) * 4);
+            l = fmaf(__builtin_amdgcn_exp2f(m_s[w][own] - top), l_s[w][own], l);
+            sum += *(const f32x4*)(lds + w * REGION + (own * D + c) * 4);
         }
         const int tok = row / s.group, head = a * s.group + (row - tok * s.group);
         if (parts.splits > 1) {
@@ -283,10 +284,15 @@ template <typename T, int D>
 hipError_t launch_step(const Shape& s, const void* q, const void* k, const void* v, void* out,
                        float* lse, const Parts& parts, hipStream_t stream)
 {
-    const uint32_t items = (uint32_t)(s.batch * s.kv_heads * parts.splits);
-    auto kernel = s.rows <= 16 ? window_step_kernel<T, D, 1> : window_step_kernel<T, D, 2>;
-    kernel<<<items, 64 * kStepWaves, 0, stream>>>((const T*)q, (const T*)k, (const T*)v, (T*)out, lse,
-                                                  s, parts, items);
+    const uint32_t row_tiles = s.rows <= 16 ? 1u : ((uint32_t)s.rows + 31) / 32;
+    const uint32_t items = row_tiles * (uint32_t)(s.batch * s.kv_heads * parts.splits);
+    constexpr int WIDE = step_waves(sizeof(T), D);
+    const bool wide = is_wide_step(sizeof(T) == 2, D, s);
+    auto kernel = s.rows > 16 ? window_step_kernel<T, D, 2, 4>
+                  : wide      ? window_step_kernel<T, D, 1, WIDE>
+                              : window_step_kernel<T, D, 1, 4>;
+    kernel<<<items, 64 * (wide ? WIDE : 4), 0, stream>>>((const T*)q, (const T*)k, (const T*)v, (T*)out,
+                                                         lse, s, parts, row_tiles, items);
     return hipGetLastError();
 }
 
