@@ -51,7 +51,7 @@ __device__ __forceinline__ void add_waves(unsigned char* lds, int wave, int lane
 // NARROW: the four wavefronts own the same 32 rows and take the tiles of keys in turn, with tiles of
 // their own and no barrier between them; else 32 rows each and the tiles are shared.
 template <typename T, int D, bool NARROW>
-__global__ __launch_bounds__(256) void window_dq_kernel(
+__global__ __launch_bounds__(256, D == 32 ? 3 : 1) void window_dq_kernel(
     const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
     const T* __restrict__ out, const float* __restrict__ lse, const T* __restrict__ dout,
     float* __restrict__ delta, float* __restrict__ lse2, T* __restrict__ dq, const Shape s,

@@ -27,11 +27,12 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_mfma_kernel(
     const float* __restrict__ lse2, uint16_t* __restrict__ dk, uint16_t* __restrict__ dv,
     const Shape s, const Far far, uint32_t key_tiles, uint32_t items)
 {
-    constexpr int KS = D / 16, DT = D / 32, RT = D == 64 ? 64 : 32, ROW = 2 * D, TILE = RT * ROW;
-    constexpr int VB = D == 64 ? 16 : 32 * ROW;         // (no V in LDS at head dim 64)
+    using R = Rows<D>;
+    constexpr int KS = D / 16, DT = D / 32, RT = D == 64 ? 64 : 32, TILE = R::bytes(RT);
+    constexpr int VB = D == 64 ? 16 : R::bytes(32);     // (no V in LDS at head dim 64)
     using G = Gather<D, RT, 4>;
-    // [buffer][Q, dO]; the buffers alternate by bit 14 of the address
-    __shared__ __attribute__((aligned(32768))) unsigned char tiles_s[2][2][TILE];
+    // [buffer][Q, dO]
+    __shared__ __attribute__((aligned(1024))) unsigned char tiles_s[2][2][TILE];
     __shared__ __attribute__((aligned(1024))) float rows_s[2][2][64];    // [buffer][lse, delta]
     __shared__ __attribute__((aligned(1024))) unsigned char v_s[4][VB];
 
@@ -78,7 +79,7 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_mfma_kernel(
             kf[ks] = here ? *(const bf16x8*)(kp + 16 * ks) : bf16x8{};
             const bf16x8 x = negated(here ? *(const bf16x8*)(vp + 16 * ks) : bf16x8{});
             if constexpr (D == 64) vf[ks] = x;
-            else *(bf16x8*)(v_s[wave] + l32 * ROW + swz(l32, 2 * ks + half) * 16) = x;
+            else *(bf16x8*)(v_s[wave] + R::place(l32, 2 * ks + half)) = x;
         }
     }
     const float c2 = s.scale * kLog2e;
@@ -87,34 +88,16 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_mfma_kernel(
     for (int dt = 0; dt < DT; ++dt) ak[dt] = av[dt] = splat(0.0f);
 
     // addresses of this lane's fragments in the buffer that is read next
-    uint32_t row_at[4], v_at[4], tr_at[2], val_at;
-    {
-        const uint32_t base = lds_address(tiles_s), vbase = lds_address(v_s[wave]);
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-            const uint32_t at = (uint32_t)(l32 * ROW + swz(l32, 2 * ks + half) * 16);
-            row_at[ks] = base + at;
-            v_at[ks] = vbase + at;
-        }
-        const int s16 = lane & 15, gq4 = lane >> 4, r = 4 * (gq4 >> 1) + (s16 >> 2);
-#pragma unroll
-        for (int dt = 0; dt < 2; ++dt) {
-            const int col = 16 * (gq4 & 1) + 4 * (s16 & 3) + 32 * dt;
-            tr_at[dt] = base + (uint32_t)(r * ROW + swz(r, col >> 3) * 16 + (col & 7) * 2);
-        }
-        val_at = lds_address(rows_s) + 16u * (uint32_t)half;
-    }
+    uint32_t row_at[4], v_at[4], tr_at[DT], val_at = lds_address(rows_s) + 16u * (uint32_t)half;
+    R::row_addresses(lds_address(tiles_s), lane, row_at);
+    R::row_addresses(lds_address(v_s[wave]), lane, v_at);
+    R::trans_addresses(lds_address(tiles_s), lane, tr_at);
+    uint32_t to_other = 2u * TILE;                      // from this buffer to the other one
     auto row_frag = [&](int is_g, int row0, int ks) {
-        return lds_read<bf16x8>(row_at[ks & 3], is_g * TILE + row0 * ROW + (ks >> 2) * 128);
+        return lds_read<bf16x8>(row_at[R::index(ks)], is_g * TILE + R::bytes(row0) + R::offset(ks));
     };
     auto trans_frag = [&](int is_g, int row0, int dt) {
-        bf16x4 part[2];
-#pragma unroll
-        for (int rd = 0; rd < 2; ++rd)
-            part[rd] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
-                (__attribute__((address_space(3))) bf16x4*)(uintptr_t)(
-                    tr_at[dt & 1] + (uint32_t)(is_g * TILE + (row0 + 8 * rd) * ROW + (dt >> 1) * 128)));
-        return __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
+        return R::trans_frag(tr_at[dt] + (uint32_t)(is_g * TILE), row0);
     };
 
     // What S starts from: 0, and -infinity where the lane's key does not see the query, which
@@ -209,7 +192,7 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_mfma_kernel(
             if (i < 8) return row_frag(0, 0, i);
             if (i < 24) {
                 const int ks = (i - 8) >> 1;
-                if (i & 1) return lds_read<bf16x8>(v_at[ks & 3], (ks >> 2) * 128);
+                if (i & 1) return lds_read<bf16x8>(v_at[R::index(ks)], R::offset(ks));
                 return row_frag(1, 0, ks);
             }
             return trans_frag(i < 32, 16 * ((i >> 2) & 1), i & 3);
@@ -294,8 +277,10 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_mfma_kernel(
         head = next_head;
         t0 = next_t0;
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) row_at[ks] ^= 16384u;
-        tr_at[0] ^= 16384u; tr_at[1] ^= 16384u;
+        for (int i = 0; i < 4; ++i) row_at[i] += to_other;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) tr_at[dt] += to_other;
+        to_other = 0u - to_other;
         val_at ^= 512u;
     }
     if (jw / 32 < far.groups) add_far<D>(far, slice, jw / 32, l32, half, ak, av, -1.0f);
@@ -316,10 +301,11 @@ __global__ __launch_bounds__(256, 2) void window_dq_mfma_kernel(
     const uint16_t* __restrict__ dout, float* __restrict__ delta, float* __restrict__ lse2,
     uint16_t* __restrict__ dq, const Shape s, uint32_t row_tiles, uint32_t items)
 {
-    constexpr int KS = D / 16, DT = D / 32, ROW = 2 * D, TILE = 64 * ROW;
+    using R = Rows<D>;
+    constexpr int KS = D / 16, DT = D / 32, TILE = R::bytes(64);
     using G = KeyGather<D, 64, 4>;
     // [buffer][K, V]
-    __shared__ __attribute__((aligned(4 * TILE))) unsigned char tiles_s[2][2][TILE];
+    __shared__ __attribute__((aligned(1024))) unsigned char tiles_s[2][2][TILE];
 
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -339,9 +325,9 @@ __global__ __launch_bounds__(256, 2) void window_dq_mfma_kernel(
 
     const uint32_t k_stride = (uint32_t)s.k.token * 2u, v_stride = (uint32_t)s.v.token * 2u;
     const i32x4 k_rsrc = buffer_desc(k + (int64_t)b * s.k.batch + (int64_t)a * s.k.head,
-                                     (uint32_t)(s.k_tokens - 1) * k_stride + ROW);
+                                     (uint32_t)(s.k_tokens - 1) * k_stride + R::ROW_BYTES);
     const i32x4 v_rsrc = buffer_desc(v + (int64_t)b * s.v.batch + (int64_t)a * s.v.head,
-                                     (uint32_t)(s.k_tokens - 1) * v_stride + ROW);
+                                     (uint32_t)(s.k_tokens - 1) * v_stride + R::ROW_BYTES);
     auto issue = [&](int c) {
         G::gather(k_rsrc, k_stride, keys, 64 * c, lds_address(tiles_s[c & 1][0]), wave, lane);
         G::gather(v_rsrc, v_stride, keys, 64 * c, lds_address(tiles_s[c & 1][1]), wave, lane);
@@ -389,30 +375,13 @@ __global__ __launch_bounds__(256, 2) void window_dq_mfma_kernel(
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) acc[dt] = splat(0.0f);
 
-    uint32_t row_at[4], tr_at[2];
-    {
-        const uint32_t base = lds_address(tiles_s);
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks) row_at[ks] = base + (uint32_t)(l32 * ROW + swz(l32, 2 * ks + half) * 16);
-        const int s16 = lane & 15, gq4 = lane >> 4, r = 4 * (gq4 >> 1) + (s16 >> 2);
-#pragma unroll
-        for (int dt = 0; dt < 2; ++dt) {
-            const int col = 16 * (gq4 & 1) + 4 * (s16 & 3) + 32 * dt;
-            tr_at[dt] = base + (uint32_t)(r * ROW + swz(r, col >> 3) * 16 + (col & 7) * 2);
-        }
-    }
+    uint32_t row_at[4], tr_at[DT], to_other = 2u * TILE;
+    R::row_addresses(lds_address(tiles_s), lane, row_at);
+    R::trans_addresses(lds_address(tiles_s), lane, tr_at);
     auto row_frag = [&](int is_v, int r0, int ks) {
-        return lds_read<bf16x8>(row_at[ks & 3], is_v * TILE + r0 * ROW + (ks >> 2) * 128);
+        return lds_read<bf16x8>(row_at[R::index(ks)], is_v * TILE + R::bytes(r0) + R::offset(ks));
     };
-    auto trans_frag = [&](int r0, int dt) {
-        bf16x4 part[2];
-#pragma unroll
-        for (int rd = 0; rd < 2; ++rd)
-            part[rd] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
-                (__attribute__((address_space(3))) bf16x4*)(uintptr_t)(
-                    tr_at[dt & 1] + (uint32_t)((r0 + 8 * rd) * ROW + (dt >> 1) * 128)));
-        return __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
-    };
+    auto trans_frag = [&](int r0, int dt) { return R::trans_frag(tr_at[dt], r0); };
 
     // One tile of 64 keys: S^T and dP^T of both halves, then dQ^T += K^T dS^T of both; behind dP of a
     // half go its exponentials, behind what follows the products.  Fragments are read W ahead.
@@ -496,8 +465,10 @@ __global__ __launch_bounds__(256, 2) void window_dq_mfma_kernel(
             tile(st);
         }
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) row_at[ks] ^= 2u * TILE;
-        tr_at[0] ^= 2u * TILE; tr_at[1] ^= 2u * TILE;
+        for (int i = 0; i < 4; ++i) row_at[i] += to_other;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) tr_at[dt] += to_other;
+        to_other = 0u - to_other;
     }
     __syncthreads();                                    // the tiles are used up
     store_wave_rows<D>(dq + (int64_t)b * s.dq.batch + (int64_t)a * s.group * s.dq.head, s.dq, s,

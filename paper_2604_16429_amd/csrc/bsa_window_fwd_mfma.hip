@@ -25,12 +25,13 @@ __global__ __launch_bounds__(256, 2) void window_fwd_mfma_kernel(
     uint16_t* __restrict__ out, float* __restrict__ lse, const Shape s, const Parts parts,
     uint32_t row_tiles, uint32_t items)
 {
-    constexpr int KS = D / 16, DT = D / 32, ROW = 2 * D, TILE = 64 * ROW;
+    using R = Rows<D>;
+    constexpr int KS = D / 16, DT = D / 32, TILE = R::bytes(64);
     constexpr int SLOTS = KS + 2 * DT;                 // matrix instructions of a step
     constexpr int PER = 16 / SLOTS;                    // weights behind each: 1, at head dim 64 2
     using G = KeyGather<D, 64, 4>;
     // K, then V: two buffers each
-    __shared__ __attribute__((aligned(4 * TILE))) unsigned char tiles_s[2][2][TILE];
+    __shared__ __attribute__((aligned(1024))) unsigned char tiles_s[2][2][TILE];
 
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -57,9 +58,9 @@ __global__ __launch_bounds__(256, 2) void window_fwd_mfma_kernel(
 
     const uint32_t k_stride = (uint32_t)s.k.token * 2u, v_stride = (uint32_t)s.v.token * 2u;
     const i32x4 k_rsrc = buffer_desc(k + (int64_t)b * s.k.batch + (int64_t)a * s.k.head,
-                                     (uint32_t)(s.k_tokens - 1) * k_stride + ROW);
+                                     (uint32_t)(s.k_tokens - 1) * k_stride + R::ROW_BYTES);
     const i32x4 v_rsrc = buffer_desc(v + (int64_t)b * s.v.batch + (int64_t)a * s.v.head,
-                                     (uint32_t)(s.k_tokens - 1) * v_stride + ROW);
+                                     (uint32_t)(s.k_tokens - 1) * v_stride + R::ROW_BYTES);
     auto issue_k = [&](int c) {
         if (c < c_e) G::gather(k_rsrc, k_stride, keys, 64 * c, lds_address(tiles_s[0][(c - c_a) & 1]), wave, lane);
     };
@@ -88,36 +89,30 @@ __global__ __launch_bounds__(256, 2) void window_fwd_mfma_kernel(
     float m_ref = kNoRef, l_run = 0.0f;
 
     // addresses of this lane's fragments: K of the buffer read next, V likewise
-    uint32_t k_at[4], v_at[2];
-    {
-        const uint32_t base = lds_address(tiles_s);
+    uint32_t k_at[4], v_at[DT], k_other = TILE, v_other = TILE;      // ... and the way to the other one
+    R::row_addresses(lds_address(tiles_s[0][0]), lane, k_at);
+    R::trans_addresses(lds_address(tiles_s[1][0]), lane, v_at);
+    auto swap_k = [&] {
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) k_at[ks] = base + (uint32_t)(l32 * ROW + swz(l32, 2 * ks + half) * 16);
-        const int s16 = lane & 15, gq4 = lane >> 4, r = 4 * (gq4 >> 1) + (s16 >> 2);
+        for (int i = 0; i < 4; ++i) k_at[i] += k_other;
+        k_other = 0u - k_other;
+    };
+    auto swap_v = [&] {
 #pragma unroll
-        for (int dt = 0; dt < 2; ++dt) {
-            const int col = 16 * (gq4 & 1) + 4 * (s16 & 3) + 32 * dt;
-            v_at[dt] = base + (uint32_t)(2 * TILE + r * ROW + swz(r, col >> 3) * 16 + (col & 7) * 2);
-        }
-    }
+        for (int dt = 0; dt < DT; ++dt) v_at[dt] += v_other;
+        v_other = 0u - v_other;
+    };
     bf16x8 kf[KS], vf[DT][2];
     auto read_k = [&](int hh) {
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) kf[ks] = lds_read<bf16x8>(k_at[ks & 3], hh * 32 * ROW + (ks >> 2) * 128);
+        for (int ks = 0; ks < KS; ++ks)
+            kf[ks] = lds_read<bf16x8>(k_at[R::index(ks)], R::bytes(32 * hh) + R::offset(ks));
     };
     auto read_v = [&](int hh) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt) {
-                bf16x4 part[2];
-#pragma unroll
-                for (int rd = 0; rd < 2; ++rd)
-                    part[rd] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
-                        (__attribute__((address_space(3))) bf16x4*)(uintptr_t)(
-                            v_at[dt & 1] + (uint32_t)((32 * hh + 16 * h + 8 * rd) * ROW + (dt >> 1) * 128)));
-                vf[dt][h] = __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
-            }
+            for (int dt = 0; dt < DT; ++dt) vf[dt][h] = R::trans_frag(v_at[dt], 32 * hh + 16 * h);
     };
 
     if (c_a < c_e) {
@@ -132,8 +127,7 @@ __global__ __launch_bounds__(256, 2) void window_fwd_mfma_kernel(
             st[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], qf[ks], st[0], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
         read_k(1);
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks) k_at[ks] ^= TILE;
+        swap_k();
         // the first step adds nothing to O
         p[1][0] = p[1][1] = bf16x8{};
 #pragma unroll
@@ -226,12 +220,11 @@ __global__ __launch_bounds__(256, 2) void window_fwd_mfma_kernel(
             step(std::integral_constant<int, 1>{}, 64 * c + 64,
                  [&] {
                      read_k(1);
-#pragma unroll
-                     for (int ks = 0; ks < 4; ++ks) k_at[ks] ^= TILE;
+                     swap_k();
                  },
                  [&] {
                      read_v(1);
-                     v_at[0] ^= TILE; v_at[1] ^= TILE;
+                     swap_v();
                  });
         }
 #pragma unroll
