@@ -72,9 +72,10 @@ __global__ __launch_bounds__(256, D == 32 ? 3 : 1) void window_dq_kernel(
     unsigned char* const v_lds = tiles_s[NARROW ? wave : 0][1];
     const int loader = NARROW ? lane : tid;
 
-    const uint32_t item = item_of(blockIdx.x, items);
-    const uint32_t slice = item / row_tiles;
-    const int row0 = (int)(item - slice * row_tiles) * ROWS;
+    uint32_t slice;
+    int tile_at;
+    map_item(s, blockIdx.x, items, row_tiles, true, slice, tile_at);
+    const int row0 = tile_at * ROWS;
     const int b = (int)(slice / (uint32_t)s.kv_heads), a = (int)(slice - (uint32_t)b * s.kv_heads);
     int ql, kl;
     lengths(s, b, ql, kl);
@@ -272,9 +273,9 @@ __global__ __launch_bounds__(256) void window_dkdv_kernel(
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, half = lane >> 5;
 
-    const uint32_t item = item_of(blockIdx.x, items);
-    const uint32_t slice = item / key_tiles;
-    const int key_tile = (int)(item - slice * key_tiles);
+    uint32_t slice;
+    int key_tile;
+    map_item(s, blockIdx.x, items, key_tiles, false, slice, key_tile);
     const int b = (int)(slice / (uint32_t)s.kv_heads), a = (int)(slice - (uint32_t)b * s.kv_heads);
     int ql, kl;
     lengths(s, b, ql, kl);
@@ -363,11 +364,10 @@ __global__ __launch_bounds__((64 * narrow_waves<T, D>())) void window_dkdv_narro
     const int l32 = lane & 31, half = lane >> 5;
 
     const uint32_t chunks = FAR ? (uint32_t)far.chunks : 1u;
-    const uint32_t work = item_of(blockIdx.x, items);
-    const int chunk = (int)(work % chunks);
-    const uint32_t item = work / chunks;
-    const uint32_t slice = item / key_groups;
-    const int group = (int)(item - slice * key_groups);
+    const int chunk = (int)(blockIdx.x % chunks);
+    uint32_t slice;
+    int group;
+    map_item(s, blockIdx.x / chunks, items / chunks, key_groups, false, slice, group);
     const int b = (int)(slice / (uint32_t)s.kv_heads), a = (int)(slice - (uint32_t)b * s.kv_heads);
     int ql, kl;
     lengths(s, b, ql, kl);

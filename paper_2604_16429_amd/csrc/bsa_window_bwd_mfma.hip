@@ -40,9 +40,9 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_mfma_kernel(
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l32 = lane & 31, half = lane >> 5;
 
-    const uint32_t item = item_of(blockIdx.x, items);
-    const uint32_t slice = item / key_tiles;
-    const int key_tile = (int)(item - slice * key_tiles);
+    uint32_t slice;
+    int key_tile;
+    map_item(s, blockIdx.x, items, key_tiles, false, slice, key_tile);
     const int b = (int)(slice / (uint32_t)s.kv_heads), a = (int)(slice - (uint32_t)b * s.kv_heads);
     int ql, kl;
     lengths(s, b, ql, kl);
@@ -311,9 +311,10 @@ __global__ __launch_bounds__(256, 2) void window_dq_mfma_kernel(
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l32 = lane & 31, half = lane >> 5;
 
-    const uint32_t item = item_of(blockIdx.x, items);
-    const uint32_t slice = item / row_tiles;
-    const int row0 = (int)(item - slice * row_tiles) * 128;
+    uint32_t slice;
+    int tile_at;
+    map_item(s, blockIdx.x, items, row_tiles, true, slice, tile_at);
+    const int row0 = tile_at * 128;
     const int b = (int)(slice / (uint32_t)s.kv_heads), a = (int)(slice - (uint32_t)b * s.kv_heads);
     int ql, kl;
     lengths(s, b, ql, kl);

@@ -34,11 +34,12 @@ __global__ __launch_bounds__(256) void window_fwd_kernel(const T* __restrict__ q
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, half = lane >> 5;
 
-    const uint32_t work = item_of(blockIdx.x, items);
-    const int split = (int)(work % (uint32_t)parts.splits);
-    const uint32_t item = work / (uint32_t)parts.splits;
-    const uint32_t slice = item / row_tiles;
-    const int row0 = (int)(item - slice * row_tiles) * 128;
+    const int split = (int)(blockIdx.x % (uint32_t)parts.splits);
+    uint32_t slice;
+    int tile_at;
+    map_item(s, blockIdx.x / (uint32_t)parts.splits, items / (uint32_t)parts.splits, row_tiles, true,
+             slice, tile_at);
+    const int row0 = tile_at * 128;
     const int b = (int)(slice / (uint32_t)s.kv_heads), a = (int)(slice - (uint32_t)b * s.kv_heads);
     int ql, kl;
     lengths(s, b, ql, kl);

@@ -74,11 +74,12 @@ __global__ __launch_bounds__(64 * W) void window_step_kernel(
     const int l16 = lane & 15, grp = lane >> 4;
     unsigned char* const mine = lds + wave * REGION;
 
-    const uint32_t work = item_of(blockIdx.x, items);
-    const int split = (int)(work % (uint32_t)parts.splits);
-    const uint32_t item = work / (uint32_t)parts.splits;
-    const uint32_t slice = item / row_tiles;
-    const int row0 = (int)(item - slice * row_tiles) * (16 * NR), row_n = min(16 * NR, s.rows - row0);
+    const int split = (int)(blockIdx.x % (uint32_t)parts.splits);
+    uint32_t slice;
+    int tile_at;
+    map_item(s, blockIdx.x / (uint32_t)parts.splits, items / (uint32_t)parts.splits, row_tiles, true,
+             slice, tile_at);
+    const int row0 = tile_at * (16 * NR), row_n = min(16 * NR, s.rows - row0);
     const int b = (int)(slice / (uint32_t)s.kv_heads), a = (int)(slice - (uint32_t)b * s.kv_heads);
     int ql, kl;
     lengths(s, b, ql, kl);
