@@ -460,8 +460,8 @@ __global__ __launch_bounds__(256, 2) void window_dq_mfma_kernel(
         if (rows.any(64 * c, 64)) {
             f32x16 st[2] = {splat(0.0f), splat(0.0f)};
             if (!rows.all(64 * c, 64)) {
-                st[0] = start_of(see, 64 * c, half);
-                st[1] = start_of(see, 64 * c + 32, half);
+                st[0] = start_of(see, 64 * c, half, rows.sinks);
+                st[1] = start_of(see, 64 * c + 32, half, rows.sinks);
             }
             tile(st);
         }

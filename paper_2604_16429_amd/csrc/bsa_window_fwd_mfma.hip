@@ -122,7 +122,7 @@ __global__ __launch_bounds__(256, 2) void window_fwd_mfma_kernel(
         wait_gathers_and_reads();
         __syncthreads();
         read_k(0);
-        st[0] = rows.all(64 * c_a, 32) ? splat(0.0f) : start_of(see, 64 * c_a, half);
+        st[0] = rows.all(64 * c_a, 32) ? splat(0.0f) : start_of(see, 64 * c_a, half, rows.sinks);
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks)
             st[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], qf[ks], st[0], 0, 0, 0);
@@ -162,7 +162,7 @@ __global__ __launch_bounds__(256, 2) void window_fwd_mfma_kernel(
             if (rows.all(next_slot, 32))
                 st[1 - J] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[0], qf[0], splat(0.0f), 0, 0, 0);
             else
-                st[1 - J] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[0], qf[0], start_of(see, next_slot, half), 0, 0, 0);
+                st[1 - J] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[0], qf[0], start_of(see, next_slot, half, rows.sinks), 0, 0, 0);
             f[0][0] = fmaf(st[J][0], c2, neg_m);
             f[0][1] = fmaf(st[J][1], c2, neg_m);
             __builtin_amdgcn_sched_barrier(0);

@@ -130,13 +130,24 @@ inline bool slices_fit(const Shape& s)
 }
 
 // What S^T of a 32 x 32 tile starts from: 0, and -infinity for slots that the lane's query does not
-// see, which makes their weights 0.
-__device__ __forceinline__ f32x16 start_of(const Sight& see, int slot0, int half)
+// see, which makes their weights 0.  Slots below `sinks` (of all the wavefront's queries) take one
+// comparison more.
+__device__ __forceinline__ f32x16 start_of(const Sight& see, int slot0, int half, int sinks)
 {
     f32x16 st;
+    const uint32_t x = (uint32_t)(slot0 + 4 * half - see.first);
+    if (slot0 < sinks) {
+        const int y = see.sinks - slot0 - 4 * half;
 #pragma unroll
-    for (int e = 0; e < 16; ++e)
-        st[e] = see.sees(slot0 + 8 * (e >> 2) + (e & 3) + 4 * half) ? 0.0f : -INFINITY;
+        for (int e = 0; e < 16; ++e) {
+            const int c = 8 * (e >> 2) + (e & 3);
+            st[e] = x + (uint32_t)c <= see.span || c < y ? 0.0f : -INFINITY;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            st[e] = x + (uint32_t)(8 * (e >> 2) + (e & 3)) <= see.span ? 0.0f : -INFINITY;
+    }
     return st;
 }
 
