@@ -440,14 +440,14 @@ size_t row_bytes(const Shape& s)
 }
 
 // Launches of few workgroups of 128 keys give every 32 keys a workgroup of their own.
-bool is_narrow(const Shape& s)
+bool is_narrow(bool mfma, const Shape& s)
 {
-    return (int64_t)s.batch * s.kv_heads * ((s.k_tokens + kKeys - 1) / kKeys) < 256;
+    return (int64_t)s.batch * s.kv_heads * ((s.k_tokens + kKeys - 1) / kKeys) < (mfma ? 128 : 256);
 }
 
-Far far_of(const Shape& s)
+Far far_of(const Shape& s, bool narrow)
 {
-    Far f = {nullptr, 0, 0, is_narrow(s) ? 32 : kKeys};
+    Far f = {nullptr, 0, 0, narrow ? 32 : kKeys};
     // queries beyond the window of a sink exist where the window is shorter than the sequence
     if (s.sinks == 0 || s.left >= s.k_tokens) return f;
     f.groups = (s.sinks + 31) / 32;
@@ -460,7 +460,7 @@ Far far_of(const Shape& s)
 
 size_t far_bytes(const Shape& s, int D)
 {
-    const Far f = far_of(s);
+    const Far f = far_of(s, false);                    // (the same sums either way)
     return rounded((size_t)s.batch * s.kv_heads * f.groups * f.chunks * 64 * D * sizeof(float));
 }
 
@@ -475,13 +475,14 @@ hipError_t launch_bwd(const Shape& s, const void* q_, const void* k_, const void
     const int64_t slices = (int64_t)s.batch * s.kv_heads;
     float* delta = (float*)workspace;
     float* lse2 = (float*)((char*)workspace + row_bytes(s));
-    Far far = far_of(s);
+    const bool mfma = window_bwd_mfma_supported(sizeof(T) == 2, D, s), narrow = is_narrow(mfma, s);
+    Far far = far_of(s, narrow);
     far.sums = (float*)((char*)workspace + 2 * row_bytes(s));
 
     hipError_t e;
     // launches of fewer workgroups of 128 rows than CUs: 32 rows to each
     const bool few_rows = slices * (((int64_t)s.rows + 127) / 128) < 256;
-    if (!few_rows && window_bwd_mfma_supported(sizeof(T) == 2, D, s)) {
+    if (!few_rows && mfma) {
         e = launch_window_dq_mfma(D, s, q, k, v, out, lse, dout, delta, lse2, dq, stream);
     } else {
         const uint32_t per = few_rows ? 32 : 128, row_tiles = ((uint32_t)s.rows + per - 1) / per;
@@ -499,13 +500,13 @@ hipError_t launch_bwd(const Shape& s, const void* q_, const void* k_, const void
             q, k, v, dout, delta, lse2, dk, dv, s, far, (uint32_t)far.groups, n);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
-    const uint32_t per = is_narrow(s) ? 32 : kKeys;
+    const uint32_t per = narrow ? 32 : kKeys;
     const uint32_t key_tiles = ((uint32_t)s.k_tokens + per - 1) / per;
     const uint32_t k_items = (uint32_t)slices * key_tiles;
-    if (is_narrow(s))
+    if (narrow)
         window_dkdv_narrow_kernel<T, D, false><<<k_items, 64 * narrow_waves<T, D>(), 0, stream>>>(
             q, k, v, dout, delta, lse2, dk, dv, s, far, key_tiles, k_items);
-    else if (window_bwd_mfma_supported(sizeof(T) == 2, D, s))
+    else if (mfma)
         return launch_window_dkdv_mfma(D, s, q, k, v, dout, delta, lse2, dk, dv, far, stream);
     else
         window_dkdv_kernel<T, D><<<k_items, 256, 0, stream>>>(q, k, v, dout, delta, lse2, dk, dv, s, far,
