@@ -439,7 +439,9 @@ size_t row_bytes(const Shape& s)
     return rounded((size_t)s.batch * s.kv_heads * s.rows * sizeof(float));
 }
 
-// Launches of few workgroups of 128 keys give every 32 keys a workgroup of their own.
+// Launches of few workgroups of 128 keys give every 32 keys a workgroup of their own.  Four query heads to
+// a key head, us, narrow | not: 120 workgroups, head dim 64, windows 64 and 300 32 | 43 and 40 | 65;
+// from 128 on, whole training pass, head dim 128, window 700: 142 334 | 289, 204 425 | 326.
 bool is_narrow(bool mfma, const Shape& s)
 {
     return (int64_t)s.batch * s.kv_heads * ((s.k_tokens + kKeys - 1) / kKeys) < (mfma ? 128 : 256);
@@ -480,8 +482,10 @@ hipError_t launch_bwd(const Shape& s, const void* q_, const void* k_, const void
     far.sums = (float*)((char*)workspace + 2 * row_bytes(s));
 
     hipError_t e;
-    // launches of fewer workgroups of 128 rows than CUs: 32 rows to each
-    const bool few_rows = slices * (((int64_t)s.rows + 127) / 128) < 256;
+    // launches of few workgroups of 128 rows: 32 rows to each.  The matrix-core kernel is the faster one
+    // from about 96 on (us, narrow | not, head dim 64 and 128, window 300: 64 workgroups 11.3 | 12.4
+    // and 16.6 | 17.4, 128 13.9 | 13.2 and 31 | 18).
+    const bool few_rows = slices * (((int64_t)s.rows + 127) / 128) < (mfma ? 96 : 256);
     if (!few_rows && mfma) {
         e = launch_window_dq_mfma(D, s, q, k, v, out, lse, dout, delta, lse2, dq, stream);
     } else {
