@@ -24,28 +24,28 @@ namespace win {
 template <typename T, int D>
 constexpr int narrow_waves() { return D * (int)sizeof(T) <= 128 ? 8 : 4; }
 
-// A wavefront's values lane by lane through LDS: those of wavefronts 1 .. are added to wavefront 0's in
-// their order.  `lds` has room for one wavefront's.  All wavefronts call it.
+// The wavefronts' values lane by lane through LDS: those of wavefronts 1 .. are added to wavefront 0's in
+// their order.  All wavefronts call it.
+template <int NW, int COUNT>
+constexpr int add_waves_bytes() { return (NW - 1) * COUNT * 16 * 64 * 4; }
 template <int NW, int COUNT>
 __device__ __forceinline__ void add_waves(unsigned char* lds, int wave, int lane, f32x16 (&x)[COUNT])
 {
     float* const region = (float*)lds + lane;
-    for (int w = 1; w < NW; ++w) {
-        __syncthreads();
-        if (wave == w) {
+    __syncthreads();                                    // the tiles (the last values) are used up
+    if (wave > 0) {
 #pragma unroll
-            for (int c = 0; c < COUNT; ++c)
+        for (int c = 0; c < COUNT; ++c)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) region[(c * 16 + r) * 64] = x[c][r];
-        }
-        __syncthreads();
-        if (wave == 0) {
-#pragma unroll
-            for (int c = 0; c < COUNT; ++c)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) x[c][r] += region[(c * 16 + r) * 64];
-        }
+            for (int r = 0; r < 16; ++r) region[(((wave - 1) * COUNT + c) * 16 + r) * 64] = x[c][r];
     }
+    __syncthreads();
+    if (wave > 0) return;
+    for (int w = 0; w < NW - 1; ++w)
+#pragma unroll
+        for (int c = 0; c < COUNT; ++c)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) x[c][r] += region[((w * COUNT + c) * 16 + r) * 64];
 }
 
 // NARROW: the four wavefronts own the same 32 rows and take the tiles of keys in turn, with tiles of
@@ -63,7 +63,7 @@ __global__ __launch_bounds__(256, D == 32 ? 3 : 1) void window_dq_kernel(
     using M = Mma<T>;
     using Frag = typename M::Frag;
     __shared__ __attribute__((aligned(1024))) unsigned char tiles_s[SETS][2][Tl::BYTES];
-    static_assert(!NARROW || DT * 16 * 64 * 4 <= (int)sizeof(tiles_s), "a wavefront's sums fit the tiles");
+    static_assert(!NARROW || add_waves_bytes<4, DT>() <= (int)sizeof(tiles_s), "the sums fit the tiles");
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -357,7 +357,7 @@ __global__ __launch_bounds__((64 * narrow_waves<T, D>())) void window_dkdv_narro
     using Frag = typename Mma<T>::Frag;
     __shared__ __attribute__((aligned(1024))) unsigned char tiles_s[NW][2][Tl::BYTES];
     __shared__ float l2_s[NW][RT], dl_s[NW][RT];
-    static_assert(DT * 16 * 64 * 4 <= (int)sizeof(tiles_s), "a wavefront's sums fit the tiles");
+    static_assert(add_waves_bytes<NW, DT>() <= (int)sizeof(tiles_s), "the sums fit the tiles");
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
