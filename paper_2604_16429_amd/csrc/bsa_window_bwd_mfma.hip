@@ -100,20 +100,18 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_mfma_kernel(
         return R::trans_frag(tr_at[dt] + (uint32_t)(is_g * TILE), row0);
     };
 
-    // What S starts from: 0, and -infinity where the lane's key does not see the query, which
-    // makes the weight 0.
-    auto start_of = [&](bool full, const Column& col) {
-        f32x16 st = splat(0.0f);
-        if (!full) {
+    // What S starts from in a tile that the window's border crosses: 0, and -infinity where the lane's
+    // key does not see the query, which makes the weight 0.
+    auto start_of = [&](const Column& col) {
+        f32x16 st;
 #pragma unroll
-            for (int e = 0; e < 16; ++e)
-                st[e] = col.seen(8 * (e >> 2) + (e & 3) + 4 * half) ? 0.0f : -INFINITY;
-        }
+        for (int e = 0; e < 16; ++e)
+            st[e] = col.seen(8 * (e >> 2) + (e & 3) + 4 * half) ? 0.0f : -INFINITY;
         return st;
     };
     // One tile, D = 64: S, dP of tokens 0..31, then of 32..63 with the weights of the first half
     // behind them, dV, dK of the first half with the weights of the second, dV, dK of the second.
-    auto tile64 = [&](f32x16 (&st)[2]) {
+    auto tile64 = [&](bool full, int pa, int n) __attribute__((always_inline)) {
         constexpr int W = 8;                            // fragments read ahead
         auto read_frag = [&](int i) -> bf16x8 {
             const int u = i & 3;
@@ -121,7 +119,7 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_mfma_kernel(
             return trans_frag(1 - ((i >> 2) & 1), 32 * ((i - 16) >> 3) + 16 * (u >> 1), u & 1);
         };
         bf16x8 f[W];
-        f32x16 dp[2];
+        f32x16 st[2], dp[2];
         f32x4 l4[4];
         uint32_t pw[2][8], dw[2][8];
         float fm[2][2], ex[2][2];
@@ -145,8 +143,13 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_mfma_kernel(
             const bf16x8 x = f[i % W];
             if (i < 16) {
                 const int qt = i >> 3;
-                if ((i & 4) == 0)
+                if ((i & 4) == 0 && u > 0)
                     st[qt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, kf[u], st[qt], 0, 0, 0);
+                else if ((i & 4) == 0 && full)          // (the constant 0 takes no registers)
+                    st[qt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, kf[u], splat(0.0f), 0, 0, 0);
+                else if ((i & 4) == 0)
+                    st[qt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                        x, kf[u], start_of(column(s, j, kl, pa + 32 * qt, n - 32 * qt)), 0, 0, 0);
                 else
                     dp[qt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, vf[D == 64 ? u : 0], dp[qt], 0, 0, 0);
             } else {
@@ -185,7 +188,7 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_mfma_kernel(
         }
     };
     // One tile, D = 128: S, dP, dV, dK; exponentials behind dP, products behind dV.
-    auto tile128 = [&](f32x16 st) {
+    auto tile128 = [&](bool full, int pa, int n) __attribute__((always_inline)) {
         constexpr int W = 6;
         // 0-7 Q rows (S), 8-23 dO rows and V in turn (dP), 24-31 dO transposed (dV), 32-39 Q (dK)
         auto read_frag = [&](int i) -> bf16x8 {
@@ -198,7 +201,7 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_mfma_kernel(
             return trans_frag(i < 32, 16 * ((i >> 2) & 1), i & 3);
         };
         bf16x8 f[W];
-        f32x16 dp;
+        f32x16 st, dp;
         f32x4 l4[2];
         uint32_t pw[8], dw[8];
         float fm[2][2];
@@ -211,7 +214,13 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_mfma_kernel(
 #pragma unroll
         for (int t = 0; t < 32; ++t) {
             const int i = t & 7, h = i >> 2, dt = i & 3;
-            if (t < 8) {
+            if (t == 0) {
+                if (full)                               // (the constant 0 takes no registers)
+                    st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[0], kf[0], splat(0.0f), 0, 0, 0);
+                else
+                    st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[0], kf[0], start_of(column(s, j, kl, pa, n)), 0, 0, 0);
+                ask(0);
+            } else if (t < 8) {
                 st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % W], kf[i % KS], st, 0, 0, 0);
                 ask(i);
             } else if (t < 16) {
@@ -266,13 +275,8 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_mfma_kernel(
         const bool full = n == RT && jw + 31 < kl && jw + 31 <= pa + s.right &&
                           (jw >= pa + RT - 1 - s.left || jw + 31 < s.sinks);
         if (any) {
-            if constexpr (D == 64) {
-                f32x16 st[2] = {start_of(full, column(s, j, kl, pa, n)),
-                                start_of(full, column(s, j, kl, pa + 32, n - 32))};
-                tile64(st);
-            } else {
-                tile128(start_of(full, column(s, j, kl, pa, n)));
-            }
+            if constexpr (D == 64) tile64(full, pa, n);
+            else tile128(full, pa, n);
         }
         head = next_head;
         t0 = next_t0;
@@ -386,15 +390,16 @@ __global__ __launch_bounds__(256, 2) void window_dq_mfma_kernel(
 
     // One tile of 64 keys: S^T and dP^T of both halves, then dQ^T += K^T dS^T of both; behind dP of a
     // half go its exponentials, behind what follows the products.  Fragments are read W ahead.
-    auto tile = [&](f32x16 (&st)[2]) {
+    auto tile = [&](int slot0) __attribute__((always_inline)) {
         constexpr int W = 8, N = KS, ALL = 4 * N + 4 * DT;       // matrix instructions
+        const bool full = rows.all(slot0, 64);
         auto read_frag = [&](int i) -> bf16x8 {
             if (i < 4 * N) return row_frag((i / N) & 1, 32 * (i / (2 * N)), i % N);
             const int u = i - 4 * N;
             return trans_frag(32 * (u / (2 * DT)) + 16 * ((u / DT) & 1), u % DT);
         };
         bf16x8 f[W];
-        f32x16 dp[2];
+        f32x16 st[2], dp[2];
         uint32_t w[2][8];
         float fm[2][2];
 #pragma unroll
@@ -403,13 +408,28 @@ __global__ __launch_bounds__(256, 2) void window_dq_mfma_kernel(
         // two weights to a slot at head dim 128, four at 64: the fma from slot F on, exponentials a
         // slot later, products from slot X on
         constexpr int PER = 16 / N, F = N + 1, X = 2 * N + 2;
-#pragma unroll
-        for (int t = 0; t < ALL; ++t) {
+        // What S^T of a half starts from.  Head dim 64: its first product stands apart, where the constant 0
+        // of a tile without border takes no registers (195 -> 186 us); at 128 the registers that
+        // this leaves in the way cost more than 32 moves (1,430 -> 1,700).
+        constexpr bool APART = D == 64;
+        auto start = [&](int hh) __attribute__((always_inline)) {
+            if (!APART) {
+                st[hh] = full ? splat(0.0f) : start_of(see, slot0 + 32 * hh, half, rows.sinks);
+                return;
+            }
+            const bf16x8 x = f[(2 * N * hh) % W];
+            if (full)
+                st[hh] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, qf[0], splat(0.0f), 0, 0, 0);
+            else
+                st[hh] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                    x, qf[0], start_of(see, slot0 + 32 * hh, half, rows.sinks), 0, 0, 0);
+        };
+        auto slot = [&](int t) __attribute__((always_inline)) {
             if (t < 4 * N) {
                 const int hh = t / (2 * N), u = t % N;
                 if ((t / N) & 1)
                     dp[hh] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[t % W], gf[u], u == 0 ? neg_dl : dp[hh], 0, 0, 0);
-                else
+                else if (!APART || u > 0)
                     st[hh] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[t % W], qf[u], st[hh], 0, 0, 0);
             } else {
                 const int u = t - 4 * N, hh = u / (2 * DT), h = (u / DT) & 1, dt = u % DT;
@@ -450,21 +470,21 @@ __global__ __launch_bounds__(256, 2) void window_dq_mfma_kernel(
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
-        }
+        };
+        start(0);
+        if (!APART) start(1);
+#pragma unroll
+        for (int t = 0; t < 2 * N; ++t) slot(t);
+        if (APART) start(1);
+#pragma unroll
+        for (int t = 2 * N; t < ALL; ++t) slot(t);
     };
     for (int c = 0; c < tiles; ++c) {
         // tile c has landed and everyone is done with the other buffer
         wait_gathers();
         __syncthreads();
         if (c + 1 < tiles) issue(c + 1);
-        if (rows.any(64 * c, 64)) {
-            f32x16 st[2] = {splat(0.0f), splat(0.0f)};
-            if (!rows.all(64 * c, 64)) {
-                st[0] = start_of(see, 64 * c, half, rows.sinks);
-                st[1] = start_of(see, 64 * c + 32, half, rows.sinks);
-            }
-            tile(st);
-        }
+        if (rows.any(64 * c, 64)) tile(64 * c);
 #pragma unroll
         for (int i = 0; i < 4; ++i) row_at[i] += to_other;
 #pragma unroll
