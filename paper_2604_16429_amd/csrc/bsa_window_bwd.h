@@ -10,8 +10,9 @@ namespace win {
 constexpr int kKeys = 128;             // keys of a workgroup whose wavefronts share tiles
 constexpr float kNoWeight = 3.0e38f;   // lse of a row without keys: its weights are 0
 
-// Sums of the queries beyond the window of the tiles that hold sinks: [slices][groups][chunks][2]
-// [32][D] floats, dK (without the scale) and dV of groups of 32 keys.
+// Sums of the queries beyond the window of the tiles that hold sinks: [slices][groups][chunks + 1][2]
+// [32][D] floats, dK (without the scale) and dV of groups of 32 keys; the last ones are those of the
+// queries inside the window, where both are made by one launch.
 struct Far {
     float* sums;
     int32_t groups, chunks;            // groups of keys that hold sinks (0: no such queries)
@@ -70,7 +71,7 @@ template <int D>
 __device__ __forceinline__ void add_far(const Far& far, int64_t slice, int group, int l32, int half,
                                         f32x16 (&ak)[D / 32], f32x16 (&av)[D / 32], float k_sign)
 {
-    const float* p = far.sums + ((slice * far.groups + group) * far.chunks) * (int64_t)(64 * D) + l32 * D;
+    const float* p = far.sums + ((slice * far.groups + group) * (far.chunks + 1)) * (int64_t)(64 * D) + l32 * D;
     for (int c = 0; c < far.chunks; ++c, p += 64 * D) {
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt)

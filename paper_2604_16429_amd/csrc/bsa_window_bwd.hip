@@ -11,7 +11,8 @@
 // A sink is seen by every later query, the keys behind it by window ones: a workgroup that owns
 // sinks would walk the whole sequence.  What lies beyond the window of a tile that holds sinks is
 // cut into chunks of queries, each with a workgroup of its own that leaves fp32 sums for 32 keys
-// in the workspace; the tile's own workgroup adds them in the order of the chunks before it rounds.
+// in the workspace; the tile's own workgroup, or in small launches a kernel after it, adds them in the
+// order of the chunks before it rounds.
 #include "bsa_window_bwd.h"
 
 #include "bsa_launch.h"
@@ -343,14 +344,15 @@ __global__ __launch_bounds__(256) void window_dkdv_kernel(
 
 // dK and dV of 32 keys: the wavefronts own the same keys and take the tiles of queries in turn,
 // with tiles of their own and no barrier between them; their sums are added in the order of the
-// wavefronts.  FAR: the queries beyond the window of the tile that holds the keys, one chunk to a
-// workgroup, sums to the workspace; else all inside the window.
-template <typename T, int D, bool FAR>
+// wavefronts.  Workgroups below far_items take one chunk of the queries beyond the window of the tile
+// that holds the keys and leave sums in the workspace; the others take those inside the window of
+// their group of keys and leave sums too where the keys hold sinks.
+template <typename T, int D>
 __global__ __launch_bounds__((64 * narrow_waves<T, D>())) void window_dkdv_narrow_kernel(
     const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
     const T* __restrict__ dout, const float* __restrict__ delta, const float* __restrict__ lse2,
     T* __restrict__ dk, T* __restrict__ dv, const Shape s, const Far far, uint32_t key_groups,
-    uint32_t items)
+    uint32_t far_items, uint32_t items)
 {
     constexpr int RT = 32, KS = D / 16, DT = D / 32, NW = narrow_waves<T, D>();
     using Tl = Tile<T, D, RT, 64>;
@@ -363,19 +365,22 @@ __global__ __launch_bounds__((64 * narrow_waves<T, D>())) void window_dkdv_narro
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, half = lane >> 5;
 
-    const uint32_t chunks = FAR ? (uint32_t)far.chunks : 1u;
-    const int chunk = (int)(blockIdx.x % chunks);
+    const bool is_far = blockIdx.x < far_items;
+    const uint32_t chunks = is_far ? (uint32_t)far.chunks : 1u;
+    const uint32_t w = is_far ? blockIdx.x / chunks : blockIdx.x - far_items;
+    const int chunk = is_far ? (int)(blockIdx.x - w * chunks) : far.chunks;
     uint32_t slice;
     int group;
-    map_item(s, blockIdx.x / chunks, items / chunks, key_groups, false, slice, group);
+    map_item(s, w, is_far ? far_items / chunks : items - far_items,
+             is_far ? (uint32_t)far.groups : key_groups, false, slice, group);
     const int b = (int)(slice / (uint32_t)s.kv_heads), a = (int)(slice - (uint32_t)b * s.kv_heads);
     int ql, kl;
     lengths(s, b, ql, kl);
     const int p0 = kl - ql;
     const int jw = 32 * group, j = jw + l32;
-    const Span span = FAR ? far_span(s, jw / far.near_keys * far.near_keys, far.near_keys, p0, ql, kl,
-                                     chunk, (int)chunks)
-                          : near_span(s, jw, 32, p0, ql, kl);
+    const Span span = is_far ? far_span(s, jw / far.near_keys * far.near_keys, far.near_keys, p0, ql, kl,
+                                        chunk, far.chunks)
+                             : near_span(s, jw, 32, p0, ql, kl);
 
     Frag kf[KS], vf[KS];
     load_keys<T, D>(k, v, s, b, a, j, is_seen(s, j, p0, ql, kl), half, kf, vf);
@@ -416,20 +421,45 @@ __global__ __launch_bounds__((64 * narrow_waves<T, D>())) void window_dkdv_narro
     add_waves<NW>(&tiles_s[0][0][0], wave, lane, ak);
     add_waves<NW>(&tiles_s[0][0][0], wave, lane, av);
     if (wave != 0) return;
-    if constexpr (FAR) {
-        float* p = far.sums + (((int64_t)slice * far.groups + group) * far.chunks + chunk) * (64 * D) +
+    if (group < far.groups) {
+        float* p = far.sums + (((int64_t)slice * far.groups + group) * (far.chunks + 1) + chunk) * (64 * D) +
                    l32 * D;
         store_lane_row<float, D>(p, ak, 1.0f, half);
         store_lane_row<float, D>(p + 32 * D, av, 1.0f, half);
-    } else {
-        if (group < far.groups) add_far<D>(far, slice, group, l32, half, ak, av, 1.0f);
-        if (j < s.k_tokens) {
-            store_lane_row<T, D>(dk + (int64_t)b * s.dk.batch + (int64_t)a * s.dk.head +
-                                     (int64_t)j * s.dk.token, ak, s.scale, half);
-            store_lane_row<T, D>(dv + (int64_t)b * s.dv.batch + (int64_t)a * s.dv.head +
-                                     (int64_t)j * s.dv.token, av, 1.0f, half);
-        }
+    } else if (j < s.k_tokens) {
+        store_lane_row<T, D>(dk + (int64_t)b * s.dk.batch + (int64_t)a * s.dk.head +
+                                 (int64_t)j * s.dk.token, ak, s.scale, half);
+        store_lane_row<T, D>(dv + (int64_t)b * s.dv.batch + (int64_t)a * s.dv.head +
+                                 (int64_t)j * s.dv.token, av, 1.0f, half);
     }
+}
+
+// dK and dV of the groups that hold sinks: their sums in the order of the chunks.  A thread has four
+// channels.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void window_sinks_kernel(T* __restrict__ dk, T* __restrict__ dv,
+                                                           const Shape s, const Far far, int64_t quads)
+{
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= quads) return;
+    const int in_part = (int)(at % (16 * D)) * 4;       // [2][32][D]
+    const int64_t which = at / (16 * D), slice = which / far.groups;
+    const int is_v = in_part / (32 * D), key = in_part / D % 32, c = in_part % D;
+    const int j = (int)(which - slice * far.groups) * 32 + key;
+    if (j >= s.k_tokens) return;
+    const float* p = far.sums + which * (far.chunks + 1) * (64 * D) + in_part;
+    float4 sum = *(const float4*)p;
+#pragma unroll 8
+    for (int i = 1; i <= far.chunks; ++i) {
+        const float4 x = *(const float4*)(p + (int64_t)i * (64 * D));
+        sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
+    }
+    const int b = (int)(slice / s.kv_heads), a = (int)(slice - (int64_t)b * s.kv_heads);
+    if (is_v)
+        store4(dv + (int64_t)b * s.dv.batch + (int64_t)a * s.dv.head + (int64_t)j * s.dv.token + c, sum);
+    else
+        store4(dk + (int64_t)b * s.dk.batch + (int64_t)a * s.dk.head + (int64_t)j * s.dk.token + c,
+               make_float4(sum.x * s.scale, sum.y * s.scale, sum.z * s.scale, sum.w * s.scale));
 }
 
 size_t rounded(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -453,9 +483,11 @@ Far far_of(const Shape& s, bool narrow)
     // queries beyond the window of a sink exist where the window is shorter than the sequence
     if (s.sinks == 0 || s.left >= s.k_tokens) return f;
     f.groups = (s.sinks + 31) / 32;
-    // a workgroup per CU and a half, of at least 8 tiles of 32 queries
-    const int64_t slices = (int64_t)s.batch * s.kv_heads;
-    const int64_t want = max((int64_t)1, 384 / (slices * f.groups)), most = max(1, s.rows / 256);
+    // One workgroup of the narrow kernel runs on a CU: a round of them, or what the groups of 32 keys of
+    // the same launch leave of their last round, of at least 8 tiles of 32 queries each.
+    const int64_t slices = (int64_t)s.batch * s.kv_heads, groups = slices * ((s.k_tokens + 31) / 32);
+    const int64_t room = groups >= 1024 ? 256 : max((int64_t)64, (groups + 255) / 256 * 256 - groups);
+    const int64_t want = max((int64_t)1, room / (slices * f.groups)), most = max(1, s.rows / 256);
     f.chunks = (int)min(min(want, most), (int64_t)32);
     return f;
 }
@@ -463,7 +495,7 @@ Far far_of(const Shape& s, bool narrow)
 size_t far_bytes(const Shape& s, int D)
 {
     const Far f = far_of(s, false);                    // (the same sums either way)
-    return rounded((size_t)s.batch * s.kv_heads * f.groups * f.chunks * 64 * D * sizeof(float));
+    return rounded((size_t)s.batch * s.kv_heads * f.groups * (f.chunks + 1) * 64 * D * sizeof(float));
 }
 
 template <typename T, int D>
@@ -498,23 +530,25 @@ hipError_t launch_bwd(const Shape& s, const void* q_, const void* k_, const void
     }
     if (e != hipSuccess) return e;
 
-    if (far.groups) {
-        const uint32_t n = (uint32_t)slices * (uint32_t)(far.groups * far.chunks);
-        window_dkdv_narrow_kernel<T, D, true><<<n, 64 * narrow_waves<T, D>(), 0, stream>>>(
-            q, k, v, dout, delta, lse2, dk, dv, s, far, (uint32_t)far.groups, n);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
     const uint32_t per = narrow ? 32 : kKeys;
     const uint32_t key_tiles = ((uint32_t)s.k_tokens + per - 1) / per;
     const uint32_t k_items = (uint32_t)slices * key_tiles;
-    if (narrow)
-        window_dkdv_narrow_kernel<T, D, false><<<k_items, 64 * narrow_waves<T, D>(), 0, stream>>>(
-            q, k, v, dout, delta, lse2, dk, dv, s, far, key_tiles, k_items);
-    else if (mfma)
-        return launch_window_dkdv_mfma(D, s, q, k, v, dout, delta, lse2, dk, dv, far, stream);
-    else
-        window_dkdv_kernel<T, D><<<k_items, 256, 0, stream>>>(q, k, v, dout, delta, lse2, dk, dv, s, far,
-                                                             key_tiles, k_items);
+    const uint32_t far_items = (uint32_t)slices * (uint32_t)(far.groups * far.chunks);
+    const uint32_t narrow_items = far_items + (narrow ? k_items : 0);
+    if (narrow_items) {
+        window_dkdv_narrow_kernel<T, D><<<narrow_items, 64 * narrow_waves<T, D>(), 0, stream>>>(
+            q, k, v, dout, delta, lse2, dk, dv, s, far, key_tiles, far_items, narrow_items);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    if (narrow) {
+        if (far.groups == 0) return hipSuccess;
+        const int64_t quads = slices * far.groups * (16 * D);
+        window_sinks_kernel<T, D><<<(unsigned)((quads + 255) / 256), 256, 0, stream>>>(dk, dv, s, far, quads);
+        return hipGetLastError();
+    }
+    if (mfma) return launch_window_dkdv_mfma(D, s, q, k, v, dout, delta, lse2, dk, dv, far, stream);
+    window_dkdv_kernel<T, D><<<k_items, 256, 0, stream>>>(q, k, v, dout, delta, lse2, dk, dv, s, far,
+                                                         key_tiles, k_items);
     return hipGetLastError();
 }
 
