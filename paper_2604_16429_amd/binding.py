@@ -124,7 +124,8 @@ class Rotation:
 class _StridedParams:
     """Parameters whose C struct also carries the tensors' strides.  The struct is made when a
     call first needs it and after a parameter was set; a tensor is looked at closely where its
-    type, shape or strides differ from those that its field had in the call before."""
+    type, shape or strides, or what the call wants there, differ from the call before.  One thread
+    at a time uses an object."""
 
     _C = None
     _SCALARS = ()
@@ -154,7 +155,7 @@ class _StridedParams:
                     seen[field] = None
                 pointers.append(t)
                 continue
-            now = (t.shape, t.stride(), t.dtype, t.is_cuda, tokens)
+            now = (t.shape, t.stride(), t.dtype, t.is_cuda, heads, tokens)
             if seen.get(field) != now:
                 self._look(field, t, heads, tokens)
                 seen[field] = now

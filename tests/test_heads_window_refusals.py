@@ -187,6 +187,38 @@ def test_tensors_that_do_not_fit_the_parameters():
         rope(heads(), M.Rotation(64), pos=torch.zeros(8, dtype=torch.int64))
 
 
+class OnGpu:
+    """What the binding looks at of a tensor, without its memory."""
+
+    def __init__(self, *shape, strides=None):
+        x = torch.empty(shape, dtype=torch.bfloat16, device="meta")
+        self.shape, self.dtype, self.is_cuda = x.shape, x.dtype, True
+        self.strides = x.stride() if strides is None else strides
+
+    def stride(self):
+        return self.strides
+
+    def data_ptr(self):
+        return FAKE
+
+
+def test_a_field_that_two_calls_use_is_looked_at_for_each():
+    """v of the forward and dq of the norm's gradient share a field, with other numbers of heads."""
+    p, rot = heads(), M.Rotation(64)
+    q, k = OnGpu(2, 4, 8, 64), OnGpu(2, 2, 8, 64)
+    n = M.mosaic_bsa_qk_norm_rope_workspace_bytes(p)
+    # (a missing weight ends both calls on the host)
+    assert code_of(lambda: M.mosaic_bsa_qk_norm_rope_fwd(p, rot, FAKE, q, k, None, FAKE, q, k, v=k, v_out=k,
+                                                         stream=0)) == -1
+    with pytest.raises(ValueError):
+        M.mosaic_bsa_qk_norm_rope_bwd(p, rot, FAKE, q, k, None, FAKE, q, k, k, k, FAKE, FAKE, FAKE,
+                                      stream=0, workspace_bytes=n)
+    assert code_of(lambda: M.mosaic_bsa_qk_norm_rope_bwd(p, rot, FAKE, q, k, None, FAKE, q, k, q, k, FAKE,
+                                                         FAKE, FAKE, stream=0, workspace_bytes=n)) == -1
+    with pytest.raises(ValueError):
+        M.mosaic_bsa_qk_norm_rope_fwd(p, rot, FAKE, q, k, None, FAKE, q, k, v=q, v_out=k, stream=0)
+
+
 @pytest.mark.parametrize("code", [-10, -11, -12])
 def test_error_texts(code):
     assert M.mosaic_bsa_strerror(code) not in ("", "unknown error code")
