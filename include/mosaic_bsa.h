@@ -81,8 +81,8 @@ enum {
     MOSAIC_BSA_ERR_LAUNCH = -8,    /* HIP refused a launch (see hipGetLastError) */
     MOSAIC_BSA_ERR_OP = -9,        /* unknown op for mosaic_bsa_workspace_bytes */
     MOSAIC_BSA_ERR_ROTATION = -10, /* rotation: rotary_dim, axes, layout or scaling */
-    MOSAIC_BSA_ERR_STRIDE = -11,   /* a stride that is negative, too large, or 0 where
-                                      an output has more than one entry */
+    MOSAIC_BSA_ERR_STRIDE = -11,   /* a stride that is negative or too large, or rows of an
+                                      output that share memory */
     MOSAIC_BSA_ERR_WINDOW = -12    /* window: negative sinks, ring too small for the
                                       window, or a ring in a backward pass */
 };
@@ -304,7 +304,8 @@ int mosaic_bsa_bwd_three_branch(const mosaic_bsa_params *params, int32_t local_h
  */
 /* Strides in elements.  token == 0: a contiguous [batch, heads, tokens, head_dim]
  * tensor (batch and head are then ignored).  batch or head may be 0 in an input
- * that is shared by all of them, never in an output that has more than one. */
+ * that is shared by all of them.  Rows of an output must not share memory: each of its
+ * strides steps over all that the dimensions with smaller strides reach. */
 typedef struct {
     int64_t batch, head, token;
 } mosaic_bsa_strides;

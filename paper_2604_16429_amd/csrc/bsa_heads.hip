@@ -496,7 +496,8 @@ int check_pair(const void* in, const void* out, bool required, const mosaic_bsa_
     const int esz = c.is_bf16 ? 2 : 4;
     if (unaligned(in, esz) || unaligned(out, esz)) return MOSAIC_BSA_ERR_ALIGN;
     if (bad_strides(is, batch, heads, tokens, c.D, false) ||
-        bad_strides(os, batch, heads, out_tokens, c.D, true))
+        bad_strides(os, batch, heads, out_tokens, c.D, true) ||
+        rows_meet(os, batch, heads, out_tokens, c.D))
         return MOSAIC_BSA_ERR_STRIDE;
     return MOSAIC_BSA_OK;
 }

@@ -68,6 +68,7 @@ int check_tensor(const Checked& c, const void* ptr, const mosaic_bsa_strides& st
     *to = bsa::strides_of(st, heads, tokens, D);
     if ((uintptr_t)ptr & 15u || to->batch % per16 || to->head % per16 || to->token % per16)
         return MOSAIC_BSA_ERR_ALIGN;
+    if (output && bsa::rows_meet(st, c.s.batch, heads, tokens, D)) return MOSAIC_BSA_ERR_STRIDE;
     return MOSAIC_BSA_OK;
 }
 

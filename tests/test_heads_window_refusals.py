@@ -219,6 +219,34 @@ def test_a_field_that_two_calls_use_is_looked_at_for_each():
         M.mosaic_bsa_qk_norm_rope_fwd(p, rot, FAKE, q, k, None, FAKE, q, k, v=q, v_out=k, stream=0)
 
 
+@pytest.mark.parametrize("strides,bad", [
+    ((64, 64, 64), True),            # heads and tokens on each other
+    ((4096, 64, 128), True),         # four heads of 64 channels in tokens 128 apart
+    ((4096, 64, 255), True),
+    ((1024, 512, 64), True),         # batch entries inside each other
+    ((2048, 64, 256), False), ((2048, 512, 64), False), ((64, 1024, 128), False),
+    ((1 << 40, 64, 256), False),
+])
+def test_rows_of_an_output_that_share_memory(strides, bad):
+    rot, p = M.Rotation(64), heads()
+    p._c().q_out = binding._CStrides(*strides)
+    lib = M.load_library()
+    # (k without k_out ends the call on the host where the strides pass)
+    assert code_of(lambda: binding._check(lib.mosaic_bsa_rope_fwd(
+        p._ref, rot.ref, FAKE, FAKE, FAKE, None, None, FAKE, None, None, None))) == (-11 if bad else -1)
+    if strides[2] % 8 == 0:
+        p = window()
+        p._c().dq = binding._CStrides(*strides)
+        # (no workspace)
+        assert code_of(lambda: win_bwd_as_it_is(p)) == (-11 if bad else -6)
+
+
+def win_bwd_as_it_is(p):
+    """The C entry point with the strides that the struct has."""
+    binding._check(M.load_library().mosaic_bsa_window_bwd(
+        p._ref, *([FAKE] * 6), None, None, *([FAKE] * 3), None, 0, None))
+
+
 @pytest.mark.parametrize("code", [-10, -11, -12])
 def test_error_texts(code):
     assert M.mosaic_bsa_strerror(code) not in ("", "unknown error code")
