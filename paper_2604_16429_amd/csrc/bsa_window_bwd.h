@@ -19,6 +19,26 @@ struct Far {
     int32_t near_keys;                 // a group's tile is this many keys: 32 or kKeys
 };
 
+// Launches of few workgroups share the walk of a workgroup's keys out to `splits` of them, which leave
+// sums: [slices][groups of 32 keys][splits][2][32][D] floats, dK (without the scale) and dV.  A kernel
+// after them adds these, then the far sums, in their order.
+struct Near {
+    float* sums;
+    int32_t groups, splits;            // splits 1: none
+    // tiles first .. end - 1 of `all`, those of split `split`
+    __device__ __forceinline__ void share(int split, int all, int& first, int& end) const
+    {
+        const int per = (all + splits - 1) / splits;
+        first = min(all, split * per);
+        end = min(all, first + per);
+    }
+};
+template <int D>
+__device__ __forceinline__ float* near_part(const Near& near, uint32_t slice, int group, int split, int key)
+{
+    return near.sums + (((int64_t)slice * near.groups + group) * near.splits + split) * (64 * D) + key * D;
+}
+
 // Query tokens a .. e - 1 of a sequence that see keys J .. J + n - 1 inside the window.
 struct Span {
     int a, e;
@@ -97,6 +117,6 @@ hipError_t launch_window_dq_mfma(int D, const win::Shape& s, const void* q, cons
 hipError_t launch_window_dkdv_mfma(int D, const win::Shape& s, const void* q, const void* k,
                                    const void* v, const void* dout, const float* delta,
                                    const float* lse2, void* dk, void* dv, const win::Far& far,
-                                   hipStream_t stream);
+                                   const win::Near& near, hipStream_t stream);
 
 }  // namespace bsa

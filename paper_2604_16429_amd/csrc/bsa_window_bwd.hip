@@ -13,6 +13,8 @@
 // cut into chunks of queries, each with a workgroup of its own that leaves fp32 sums for 32 keys
 // in the workspace; the tile's own workgroup, or in small launches a kernel after it, adds them in the
 // order of the chunks before it rounds.
+#include <algorithm>
+
 #include "bsa_window_bwd.h"
 
 #include "bsa_launch.h"
@@ -259,8 +261,8 @@ template <typename T, int D>
 __global__ __launch_bounds__(256) void window_dkdv_kernel(
     const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
     const T* __restrict__ dout, const float* __restrict__ delta, const float* __restrict__ lse2,
-    T* __restrict__ dk, T* __restrict__ dv, const Shape s, const Far far, uint32_t key_tiles,
-    uint32_t items)
+    T* __restrict__ dk, T* __restrict__ dv, const Shape s, const Far far, const Near near,
+    uint32_t key_tiles, uint32_t items)
 {
     constexpr int RT = sizeof(T) == 2 ? 64 : 32;        // tokens of a tile
     constexpr int KS = D / 16, DT = D / 32;
@@ -276,7 +278,8 @@ __global__ __launch_bounds__(256) void window_dkdv_kernel(
 
     uint32_t slice;
     int key_tile;
-    map_item(s, blockIdx.x, items, key_tiles, false, slice, key_tile);
+    const int split = (int)(blockIdx.x / items);
+    map_item(s, blockIdx.x - (uint32_t)split * items, items, key_tiles, false, slice, key_tile);
     const int b = (int)(slice / (uint32_t)s.kv_heads), a = (int)(slice - (uint32_t)b * s.kv_heads);
     int ql, kl;
     lengths(s, b, ql, kl);
@@ -307,10 +310,12 @@ __global__ __launch_bounds__(256) void window_dkdv_kernel(
         }
     };
     const int tiles = span.e > span.a ? (span.e - span.a + RT - 1) / RT : 0;
-    const int all = tiles * s.group;
-    if (all > 0) fetch(a * s.group, span.a);
-    int head = a * s.group, t0 = span.a;
-    for (int it = 0; it < all; ++it) {
+    int it0, all;                                       // this workgroup's tiles, head by head
+    near.share(split, tiles * s.group, it0, all);
+    const int head0 = it0 < all ? it0 / tiles : 0;
+    int head = a * s.group + head0, t0 = span.a + (it0 - head0 * tiles) * RT;
+    if (it0 < all) fetch(head, t0);
+    for (int it = it0; it < all; ++it) {
         __syncthreads();
         qt.put(q_lds, tid);
         gt.put(g_lds, tid);
@@ -333,6 +338,14 @@ __global__ __launch_bounds__(256) void window_dkdv_kernel(
         head = next_head;
         t0 = next_t0;
     }
+    if (near.splits > 1) {
+        if (jw / 32 < near.groups) {
+            float* p = near_part<D>(near, slice, jw / 32, split, l32);
+            store_lane_row<float, D>(p, ak, 1.0f, half);
+            store_lane_row<float, D>(p + 32 * D, av, 1.0f, half);
+        }
+        return;
+    }
     if (jw / 32 < far.groups) add_far<D>(far, slice, jw / 32, l32, half, ak, av, 1.0f);
     if (j < s.k_tokens) {
         store_lane_row<T, D>(dk + (int64_t)b * s.dk.batch + (int64_t)a * s.dk.head +
@@ -346,13 +359,13 @@ __global__ __launch_bounds__(256) void window_dkdv_kernel(
 // with tiles of their own and no barrier between them; their sums are added in the order of the
 // wavefronts.  Workgroups below far_items take one chunk of the queries beyond the window of the tile
 // that holds the keys and leave sums in the workspace; the others take those inside the window of
-// their group of keys and leave sums too where the keys hold sinks.
+// their group of keys, or a share of them, and leave sums too where it is a share or the keys hold sinks.
 template <typename T, int D>
 __global__ __launch_bounds__((64 * narrow_waves<T, D>())) void window_dkdv_narrow_kernel(
     const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
     const T* __restrict__ dout, const float* __restrict__ delta, const float* __restrict__ lse2,
-    T* __restrict__ dk, T* __restrict__ dv, const Shape s, const Far far, uint32_t key_groups,
-    uint32_t far_items, uint32_t items)
+    T* __restrict__ dk, T* __restrict__ dv, const Shape s, const Far far, const Near near,
+    uint32_t key_groups, uint32_t far_items, uint32_t near_items)
 {
     constexpr int RT = 32, KS = D / 16, DT = D / 32, NW = narrow_waves<T, D>();
     using Tl = Tile<T, D, RT, 64>;
@@ -367,12 +380,13 @@ __global__ __launch_bounds__((64 * narrow_waves<T, D>())) void window_dkdv_narro
 
     const bool is_far = blockIdx.x < far_items;
     const uint32_t chunks = is_far ? (uint32_t)far.chunks : 1u;
-    const uint32_t w = is_far ? blockIdx.x / chunks : blockIdx.x - far_items;
+    const int split = is_far ? 0 : (int)((blockIdx.x - far_items) / near_items);
+    const uint32_t w = is_far ? blockIdx.x / chunks : blockIdx.x - far_items - (uint32_t)split * near_items;
     const int chunk = is_far ? (int)(blockIdx.x - w * chunks) : far.chunks;
     uint32_t slice;
     int group;
-    map_item(s, w, is_far ? far_items / chunks : items - far_items,
-             is_far ? (uint32_t)far.groups : key_groups, false, slice, group);
+    map_item(s, w, is_far ? far_items / chunks : near_items, is_far ? (uint32_t)far.groups : key_groups,
+             false, slice, group);
     const int b = (int)(slice / (uint32_t)s.kv_heads), a = (int)(slice - (uint32_t)b * s.kv_heads);
     int ql, kl;
     lengths(s, b, ql, kl);
@@ -392,7 +406,8 @@ __global__ __launch_bounds__((64 * narrow_waves<T, D>())) void window_dkdv_narro
     Tl qt, gt;
     float row_held = 0.0f;                              // lse in lanes 0 .. 31, delta in the others
     const int tiles = span.e > span.a ? (span.e - span.a + RT - 1) / RT : 0;
-    const int all = tiles * s.group;
+    int it0 = 0, all = tiles * s.group;
+    if (!is_far) near.share(split, all, it0, all);
     auto fetch = [&](int it) {
         const int hd = it / tiles, head = a * s.group + hd, t0 = span.a + (it - hd * tiles) * RT;
         const T* qb = q + (int64_t)b * s.q.batch + (int64_t)head * s.q.head + (int64_t)t0 * s.q.token;
@@ -404,8 +419,8 @@ __global__ __launch_bounds__((64 * narrow_waves<T, D>())) void window_dkdv_narro
         const int64_t at = ((int64_t)b * s.heads + head) * s.q_tokens + t0 + l32;
         row_held = l32 < n ? (half ? delta[at] : lse2[at]) : half ? 0.0f : kNoWeight;
     };
-    if (wave < all) fetch(wave);
-    for (int it = wave; it < all; it += NW) {
+    if (it0 + wave < all) fetch(it0 + wave);
+    for (int it = it0 + wave; it < all; it += NW) {
         lane_exchange();
         qt.put(tiles_s[wave][0], lane);
         gt.put(tiles_s[wave][1], lane);
@@ -421,7 +436,11 @@ __global__ __launch_bounds__((64 * narrow_waves<T, D>())) void window_dkdv_narro
     add_waves<NW>(&tiles_s[0][0][0], wave, lane, ak);
     add_waves<NW>(&tiles_s[0][0][0], wave, lane, av);
     if (wave != 0) return;
-    if (group < far.groups) {
+    if (!is_far && near.splits > 1) {
+        float* p = near_part<D>(near, slice, group, split, l32);
+        store_lane_row<float, D>(p, ak, 1.0f, half);
+        store_lane_row<float, D>(p + 32 * D, av, 1.0f, half);
+    } else if (group < far.groups) {
         float* p = far.sums + (((int64_t)slice * far.groups + group) * (far.chunks + 1) + chunk) * (64 * D) +
                    l32 * D;
         store_lane_row<float, D>(p, ak, 1.0f, half);
@@ -434,26 +453,34 @@ __global__ __launch_bounds__((64 * narrow_waves<T, D>())) void window_dkdv_narro
     }
 }
 
-// dK and dV of the groups that hold sinks: their sums in the order of the chunks.  A thread has four
-// channels.
+// dK and dV of the first `groups` groups of 32 keys of each slice: shares of the near walk in their
+// order, if there are any, then the far sums of groups that hold sinks in the order of the chunks (the
+// last of which is the near walk where that is not shared out).  A thread has four channels.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void window_sinks_kernel(T* __restrict__ dk, T* __restrict__ dv,
-                                                           const Shape s, const Far far, int64_t quads)
+__global__ __launch_bounds__(256) void window_keys_kernel(T* __restrict__ dk, T* __restrict__ dv,
+                                                          const Shape s, const Far far, const Near near,
+                                                          int groups, int64_t quads)
 {
     const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (at >= quads) return;
     const int in_part = (int)(at % (16 * D)) * 4;       // [2][32][D]
-    const int64_t which = at / (16 * D), slice = which / far.groups;
+    const int64_t which = at / (16 * D), slice = which / groups;
     const int is_v = in_part / (32 * D), key = in_part / D % 32, c = in_part % D;
-    const int j = (int)(which - slice * far.groups) * 32 + key;
+    const int group = (int)(which - slice * groups), j = group * 32 + key;
     if (j >= s.k_tokens) return;
-    const float* p = far.sums + which * (far.chunks + 1) * (64 * D) + in_part;
-    float4 sum = *(const float4*)p;
+    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    auto add = [&](const float* p, int n) __attribute__((always_inline)) {
 #pragma unroll 8
-    for (int i = 1; i <= far.chunks; ++i) {
-        const float4 x = *(const float4*)(p + (int64_t)i * (64 * D));
-        sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
-    }
+        for (int i = 0; i < n; ++i) {
+            const float4 x = *(const float4*)(p + (int64_t)i * (64 * D));
+            sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
+        }
+    };
+    const bool shared = near.splits > 1;
+    if (shared) add(near_part<D>(near, (uint32_t)slice, group, 0, 0) + in_part, near.splits);
+    if (group < far.groups)
+        add(far.sums + (slice * far.groups + group) * (far.chunks + 1) * (64 * D) + in_part,
+            far.chunks + (shared ? 0 : 1));
     const int b = (int)(slice / s.kv_heads), a = (int)(slice - (int64_t)b * s.kv_heads);
     if (is_v)
         store4(dv + (int64_t)b * s.dv.batch + (int64_t)a * s.dv.head + (int64_t)j * s.dv.token + c, sum);
@@ -469,33 +496,64 @@ size_t row_bytes(const Shape& s)
     return rounded((size_t)s.batch * s.kv_heads * s.rows * sizeof(float));
 }
 
-// Launches of few workgroups of 128 keys give every 32 keys a workgroup of their own.  Four query heads to
-// a key head, us, narrow | not: 120 workgroups, head dim 64, windows 64 and 300 32 | 43 and 40 | 65;
-// from 128 on, whole training pass, head dim 128, window 700: 142 334 | 289, 204 425 | 326.
-bool is_narrow(bool mfma, const Shape& s)
-{
-    return (int64_t)s.batch * s.kv_heads * ((s.k_tokens + kKeys - 1) / kKeys) < (mfma ? 128 : 256);
-}
+// How dK and dV are launched.
+struct Plan {
+    bool narrow;                       // 32 keys a workgroup
+    Far far;
+    Near near;
+    size_t far_bytes, near_bytes;
+};
 
-Far far_of(const Shape& s, bool narrow)
+// Few workgroups of 128 keys: every 32 keys get one of their own.  Four query heads to a key head, us,
+// narrow | not: 120 workgroups, head dim 64, windows 64 and 300 32 | 43 and 40 | 65; from 128 on, whole
+// training pass, head dim 128, window 700: 142 334 | 289, 204 425 | 326.
+//
+// Where that leaves CUs idle, or one round and a bit of workgroups, the walk is shared out.  us, whole |
+// shared: under 256 workgroups, up to 512 shares of 4 tiles at least: head dim 128, window 641, 237 191 |
+// 114, both sides 1,555, 196 579 | 456, head dim 64, window 219, 184 95 | 77; 256 to 511 (any number in
+// the kernels without an order of their own), up to 2,048 of 16 tiles (24 with one): head dim 64, both sides 2,577, 354
+// 1,157 | 1,033, fp32, head dim 32, window 482, 944 2,800 | 2,460 (with shares of 4 tiles: head dim 128,
+// window 56, 295 92 | 124; with an order of their own, 840 workgroups 557 | 633).
+Plan plan_of(bool mfma, int element, int D, const Shape& s)
 {
-    Far f = {nullptr, 0, 0, narrow ? 32 : kKeys};
+    Plan p;
+    const int64_t slices = (int64_t)s.batch * s.kv_heads, groups = ((int64_t)s.k_tokens + 31) / 32;
+    const int64_t key_tiles = slices * (((int64_t)s.k_tokens + kKeys - 1) / kKeys);
+    p.narrow = key_tiles < (mfma ? 128 : 256);
+    // shares of workgroups with n keys: at least `least` tiles of `rows` queries to each
+    auto shares = [&](int64_t room, int64_t workgroups, int n, int rows, int least) {
+        const int64_t left = min(s.left, s.k_tokens), right = min(s.right, s.k_tokens);
+        const int64_t walk = min((int64_t)s.q_tokens, left + right + n);
+        const int64_t tiles = (walk + rows - 1) / rows * s.group;
+        return (int)max((int64_t)1, min(min(room / workgroups, tiles / least), (int64_t)32));
+    };
+    int splits;
+    if (p.narrow) {
+        const int waves = D * element <= 128 ? 8 : 4;
+        splits = shares(256, slices * groups, 32, 32, 2 * waves);
+    } else {
+        const int rows = element == 4 || (mfma && D == 128) ? 32 : 64;
+        splits = key_tiles < 256            ? shares(512, key_tiles, kKeys, rows, 4)
+                 : mfma && key_tiles >= 512 ? 1
+                                            : shares(2048, key_tiles, kKeys, rows, mfma ? 24 : 16);
+    }
+    p.near = {nullptr, (int32_t)groups, splits};
+    p.near_bytes = p.near.splits == 1 ? 0 : rounded((size_t)(slices * groups * p.near.splits) * 64 * D * sizeof(float));
+
+    p.far = {nullptr, 0, 0, p.narrow ? 32 : kKeys};
+    p.far_bytes = 0;
     // queries beyond the window of a sink exist where the window is shorter than the sequence
-    if (s.sinks == 0 || s.left >= s.k_tokens) return f;
+    if (s.sinks == 0 || s.left >= s.k_tokens) return p;
+    Far& f = p.far;
     f.groups = (s.sinks + 31) / 32;
     // One workgroup of the narrow kernel runs on a CU: a round of them, or what the groups of 32 keys of
     // the same launch leave of their last round, of at least 8 tiles of 32 queries each.
-    const int64_t slices = (int64_t)s.batch * s.kv_heads, groups = slices * ((s.k_tokens + 31) / 32);
-    const int64_t room = groups >= 1024 ? 256 : max((int64_t)64, (groups + 255) / 256 * 256 - groups);
+    const int64_t beside = slices * groups * p.near.splits;
+    const int64_t room = p.narrow ? max((int64_t)64, (beside + 255) / 256 * 256 - beside) : 256;
     const int64_t want = max((int64_t)1, room / (slices * f.groups)), most = max(1, s.rows / 256);
     f.chunks = (int)min(min(want, most), (int64_t)32);
-    return f;
-}
-
-size_t far_bytes(const Shape& s, int D)
-{
-    const Far f = far_of(s, false);                    // (the same sums either way)
-    return rounded((size_t)s.batch * s.kv_heads * f.groups * (f.chunks + 1) * 64 * D * sizeof(float));
+    p.far_bytes = rounded((size_t)slices * f.groups * (f.chunks + 1) * 64 * D * sizeof(float));
+    return p;
 }
 
 template <typename T, int D>
@@ -509,9 +567,13 @@ hipError_t launch_bwd(const Shape& s, const void* q_, const void* k_, const void
     const int64_t slices = (int64_t)s.batch * s.kv_heads;
     float* delta = (float*)workspace;
     float* lse2 = (float*)((char*)workspace + row_bytes(s));
-    const bool mfma = window_bwd_mfma_supported(sizeof(T) == 2, D, s), narrow = is_narrow(mfma, s);
-    Far far = far_of(s, narrow);
+    const bool mfma = window_bwd_mfma_supported(sizeof(T) == 2, D, s);
+    Plan plan = plan_of(mfma, (int)sizeof(T), D, s);
+    Far& far = plan.far;
+    Near& near = plan.near;
+    const bool narrow = plan.narrow;
     far.sums = (float*)((char*)workspace + 2 * row_bytes(s));
+    near.sums = (float*)((char*)far.sums + plan.far_bytes);
 
     hipError_t e;
     // launches of few workgroups of 128 rows: 32 rows to each.  The matrix-core kernel is the faster one
@@ -534,29 +596,42 @@ hipError_t launch_bwd(const Shape& s, const void* q_, const void* k_, const void
     const uint32_t key_tiles = ((uint32_t)s.k_tokens + per - 1) / per;
     const uint32_t k_items = (uint32_t)slices * key_tiles;
     const uint32_t far_items = (uint32_t)slices * (uint32_t)(far.groups * far.chunks);
-    const uint32_t narrow_items = far_items + (narrow ? k_items : 0);
+    const uint32_t narrow_items = far_items + (narrow ? k_items * (uint32_t)near.splits : 0);
     if (narrow_items) {
         window_dkdv_narrow_kernel<T, D><<<narrow_items, 64 * narrow_waves<T, D>(), 0, stream>>>(
-            q, k, v, dout, delta, lse2, dk, dv, s, far, key_tiles, far_items, narrow_items);
+            q, k, v, dout, delta, lse2, dk, dv, s, far, near, key_tiles, far_items, k_items);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
-    if (narrow) {
-        if (far.groups == 0) return hipSuccess;
-        const int64_t quads = slices * far.groups * (16 * D);
-        window_sinks_kernel<T, D><<<(unsigned)((quads + 255) / 256), 256, 0, stream>>>(dk, dv, s, far, quads);
-        return hipGetLastError();
+    if (!narrow) {
+        if (mfma) {
+            e = launch_window_dkdv_mfma(D, s, q, k, v, dout, delta, lse2, dk, dv, far, near, stream);
+        } else {
+            window_dkdv_kernel<T, D><<<k_items * (uint32_t)near.splits, 256, 0, stream>>>(
+                q, k, v, dout, delta, lse2, dk, dv, s, far, near, key_tiles, k_items);
+            e = hipGetLastError();
+        }
+        if (e != hipSuccess) return e;
     }
-    if (mfma) return launch_window_dkdv_mfma(D, s, q, k, v, dout, delta, lse2, dk, dv, far, stream);
-    window_dkdv_kernel<T, D><<<k_items, 256, 0, stream>>>(q, k, v, dout, delta, lse2, dk, dv, s, far,
-                                                         key_tiles, k_items);
+    const int groups = near.splits > 1 ? near.groups : narrow ? far.groups : 0;
+    if (groups == 0) return hipSuccess;
+    const int64_t quads = slices * groups * (16 * D);
+    window_keys_kernel<T, D><<<(unsigned)((quads + 255) / 256), 256, 0, stream>>>(dk, dv, s, far, near,
+                                                                                 groups, quads);
     return hipGetLastError();
 }
 
 }  // namespace win
 
-size_t window_bwd_workspace(bool, int D, const win::Shape& s)
+size_t window_bwd_workspace(bool is_bf16, int D, const win::Shape& s)
 {
-    return 2 * win::row_bytes(s) + win::far_bytes(s, D);
+    // (without strides, on which the choice of kernels depends: enough for either)
+    size_t most = 0;
+    for (const bool mfma : {false, true}) {
+        if (mfma && !(is_bf16 && D >= 64)) continue;
+        const win::Plan p = win::plan_of(mfma, is_bf16 ? 2 : 4, D, s);
+        most = std::max(most, p.far_bytes + p.near_bytes);
+    }
+    return 2 * win::row_bytes(s) + most;
 }
 
 hipError_t launch_window_bwd(bool is_bf16, int D, const win::Shape& s, const void* q, const void* k,

@@ -19,13 +19,14 @@ namespace bsa {
 
 namespace win {
 
-// D = 64: tiles of 64 tokens, V in registers.  D = 128: tiles of 32, V in LDS.
-template <int D>
+// D = 64: tiles of 64 tokens, V in registers.  D = 128: tiles of 32, V in LDS.  SHARED: the walk is
+// shared out.
+template <int D, bool SHARED>
 __global__ __launch_bounds__(256, 2) void window_dkdv_mfma_kernel(
     const uint16_t* __restrict__ q, const uint16_t* __restrict__ k, const uint16_t* __restrict__ v,
     const uint16_t* __restrict__ dout, const float* __restrict__ delta,
     const float* __restrict__ lse2, uint16_t* __restrict__ dk, uint16_t* __restrict__ dv,
-    const Shape s, const Far far, uint32_t key_tiles, uint32_t items)
+    const Shape s, const Far far, const Near near, uint32_t key_tiles, uint32_t items)
 {
     using R = Rows<D>;
     constexpr int KS = D / 16, DT = D / 32, RT = D == 64 ? 64 : 32, TILE = R::bytes(RT);
@@ -42,7 +43,9 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_mfma_kernel(
 
     uint32_t slice;
     int key_tile;
-    map_item(s, blockIdx.x, items, key_tiles, false, slice, key_tile);
+    const int split = SHARED ? (int)(blockIdx.x / items) : 0;
+    map_item(s, SHARED ? blockIdx.x - (uint32_t)split * items : blockIdx.x, items, key_tiles, false, slice,
+             key_tile);
     const int b = (int)(slice / (uint32_t)s.kv_heads), a = (int)(slice - (uint32_t)b * s.kv_heads);
     int ql, kl;
     lengths(s, b, ql, kl);
@@ -50,7 +53,8 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_mfma_kernel(
     const int J = key_tile * kKeys, jw = J + 32 * wave, j = jw + l32;
     const Span span = near_span(s, J, kKeys, p0, ql, kl);
     const int tiles = span.e > span.a ? (span.e - span.a + RT - 1) / RT : 0;
-    const int all = tiles * s.group;
+    int it0 = 0, all = tiles * s.group;                 // this workgroup's tiles, head by head
+    if (SHARED) near.share(split, all, it0, all);
 
     auto issue = [&](int head, int t0, int buf) {
         const int n = min(RT, span.e - t0);
@@ -64,8 +68,9 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_mfma_kernel(
         if (wave == 0) load_lds_4(buffer_desc(lse2 + at, (uint32_t)n * 4u), off, 0, lds_address(rows_s[buf][0]));
         if (wave == 3) load_lds_4(buffer_desc(delta + at, (uint32_t)n * 4u), off, 0, lds_address(rows_s[buf][1]));
     };
-    int head = a * s.group, t0 = span.a;
-    if (all > 0) issue(head, t0, 0);
+    const int head0 = SHARED && it0 < all ? it0 / tiles : 0;
+    int head = a * s.group + head0, t0 = span.a + (it0 - head0 * tiles) * RT;
+    if (it0 < all) issue(head, t0, 0);
 
     // K as operand; -V likewise, or to LDS.  The sign makes delta - dP of a product that starts
     // from delta, so that -dS costs one product; it goes into the scale of dK.
@@ -263,13 +268,13 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_mfma_kernel(
         }
     };
 
-    for (int it = 0; it < all; ++it) {
+    for (int it = it0; it < all; ++it) {
         // tile `it` has landed and everyone is done with the other buffer
         wait_gathers();
         __syncthreads();
         int next_head = head, next_t0 = t0 + RT;
         if (next_t0 >= span.e) { ++next_head; next_t0 = span.a; }
-        if (it + 1 < all) issue(next_head, next_t0, (it + 1) & 1);
+        if (it + 1 < all) issue(next_head, next_t0, (it - it0 + 1) & 1);
         const int n = min(RT, span.e - t0), pa = p0 + t0;
         const bool any = jw < kl && jw <= pa + n - 1 + s.right && (jw + 31 >= pa - s.left || jw < s.sinks);
         const bool full = n == RT && jw + 31 < kl && jw + 31 <= pa + s.right &&
@@ -286,6 +291,14 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_mfma_kernel(
         for (int dt = 0; dt < DT; ++dt) tr_at[dt] += to_other;
         to_other = 0u - to_other;
         val_at ^= 512u;
+    }
+    if constexpr (SHARED) {
+        if (jw / 32 < near.groups) {
+            float* p = near_part<D>(near, slice, jw / 32, split, l32);
+            store_lane_row<float, D>(p, ak, -1.0f, half);
+            store_lane_row<float, D>(p + 32 * D, av, 1.0f, half);
+        }
+        return;
     }
     if (jw / 32 < far.groups) add_far<D>(far, slice, jw / 32, l32, half, ak, av, -1.0f);
     if (j < s.k_tokens) {
@@ -523,15 +536,16 @@ hipError_t launch_window_dq_mfma(int D, const win::Shape& s, const void* q, cons
 hipError_t launch_window_dkdv_mfma(int D, const win::Shape& s, const void* q, const void* k,
                                    const void* v, const void* dout, const float* delta,
                                    const float* lse2, void* dk, void* dv, const win::Far& far,
-                                   hipStream_t stream)
+                                   const win::Near& near, hipStream_t stream)
 {
     using namespace win;
     const uint32_t key_tiles = ((uint32_t)s.k_tokens + kKeys - 1) / kKeys;
     const uint32_t items = (uint32_t)(s.batch * s.kv_heads) * key_tiles;
-    auto kernel = D == 64 ? window_dkdv_mfma_kernel<64> : window_dkdv_mfma_kernel<128>;
-    kernel<<<items, 256, 0, stream>>>((const uint16_t*)q, (const uint16_t*)k, (const uint16_t*)v,
-                                      (const uint16_t*)dout, delta, lse2, (uint16_t*)dk, (uint16_t*)dv,
-                                      s, far, key_tiles, items);
+    auto kernel = near.splits > 1 ? (D == 64 ? window_dkdv_mfma_kernel<64, true> : window_dkdv_mfma_kernel<128, true>)
+                                  : (D == 64 ? window_dkdv_mfma_kernel<64, false> : window_dkdv_mfma_kernel<128, false>);
+    kernel<<<items * (uint32_t)near.splits, 256, 0, stream>>>(
+        (const uint16_t*)q, (const uint16_t*)k, (const uint16_t*)v, (const uint16_t*)dout, delta, lse2,
+        (uint16_t*)dk, (uint16_t*)dv, s, far, near, key_tiles, items);
     return hipGetLastError();
 }
 

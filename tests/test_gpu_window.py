@@ -270,3 +270,16 @@ def test_many_key_tiles(dtype, D, h, kv, left, right, sinks):
     run(dtype, B, h, kv, n, n, D, left, right, sinks, train=True, seed=D + left,
         q_lens=[n - (i * 37) % n if i % 3 else n for i in range(B)],
         k_lens=[n - (i * 23) % 350 if i % 2 else n for i in range(B)])
+
+
+@DTYPES
+@pytest.mark.parametrize("D", [32, 64, 128])
+@pytest.mark.parametrize("B,h,n,left,right,sinks", [
+    (1, 5, 300, -1, 0, 0), (1, 5, 300, 250, 0, 40),         # 32 keys a workgroup
+    (40, 4, 389, 150, 0, 3), (40, 4, 389, -1, -1, 0),       # 160 workgroups of 128
+    (60, 4, 520, 500, 500, 2)])                             # 300
+def test_shared_walks(dtype, D, B, h, n, left, right, sinks):
+    """Backward launches in which several workgroups have the same keys."""
+    run(dtype, B, h, 1, n, n, D, left, right, sinks, train=True, seed=D + n,
+        q_lens=[n - (i * 41) % n if i % 3 == 1 else n for i in range(B)],
+        k_lens=[n - (i * 29) % 300 if i % 2 else n for i in range(B)])
