@@ -211,16 +211,20 @@ bool is_step(bool is_bf16, int D, const Shape& s)
                             (int64_t)s.batch * s.kv_heads * ((s.rows + 127) / 128) < 256);
 }
 
-// Into how many parts the keys of a launch of few workgroups are split: for up to three workgroups of
-// 32 rows to a CU, two of 128 rows, 128 keys at least to each.
+// Into how many parts the keys of a launch of few workgroups are split: up to 512 workgroups, 256 keys at
+// least to each.  Joining costs a launch, so that few keys stay whole, and two or three parts come from 1,280
+// keys on.  us, whole | split: bf16, head dim 64, 300 keys 11 | 17, 600 16 | 12, 2,255 45 | 17, 210
+// workgroups of 304 10 | 20, of 819 16 | 24, 160 of 1,700, head dim 128, 43 | 35; fp32, head dim 64, 215
+// keys 16 | 23, 411 17 | 13.  Parts of 128 keys: 9,830 keys, one token, 18 us instead of 14.
 int splits_of(bool is_bf16, int D, const Shape& s)
 {
     const bool step = is_step(is_bf16, D, s);
     if (step && is_wide_step(is_bf16, D, s)) return 1;
     const int tile = !step ? 128 : s.rows <= 16 ? s.rows : 32;
     const int64_t items = (int64_t)s.batch * s.kv_heads * ((s.rows + tile - 1) / tile);
-    const int64_t pieces = (most_keys(s, tile) + 127) / 128;
-    const int64_t n = min(min((step ? 768 : 512) / items, pieces), (int64_t)64);
+    const int64_t keys = most_keys(s, tile);
+    if (keys < (!is_bf16 ? 384 : step ? 640 : 512) || (items > 128 && keys < 1280)) return 1;
+    const int64_t n = min(min(512 / items, keys / 256), (int64_t)64);
     return n < 2 ? 1 : (int)n;
 }
 
