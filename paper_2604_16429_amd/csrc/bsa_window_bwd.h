@@ -112,8 +112,8 @@ __device__ __forceinline__ void add_far(const Far& far, int64_t slice, int group
 
 bool window_bwd_mfma_supported(bool is_bf16, int D, const win::Shape& s);
 hipError_t launch_window_dq_mfma(int D, const win::Shape& s, const void* q, const void* k,
-                                 const void* v, const void* out, const float* lse, const void* dout,
-                                 float* delta, float* lse2, void* dq, hipStream_t stream);
+                                 const void* v, const float* lse, const void* dout, float* delta,
+                                 float* lse2, void* dq, hipStream_t stream);
 hipError_t launch_window_dkdv_mfma(int D, const win::Shape& s, const void* q, const void* k,
                                    const void* v, const void* dout, const float* delta,
                                    const float* lse2, void* dk, void* dv, const win::Far& far,

@@ -3,6 +3,12 @@
 // With P = exp(scale q.k - lse) recomputed and delta = dO . O for each query,
 //   dV_j = sum_i P_ij dO_i    dS_ij = P_ij (dO_i . v_j - delta_i)
 //   dQ_i = scale sum_j dS_ij k_j    dK_j = scale sum_i dS_ij q_i
+// In bf16 delta is not taken from the rounded output, whose error (and that of the weights it was summed with)
+// adds 0.9 to 1.5e-3 to the 2.3e-3 that rounding dS and the results leaves in dQ and dK, more the fewer keys
+// share the weight.  With delta' of that output and e = sum_j P_ij (dP_ij - delta'_i), which is delta -
+// delta', dQ_i is scale (sum_j dS'_ij k_j - e_i sum_j P_ij k_j); the matrix-core kernels, which have no
+// registers for the second sum at head dim 128, take delta = sum_j P_ij dP_ij from a launch before.
+//
 // Launches: dQ, which walks the keys of 128 rows as the forward does and leaves delta and lse in base
 // 2 of each row; dK and dV, where a wavefront owns 32 keys and walks the queries that see them, in tiles
 // of consecutive tokens of one head, the heads of the group one after the other.  Every sum has
@@ -62,10 +68,12 @@ __global__ __launch_bounds__(256, D == 32 ? 3 : 1) void window_dq_kernel(
 {
     constexpr int KT = sizeof(T) == 2 && !NARROW ? 64 : 32, ROWS = NARROW ? 32 : 128;
     constexpr int KS = D / 16, DT = D / 32, SETS = NARROW ? 4 : 1;
+    constexpr bool EXACT = sizeof(T) == 2;              // correct delta by the sum of dS
     using Tl = Tile<T, D, KT, NARROW ? 64 : 256>;
     using M = Mma<T>;
     using Frag = typename M::Frag;
     __shared__ __attribute__((aligned(1024))) unsigned char tiles_s[SETS][2][Tl::BYTES];
+    __shared__ float e_s[4][32];
     static_assert(!NARROW || add_waves_bytes<4, DT>() <= (int)sizeof(tiles_s), "the sums fit the tiles");
 
     const int tid = threadIdx.x, lane = tid & 63;
@@ -119,7 +127,7 @@ __global__ __launch_bounds__(256, D == 32 ? 3 : 1) void window_dq_kernel(
             const int64_t at = ((int64_t)b * s.heads + head) * s.q_tokens + tok;
             const float l = lse[at], l2 = l == -INFINITY ? kNoWeight : l * kLog2e;
             if (half == 0 && (!NARROW || wave == 0)) {
-                delta[at] = d;
+                if (!EXACT) delta[at] = d;
                 lse2[at] = l2;
             }
             neg_l2 = -l2;
@@ -127,9 +135,14 @@ __global__ __launch_bounds__(256, D == 32 ? 3 : 1) void window_dq_kernel(
         }
     }
     const float c2 = s.scale * kLog2e;
-    f32x16 acc[DT];
+    f32x16 acc[DT], pk[EXACT ? DT : 1];
+    float e_run = 0.0f;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) acc[dt] = splat(0.0f);
+    if constexpr (EXACT) {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) pk[dt] = splat(0.0f);
+    }
 
     Tl kt, vt;
     auto fetch = [&](int slot0) {
@@ -165,27 +178,48 @@ __global__ __launch_bounds__(256, D == 32 ? 3 : 1) void window_dq_kernel(
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                float ds = __builtin_amdgcn_exp2f(fmaf(st[r], c2, neg_l2)) * dp[r];
+                float w = __builtin_amdgcn_exp2f(fmaf(st[r], c2, neg_l2));
                 if (!full) {
                     const int slot = s0 + 8 * (r >> 2) + 4 * half + (r & 3);
-                    ds = see.sees(slot) ? ds : 0.0f;
+                    w = see.sees(slot) ? w : 0.0f;
                 }
-                st[r] = ds;
+                st[r] = w;
+                dp[r] *= w;
+                if (EXACT) e_run += dp[r];
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const Frag ds = M::pack(st, h);
+                const Frag ds = M::pack(dp, h);
+                Frag w;
+                if constexpr (EXACT) w = M::pack(st, h);
 #pragma unroll
-                for (int dt = 0; dt < DT; ++dt)
-                    acc[dt] = M::mul(Tl::trans_frag(k_lds, 32 * hh + 16 * h, dt, lane), ds, acc[dt]);
+                for (int dt = 0; dt < DT; ++dt) {
+                    const Frag x = Tl::trans_frag(k_lds, 32 * hh + 16 * h, dt, lane);
+                    acc[dt] = M::mul(x, ds, acc[dt]);
+                    if constexpr (EXACT) pk[dt] = M::mul(x, w, pk[dt]);
+                }
             }
         }
     }
+    float e = e_run + swap32(e_run);
     if constexpr (NARROW) {
         add_waves<4>(&tiles_s[0][0][0], wave, lane, acc);
+        if constexpr (EXACT) {
+            add_waves<4>(&tiles_s[0][0][0], wave, lane, pk);
+            if (half == 0) e_s[wave][l32] = e;
+            __syncthreads();
+            e = (e_s[0][l32] + e_s[1][l32]) + (e_s[2][l32] + e_s[3][l32]);
+        }
         if (wave != 0) return;
     }
     if (!exists) return;
+    if constexpr (EXACT) {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[dt][r] = fmaf(-e, pk[dt][r], acc[dt][r]);
+        if (valid && half == 0) delta[((int64_t)b * s.heads + head) * s.q_tokens + tok] = e - neg_delta;
+    }
     store_lane_row<T, D>(dq + (int64_t)b * s.dq.batch + (int64_t)head * s.dq.head +
                              (int64_t)tok * s.dq.token,
                          acc, s.scale, half);
@@ -581,7 +615,7 @@ hipError_t launch_bwd(const Shape& s, const void* q_, const void* k_, const void
     // and 16.6 | 17.4, 128 13.9 | 13.2 and 31 | 18).
     const bool few_rows = slices * (((int64_t)s.rows + 127) / 128) < (mfma ? 96 : 256);
     if (!few_rows && mfma) {
-        e = launch_window_dq_mfma(D, s, q, k, v, out, lse, dout, delta, lse2, dq, stream);
+        e = launch_window_dq_mfma(D, s, q, k, v, lse, dout, delta, lse2, dq, stream);
     } else {
         const uint32_t per = few_rows ? 32 : 128, row_tiles = ((uint32_t)s.rows + per - 1) / per;
         const uint32_t q_items = row_tiles * (uint32_t)slices;

@@ -309,14 +309,112 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_mfma_kernel(
     }
 }
 
-// dQ of 128 rows: four wavefronts of 32 share tiles of 64 keys, double buffered.  It also leaves
-// delta = dO . O and lse in base 2 for the kernels of dK and dV.
+// delta_i = sum_j P_ij dP_ij of 128 rows, and lse in base 2, for the kernels of dQ, dK and dV: the tiles and
+// the two products of the dQ kernel below.  1.5 degrees, head dim 128, window 1,024: 1,260 us.
+template <int D>
+__global__ __launch_bounds__(256, 2) void window_delta_mfma_kernel(
+    const uint16_t* __restrict__ q, const uint16_t* __restrict__ k, const uint16_t* __restrict__ v,
+    const float* __restrict__ lse, const uint16_t* __restrict__ dout, float* __restrict__ delta,
+    float* __restrict__ lse2, const Shape s, uint32_t row_tiles, uint32_t items)
+{
+    using R = Rows<D>;
+    constexpr int KS = D / 16, TILE = R::bytes(64);
+    using G = KeyGather<D, 64, 4>;
+    // [buffer][K, V]
+    __shared__ __attribute__((aligned(1024))) unsigned char tiles_s[2][2][TILE];
+
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int l32 = lane & 31, half = lane >> 5;
+
+    uint32_t slice;
+    int tile_at;
+    map_item(s, blockIdx.x, items, row_tiles, true, slice, tile_at);
+    const int row0 = tile_at * 128;
+    const int b = (int)(slice / (uint32_t)s.kv_heads), a = (int)(slice - (uint32_t)b * s.kv_heads);
+    int ql, kl;
+    lengths(s, b, ql, kl);
+    const int p0 = kl - ql;
+    const int t_first = row0 / s.group, t_last = min((row0 + 127) / s.group, ql - 1);
+    KeyList keys = {};
+    if (t_first <= t_last) keys = key_list(s, p0 + t_first, p0 + t_last, kl);
+    const int tiles = (keys.count + 63) / 64;
+
+    const uint32_t k_stride = (uint32_t)s.k.token * 2u, v_stride = (uint32_t)s.v.token * 2u;
+    const i32x4 k_rsrc = buffer_desc(k + (int64_t)b * s.k.batch + (int64_t)a * s.k.head,
+                                     (uint32_t)(s.k_tokens - 1) * k_stride + R::ROW_BYTES);
+    const i32x4 v_rsrc = buffer_desc(v + (int64_t)b * s.v.batch + (int64_t)a * s.v.head,
+                                     (uint32_t)(s.k_tokens - 1) * v_stride + R::ROW_BYTES);
+    auto issue = [&](int c) {
+        G::gather(k_rsrc, k_stride, keys, 64 * c, lds_address(tiles_s[c & 1][0]), wave, lane);
+        G::gather(v_rsrc, v_stride, keys, 64 * c, lds_address(tiles_s[c & 1][1]), wave, lane);
+    };
+    if (tiles > 0) issue(0);
+
+    const int row = row0 + 32 * wave + l32;
+    const int tok = row / s.group, head = a * s.group + (row - tok * s.group);
+    const bool valid = row < s.rows && tok < ql;
+    const Sight see = sight(s, keys, p0 + tok, kl, valid);
+    const RowsSight rows = rows_sight(s, keys, row0 + 32 * wave, 32, p0, ql, kl);
+    bf16x8 qf[KS], gf[KS];
+    const uint16_t* qp = q + (int64_t)b * s.q.batch + (int64_t)head * s.q.head + (int64_t)tok * s.q.token + 8 * half;
+    const uint16_t* gp = dout + (int64_t)b * s.dout.batch + (int64_t)head * s.dout.head +
+                         (int64_t)tok * s.dout.token + 8 * half;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+        qf[ks] = valid ? *(const bf16x8*)(qp + 16 * ks) : bf16x8{};
+        gf[ks] = valid ? *(const bf16x8*)(gp + 16 * ks) : bf16x8{};
+    }
+    const int64_t at = ((int64_t)b * s.heads + head) * s.q_tokens + tok;
+    const float l = valid ? lse[at] : -INFINITY, l2 = l == -INFINITY ? kNoWeight : l * kLog2e;
+    const float c2 = s.scale * kLog2e;
+    float d0 = 0.0f, d1 = 0.0f;
+
+    uint32_t row_at[4], to_other = 2u * TILE;
+    R::row_addresses(lds_address(tiles_s), lane, row_at);
+    for (int c = 0; c < tiles; ++c) {
+        // tile c has landed and everyone is done with the other buffer
+        wait_gathers();
+        __syncthreads();
+        if (c + 1 < tiles) issue(c + 1);
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) {
+            const int s0 = 64 * c + 32 * hh;
+            if (!rows.any(s0, 32)) continue;
+            f32x16 st = rows.all(s0, 32) ? splat(0.0f) : start_of(see, s0, half, rows.sinks);
+            f32x16 dp = splat(0.0f);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+                st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                    lds_read<bf16x8>(row_at[R::index(ks)], R::bytes(32 * hh) + R::offset(ks)), qf[ks], st, 0, 0, 0);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                    lds_read<bf16x8>(row_at[R::index(ks)], TILE + R::bytes(32 * hh) + R::offset(ks)), gf[ks], dp, 0, 0, 0);
+#pragma unroll
+            for (int r = 0; r < 16; r += 2) {
+                d0 = fmaf(__builtin_amdgcn_exp2f(fmaf(st[r], c2, -l2)), dp[r], d0);
+                d1 = fmaf(__builtin_amdgcn_exp2f(fmaf(st[r + 1], c2, -l2)), dp[r + 1], d1);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) row_at[i] += to_other;
+        to_other = 0u - to_other;
+    }
+    float d = d0 + d1;
+    d += swap32(d);
+    if (valid && half == 0) {
+        delta[at] = d;
+        lse2[at] = l2;
+    }
+}
+
+// dQ of 128 rows: four wavefronts of 32 share tiles of 64 keys, double buffered.
 template <int D>
 __global__ __launch_bounds__(256, 2) void window_dq_mfma_kernel(
     const uint16_t* __restrict__ q, const uint16_t* __restrict__ k, const uint16_t* __restrict__ v,
-    const uint16_t* __restrict__ out, const float* __restrict__ lse,
-    const uint16_t* __restrict__ dout, float* __restrict__ delta, float* __restrict__ lse2,
-    uint16_t* __restrict__ dq, const Shape s, uint32_t row_tiles, uint32_t items)
+    const uint16_t* __restrict__ dout, const float* __restrict__ delta,
+    const float* __restrict__ lse2, uint16_t* __restrict__ dq, const Shape s, uint32_t row_tiles, uint32_t items)
 {
     using R = Rows<D>;
     constexpr int KS = D / 16, DT = D / 32, TILE = R::bytes(64);
@@ -363,27 +461,15 @@ __global__ __launch_bounds__(256, 2) void window_dq_mfma_kernel(
         const uint16_t* qp = q + (int64_t)b * s.q.batch + (int64_t)head * s.q.head + (int64_t)tok * s.q.token + 8 * half;
         const uint16_t* gp = dout + (int64_t)b * s.dout.batch + (int64_t)head * s.dout.head +
                              (int64_t)tok * s.dout.token + 8 * half;
-        const uint16_t* op = out + (int64_t)b * s.out.batch + (int64_t)head * s.out.head +
-                             (int64_t)tok * s.out.token + 8 * half;
-        float d = 0.0f;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             qf[ks] = valid ? *(const bf16x8*)(qp + 16 * ks) : bf16x8{};
             gf[ks] = valid ? *(const bf16x8*)(gp + 16 * ks) : bf16x8{};
-            const bf16x8 o = valid ? *(const bf16x8*)(op + 16 * ks) : bf16x8{};
-#pragma unroll
-            for (int i = 0; i < 8; ++i) d = fmaf((float)gf[ks][i], (float)o[i], d);
         }
-        d += swap32(d);
         if (valid) {
             const int64_t at = ((int64_t)b * s.heads + head) * s.q_tokens + tok;
-            const float l = lse[at], l2 = l == -INFINITY ? kNoWeight : l * kLog2e;
-            if (half == 0) {
-                delta[at] = d;
-                lse2[at] = l2;
-            }
-            neg_l2 = -l2;
-            neg_delta = -d;
+            neg_l2 = -lse2[at];
+            neg_delta = -delta[at];
         }
     }
     const float c2 = s.scale * kLog2e;
@@ -520,16 +606,19 @@ bool window_bwd_mfma_supported(bool is_bf16, int D, const win::Shape& s)
 }
 
 hipError_t launch_window_dq_mfma(int D, const win::Shape& s, const void* q, const void* k,
-                                 const void* v, const void* out, const float* lse, const void* dout,
-                                 float* delta, float* lse2, void* dq, hipStream_t stream)
+                                 const void* v, const float* lse, const void* dout, float* delta,
+                                 float* lse2, void* dq, hipStream_t stream)
 {
     using namespace win;
     const uint32_t row_tiles = ((uint32_t)s.rows + 127) / 128;
     const uint32_t items = row_tiles * (uint32_t)(s.batch * s.kv_heads);
+    auto delta_kernel = D == 64 ? window_delta_mfma_kernel<64> : window_delta_mfma_kernel<128>;
+    delta_kernel<<<items, 256, 0, stream>>>((const uint16_t*)q, (const uint16_t*)k, (const uint16_t*)v, lse,
+                                            (const uint16_t*)dout, delta, lse2, s, row_tiles, items);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     auto kernel = D == 64 ? window_dq_mfma_kernel<64> : window_dq_mfma_kernel<128>;
     kernel<<<items, 256, 0, stream>>>((const uint16_t*)q, (const uint16_t*)k, (const uint16_t*)v,
-                                      (const uint16_t*)out, lse, (const uint16_t*)dout, delta, lse2,
-                                      (uint16_t*)dq, s, row_tiles, items);
+                                      (const uint16_t*)dout, delta, lse2, (uint16_t*)dq, s, row_tiles, items);
     return hipGetLastError();
 }
 

@@ -283,3 +283,26 @@ def test_shared_walks(dtype, D, B, h, n, left, right, sinks):
     run(dtype, B, h, 1, n, n, D, left, right, sinks, train=True, seed=D + n,
         q_lens=[n - (i * 41) % n if i % 3 == 1 else n for i in range(B)],
         k_lens=[n - (i * 29) % 300 if i % 2 else n for i in range(B)])
+
+
+@pytest.mark.parametrize("D", [32, 64, 128])
+@pytest.mark.parametrize("B,n", [(1, 400), (24, 600)])
+def test_roundings_of_bf16_gradients(D, B, n):
+    """dQ and dK carry two independent roundings, that of dS and that of the result: sqrt(2) times the
+    latter's error in the 2-norm, and no more than 1.5 times with what else there is.  Short windows,
+    where delta out of the rounded output would add as much again."""
+    h, kv, left, right, sinks = 4, 2, 15, 0, 2
+    got = run(BF16, B, h, kv, n, n, D, left, right, sinks, train=True, seed=D + n, junk=False)
+    gen = torch.Generator().manual_seed(1000 + D + n)
+    q, k, v = (torch.randn(B, x, n, D, generator=gen).to(BF16).double() for x in (h, kv, kv))
+    do = torch.randn(B, h, n, D, generator=gen).to(BF16).double()
+    see = visible(n, n, n, n, left, right, sinks)
+    want = {"dq": torch.zeros_like(q), "dk": torch.zeros_like(k)}
+    for b in range(B):
+        for i in range(h):
+            r = attention(q[b, i], k[b, i // 2], v[b, i // 2], see, 1.0 / math.sqrt(D), do[b, i])
+            want["dq"][b, i] = r["dq"]
+            want["dk"][b, i // 2] += r["dk"]
+    for name, w in want.items():
+        rounding = float((w.to(BF16).double() - w).norm())
+        assert float((got[name] - w).norm()) <= 1.5 * rounding, name
