@@ -310,16 +310,17 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_mfma_kernel(
 }
 
 // delta_i = sum_j P_ij dP_ij of 128 rows, and lse in base 2, for the kernels of dQ, dK and dV: the tiles and
-// the two products of the dQ kernel below.  1.5 degrees, head dim 128, window 1,024: 1,260 us.
+// the two products of the dQ kernel below.  Little but two operands in registers: four wavefronts per SIMD, at head dim
+// 128 with tiles of 32 keys.  1.5 degrees, head dim 128, window 1,024: 1,140 us, two wavefronts and tiles of 64 1,180.
 template <int D>
-__global__ __launch_bounds__(256, 2) void window_delta_mfma_kernel(
+__global__ __launch_bounds__(256, 4) void window_delta_mfma_kernel(
     const uint16_t* __restrict__ q, const uint16_t* __restrict__ k, const uint16_t* __restrict__ v,
     const float* __restrict__ lse, const uint16_t* __restrict__ dout, float* __restrict__ delta,
     float* __restrict__ lse2, const Shape s, uint32_t row_tiles, uint32_t items)
 {
     using R = Rows<D>;
-    constexpr int KS = D / 16, TILE = R::bytes(64);
-    using G = KeyGather<D, 64, 4>;
+    constexpr int KS = D / 16, KT = D == 64 ? 64 : 32, TILE = R::bytes(KT);
+    using G = KeyGather<D, KT, 4>;
     // [buffer][K, V]
     __shared__ __attribute__((aligned(1024))) unsigned char tiles_s[2][2][TILE];
 
@@ -338,7 +339,7 @@ __global__ __launch_bounds__(256, 2) void window_delta_mfma_kernel(
     const int t_first = row0 / s.group, t_last = min((row0 + 127) / s.group, ql - 1);
     KeyList keys = {};
     if (t_first <= t_last) keys = key_list(s, p0 + t_first, p0 + t_last, kl);
-    const int tiles = (keys.count + 63) / 64;
+    const int tiles = (keys.count + KT - 1) / KT;
 
     const uint32_t k_stride = (uint32_t)s.k.token * 2u, v_stride = (uint32_t)s.v.token * 2u;
     const i32x4 k_rsrc = buffer_desc(k + (int64_t)b * s.k.batch + (int64_t)a * s.k.head,
@@ -346,8 +347,8 @@ __global__ __launch_bounds__(256, 2) void window_delta_mfma_kernel(
     const i32x4 v_rsrc = buffer_desc(v + (int64_t)b * s.v.batch + (int64_t)a * s.v.head,
                                      (uint32_t)(s.k_tokens - 1) * v_stride + R::ROW_BYTES);
     auto issue = [&](int c) {
-        G::gather(k_rsrc, k_stride, keys, 64 * c, lds_address(tiles_s[c & 1][0]), wave, lane);
-        G::gather(v_rsrc, v_stride, keys, 64 * c, lds_address(tiles_s[c & 1][1]), wave, lane);
+        G::gather(k_rsrc, k_stride, keys, KT * c, lds_address(tiles_s[c & 1][0]), wave, lane);
+        G::gather(v_rsrc, v_stride, keys, KT * c, lds_address(tiles_s[c & 1][1]), wave, lane);
     };
     if (tiles > 0) issue(0);
 
@@ -378,8 +379,8 @@ __global__ __launch_bounds__(256, 2) void window_delta_mfma_kernel(
         __syncthreads();
         if (c + 1 < tiles) issue(c + 1);
 #pragma unroll
-        for (int hh = 0; hh < 2; ++hh) {
-            const int s0 = 64 * c + 32 * hh;
+        for (int hh = 0; hh < KT / 32; ++hh) {
+            const int s0 = KT * c + 32 * hh;
             if (!rows.any(s0, 32)) continue;
             f32x16 st = rows.all(s0, 32) ? splat(0.0f) : start_of(see, s0, half, rows.sinks);
             f32x16 dp = splat(0.0f);
