@@ -610,10 +610,10 @@ hipError_t launch_bwd(const Shape& s, const void* q_, const void* k_, const void
     near.sums = (float*)((char*)far.sums + plan.far_bytes);
 
     hipError_t e;
-    // launches of few workgroups of 128 rows: 32 rows to each.  The matrix-core kernel is the faster one
-    // from about 96 on (us, narrow | not, head dim 64 and 128, window 300: 64 workgroups 11.3 | 12.4
-    // and 16.6 | 17.4, 128 13.9 | 13.2 and 31 | 18).
-    const bool few_rows = slices * (((int64_t)s.rows + 127) / 128) < (mfma ? 96 : 256);
+    // Launches of few workgroups of 128 rows: 32 rows to each.  The matrix-core kernels, which take a launch
+    // more, are the faster ones from about 256 on, at head dim 128 from 192 (us, backward, narrow | not: head dim
+    // 64, 111 workgroups 51 | 79, 235 83 | 111, 264 36 | 28; 128, 150 130 | 167, 208 138 | 106).
+    const bool few_rows = slices * (((int64_t)s.rows + 127) / 128) < (mfma && D == 128 ? 192 : 256);
     if (!few_rows && mfma) {
         e = launch_window_dq_mfma(D, s, q, k, v, lse, dout, delta, lse2, dq, stream);
     } else {
