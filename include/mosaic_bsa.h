@@ -358,7 +358,8 @@ typedef struct {
     int32_t cache_tokens;      /* rows of k_out and v_out when `rows` is given */
     int32_t position_batch;    /* int32 values from one batch entry's positions to the
                                   next's; 0: all share [N, axes] */
-    float norm_eps;            /* norm forms: added to the mean square */
+    float norm_eps;            /* norm forms: added to the mean square; >= 0 (0: a row of
+                                  zeros has no norm and gives NaN) */
     mosaic_bsa_strides q, k, v, q_out, k_out, v_out;
 } mosaic_bsa_heads_params;
 

@@ -281,7 +281,10 @@ __global__ __launch_bounds__(256, 3) void heads_kernel(const Args a, const int D
 #pragma unroll
                             for (int i = 0; i < E; ++i) sq = fmaf(e[u][i], e[u][i], sq);
                             sq = row_sum(sq, P);
-                            const float r = 1.0f / sqrtf(sq * (1.0f / (float)D) + a.eps);
+                            float r = 1.0f / sqrtf(sq * (1.0f / (float)D) + a.eps);
+                            // (lanes without a row hold zeros, and without an epsilon r is infinite
+                            // there: the weights' sums take all lanes)
+                            if (MODE == kNormGrad && !here) r = 0.0f;
                             if constexpr (MODE == kNorm) {
 #pragma unroll
                                 for (int i = 0; i < E; ++i) e[u][i] *= r * w[i];
