@@ -453,7 +453,7 @@ size_t mosaic_bsa_window_workspace_bytes(const mosaic_bsa_window_params *params,
 /*
  *   q, k, v          in   device; bases and strides multiples of 16 bytes
  *   q_lens, k_lens   in   device, int32 [batch], or NULL: q_tokens, k_tokens.  Values are held
- *                         to [0, q_tokens] and [0, k_tokens] (k_lens: >= 0 with a ring)
+ *                         to [0, q_tokens] and [0, k_tokens] (k_lens with a ring: [0, 3 * 2^29])
  *   out              out  device, must not alias an input
  *   lse              out  device, fp32 [batch, heads, q_tokens], natural log; may be NULL
  *   workspace             mosaic_bsa_window_workspace_bytes(.., OP_FWD) bytes (may be 0)

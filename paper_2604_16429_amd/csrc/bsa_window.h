@@ -21,11 +21,14 @@ constexpr float kLn2 = 0.6931471805599453f;
 // against it
 constexpr float kNoRef = -3.0e38f;
 constexpr int32_t kUnbounded = 1 << 30;
+// Longest sequence that a ring cache may have held: positions with a right bound (at most q_tokens,
+// fewer than 2^28) added stay below 2^31.
+constexpr int32_t kMostRingLength = 3 << 29;
 
 struct Shape {
     int32_t batch, heads, kv_heads, group;
     int32_t q_tokens, k_tokens, rows;      // rows = q_tokens * group
-    int32_t left, right, sinks, ring;      // left, right: kUnbounded = no bound
+    int32_t left, right, sinks, ring;      // left: kUnbounded = no bound; right: at most q_tokens
     float scale;
     const int32_t *q_lens, *k_lens;        // or null
     mosaic_bsa_strides q, k, v, out, dout, dq, dk, dv;    // elements
@@ -41,7 +44,7 @@ __device__ __forceinline__ int query_length(const Shape& s, int b)
 __device__ __forceinline__ void lengths(const Shape& s, int b, int& ql, int& kl)
 {
     ql = __builtin_amdgcn_readfirstlane(query_length(s, b));
-    kl = s.k_lens ? min(max(s.k_lens[b], 0), s.ring ? kUnbounded : s.k_tokens) : s.k_tokens;
+    kl = s.k_lens ? min(max(s.k_lens[b], 0), s.ring ? kMostRingLength : s.k_tokens) : s.k_tokens;
     kl = __builtin_amdgcn_readfirstlane(kl);
 }
 

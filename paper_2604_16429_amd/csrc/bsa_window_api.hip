@@ -2,6 +2,8 @@
 // is in include/mosaic_bsa.h.
 #include <math.h>
 
+#include <algorithm>
+
 #include "bsa_window.h"
 
 namespace {
@@ -48,7 +50,8 @@ int check_params(const mosaic_bsa_window_params* p, Checked* c)
     s.k_tokens = p->k_tokens;
     s.rows = (int32_t)rows;
     s.left = bound(p->window_left);
-    s.right = bound(p->window_right);
+    // (the queries stand at the end: no key is further to the right of one than the last query)
+    s.right = std::min(bound(p->window_right), p->q_tokens);
     s.sinks = p->n_sink < p->k_tokens ? p->n_sink : p->k_tokens;
     s.ring = p->ring;
     s.scale = p->softmax_scale > 0.0f ? p->softmax_scale : 1.0f / sqrtf((float)p->head_dim);
