@@ -332,7 +332,7 @@ enum {
  * (2 i, 2 i + 1) (PAIRS):
  *   (a, b) -> magnitude * (a cos - b sin, b cos + a sin)
  * Frequencies are kept as turns per position in units of 2^-64, so that any 32-bit
- * position gives its angle to 2^-32 turns. */
+ * position gives its angle to 2^-31 turns (frequencies up to 1 radian per position). */
 typedef struct {
     int32_t rotary_dim, axes, layout;
     float magnitude;

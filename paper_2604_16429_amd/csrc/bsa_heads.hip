@@ -13,8 +13,8 @@
 // costly piece of arithmetic, are made once for all of its heads and stay in registers.
 // They are made in the kernel instead of read from a table: a frequency is held as turns
 // per position in units of 2^-64, and the low 64 bits of its product with a 32-bit position
-// are the turn's fraction, exactly; its upper 32 bits give the angle to 1.5e-9 radians for
-// any position, where an angle in fp32 is off by 0.03 at position 10^6.
+// are the turn's fraction; its upper 32 bits give the angle to 2^-31 turns, 3e-9 radians, for
+// any position (frequencies up to 1 radian), where an angle in fp32 is off by 0.03 at position 10^6.
 #include "bsa_heads.h"
 
 #include <math.h>
@@ -556,6 +556,8 @@ extern "C" int mosaic_bsa_rotation_init(int32_t rotary_dim, int32_t axes, int32_
         (layout != MOSAIC_BSA_ROTATE_HALVES && layout != MOSAIC_BSA_ROTATE_PAIRS))
         return MOSAIC_BSA_ERR_ROTATION;
     const int d = rotary_dim / axes;
+    // (64 bits of mantissa: a double's 53 would leave angles at position 2^31 off by 1e-7)
+    long double base = theta;
     if (beta_fast == 0.0 && beta_slow == 0.0) { beta_fast = 32.0; beta_slow = 1.0; }
     if (!inv_freq) {
         if (!(theta > 0.0 && theta < INFINITY) || scaling < MOSAIC_BSA_SCALE_NONE ||
@@ -568,7 +570,7 @@ extern "C" int mosaic_bsa_rotation_init(int32_t rotary_dim, int32_t axes, int32_
               beta_fast > beta_slow && beta_fast < INFINITY))
             return MOSAIC_BSA_ERR_ROTATION;
         // one pair has one frequency, which a change of the base leaves at 1
-        if (scaling == MOSAIC_BSA_SCALE_BASE && d > 2) theta *= pow(factor, d / (d - 2.0));
+        if (scaling == MOSAIC_BSA_SCALE_BASE && d > 2) base *= powl(factor, d / (d - 2.0L));
     }
     mosaic_bsa_rotation t = {};
     t.rotary_dim = rotary_dim;
@@ -576,26 +578,27 @@ extern "C" int mosaic_bsa_rotation_init(int32_t rotary_dim, int32_t axes, int32_
     t.layout = layout;
     t.magnitude = !inv_freq && scaling == MOSAIC_BSA_SCALE_RAMP ? (float)(0.1 * log(factor) + 1.0)
                                                                 : 1.0f;
-    const double two_pi = 6.283185307179586476925;
+    const long double two_pi = 6.283185307179586476925286766559L;
     for (int i = 0; i < d / 2; ++i) {
-        double w;
+        long double w;
         if (inv_freq) {
             w = inv_freq[i];
-            if (!(fabs(w) < INFINITY)) return MOSAIC_BSA_ERR_ROTATION;
+            if (!(fabs(inv_freq[i]) < INFINITY)) return MOSAIC_BSA_ERR_ROTATION;
         } else {
-            w = pow(theta, -2.0 * i / d);
+            w = powl(base, -2.0L * i / d);
             if (scaling == MOSAIC_BSA_SCALE_LINEAR) w /= factor;
             if (scaling == MOSAIC_BSA_SCALE_RAMP) {
-                double keep = (original_tokens * w / two_pi - beta_slow) / (beta_fast - beta_slow);
-                keep = keep < 0.0 ? 0.0 : keep > 1.0 ? 1.0 : keep;
-                w = keep * w + (1.0 - keep) * w / factor;
+                long double keep = (original_tokens * w / two_pi - beta_slow) /
+                                   ((long double)beta_fast - beta_slow);
+                keep = keep < 0.0L ? 0.0L : keep > 1.0L ? 1.0L : keep;
+                w = keep * w + (1.0L - keep) * w / factor;
             }
         }
         // turns per position modulo 1, in units of 2^-64 (positions are whole numbers)
-        double turn = w / two_pi;
-        turn -= floor(turn);
-        const double units = ldexp(turn, 64);
-        t.turns[i] = units >= 18446744073709551615.0 ? 0 : (uint64_t)units;
+        long double turn = w / two_pi;
+        turn -= floorl(turn);
+        const long double units = rintl(ldexpl(turn, 64));
+        t.turns[i] = units >= 18446744073709551616.0L ? 0 : (uint64_t)units;
     }
     *out = t;
     return MOSAIC_BSA_OK;

@@ -1,9 +1,11 @@
-"""Rotation and head norms on the GPU at their edges: no epsilon, gradients over their inputs."""
+"""Rotation and head norms on the GPU at their edges: no epsilon, far positions, gradients over
+their inputs."""
 import pytest
 import torch
 
 from tests.test_gpu_heads import (BF16, DTYPES, FP32, U32, check, frequencies, lib, nan_like, normed,
-                                  pair_size, tensor)
+                                  pair_size, rotation_tol, tensor)
+from tests.test_rotation_angles import TWO_PI, decimal_frequencies, fraction
 from tests.window_reference import HALF_STEP, rotate
 
 pytestmark = pytest.mark.gpu
@@ -47,3 +49,24 @@ def test_norm_gradients_without_an_epsilon(dtype, D, rd, N):
         # dw: at most a few dozen values to a lane in 32 bits, then 64
         total = (pair_size(g64) * n).sum((0, 1, 2))
         check(dw, rw, total * (2 * rel + 16 * U32) + rw.abs() * U32, "d" + name + "_weight")
+
+
+@pytest.mark.parametrize("transpose", [False, True])
+@pytest.mark.parametrize("first", [0, -2 ** 31, 2 ** 31 - 40, 2 ** 30 + 12345])
+def test_far_positions_against_exact_angles(first, transpose):
+    """Angles of the reference in decimal arithmetic: no allowance beside the kernel's own."""
+    M, binding = lib()
+    N, D = 40, 64
+    gen = torch.Generator().manual_seed(2)
+    q, q64 = tensor((1, 1, N, D), FP32, gen, "heads")
+    pos = torch.arange(N) + first
+    out = nan_like(q)
+    p = M.HeadsParams(1, N, 1, D, binding.F32)
+    (M.mosaic_bsa_rope_bwd if transpose else M.mosaic_bsa_rope_fwd)(
+        p, M.Rotation(D), pos.to(torch.int32).cuda(), q, None, out, None)
+    angle = torch.tensor([[float(fraction(int(x) * w / TWO_PI) * TWO_PI) for w in decimal_frequencies(D)]
+                          for x in pos], dtype=torch.float64)
+    c, s = torch.cos(angle), torch.sin(angle) * (-1.0 if transpose else 1.0)
+    a, b = q64[0, 0].chunk(2, -1)
+    ref = torch.cat([a * c - b * s, b * c + a * s], -1).view(1, 1, N, D)
+    check(out, ref, rotation_tol(ref, pair_size(q64), FP32), "q")
