@@ -122,47 +122,62 @@ class Rotation:
 
 
 class _StridedParams:
-    """Parameters whose C struct also carries the tensors' strides.  The struct is made when a
-    call first needs it and after a parameter was set; a tensor is looked at closely where its
-    type, shape or strides, or what the call wants there, differ from the call before.  One thread
-    at a time uses an object."""
+    """Parameters whose C struct also carries the tensors' strides.  A call has a struct of its own for
+    the types, shapes and strides of its tensors, which is kept for the entry point's next call if that
+    has the same and not written to again: threads can call with one object at the same time (setting
+    a field of it meanwhile is another matter).  A copy keeps structs of its own."""
 
     _C = None
     _SCALARS = ()
 
     def __setattr__(self, name, value):
         self.__dict__[name] = value
-        self.__dict__["_struct"] = None
+        self.__dict__.update(_struct=None, _ref=None, _kept={})
 
-    def _c(self):
-        c = self._struct
-        if c is None:
-            c = self._C()
-            for name in self._SCALARS:
-                setattr(c, name, getattr(self, name))
-            self.__dict__.update(_struct=c, _ref=ctypes.byref(c), _seen={})
+    def __copy__(self):
+        other = object.__new__(type(self))
+        other.__dict__.update(self.__dict__, _struct=None, _ref=None, _kept={})
+        return other
+
+    def _new_struct(self):
+        c = self._C()
+        for name in self._SCALARS:
+            setattr(c, name, getattr(self, name))
         return c
 
-    def _tensors(self, *args):
-        """Device pointers of [batch, heads, tokens, head_dim] tensors, given as (field of the
-        struct, tensor, heads, tokens) one after the other.  The strides go into the fields;
-        integers and None are taken as they are (contiguous)."""
-        seen, pointers = self._seen, []
-        for field, t, heads, tokens in args:
-            if t is None or isinstance(t, int):
-                if seen.get(field) is not None:
-                    setattr(self._struct, field, _CStrides())
-                    seen[field] = None
-                pointers.append(t)
-                continue
-            now = (t.shape, t.stride(), t.dtype, t.is_cuda, heads, tokens)
-            if seen.get(field) != now:
-                self._look(field, t, heads, tokens)
-                seen[field] = now
-            pointers.append(t.data_ptr())
-        return pointers
+    def _c(self):
+        """The struct without strides (contiguous tensors)."""
+        c = self._struct
+        if c is None:
+            c = self._new_struct()
+            self.__dict__.update(_struct=c, _ref=ctypes.byref(c))
+        return c
 
-    def _look(self, field, t, heads, tokens):
+    def _call(self, entry, *args, position_batch=None):
+        """(struct, its reference, device pointers) of a call of `entry` on [batch, heads, tokens, head_dim]
+        tensors, given as (field of the struct, tensor, heads, tokens) one after the other.  Integers and
+        None are taken as they are (contiguous)."""
+        looks, pointers = [position_batch], []
+        for _, t, heads, tokens in args:
+            if t is None or isinstance(t, int):
+                looks.append(None)
+                pointers.append(t)
+            else:
+                looks.append((t.shape, t.stride(), t.dtype, t.is_cuda, heads, tokens))
+                pointers.append(t.data_ptr())
+        kept = self._kept
+        last = kept.get(entry)
+        if last is None or last[0] != looks:
+            c = self._new_struct()
+            if position_batch is not None:
+                c.position_batch = position_batch
+            for field, t, heads, tokens in args:
+                if t is not None and not isinstance(t, int):
+                    setattr(c, field, self._strides(field, t, heads, tokens))
+            last = kept[entry] = looks, c, ctypes.byref(c)
+        return last[1], last[2], pointers
+
+    def _strides(self, field, t, heads, tokens):
         wanted, strides = (self.batch, heads, tokens, self.head_dim), t.stride()
         if t.shape != wanted:
             raise ValueError(f"{field}: shape {tuple(t.shape)} instead of {wanted}")
@@ -177,7 +192,7 @@ class _StridedParams:
         token = strides[2] if tokens > 1 else self.head_dim
         head = strides[1] if heads > 1 else token * tokens
         batch = strides[0] if self.batch > 1 else head * heads
-        setattr(self._struct, field, _CStrides(batch, head, token))
+        return _CStrides(batch, head, token)
 
 
 _TORCH_DTYPES = {}
@@ -218,6 +233,7 @@ class HeadsParams(_StridedParams):
                 "norm_eps")
 
     def _positions(self, rotation, t):
+        """Pointer and values from one batch entry's positions to the next's."""
         per = 0
         if t is not None and not isinstance(t, int):
             n, axes = self.tokens, rotation.axes
@@ -228,10 +244,7 @@ class HeadsParams(_StridedParams):
             elif t.shape != (n, axes) and not (axes == 1 and t.shape == (n,)):
                 raise ValueError(f"positions: shape {tuple(t.shape)}")
             t = t.data_ptr()
-        if self._seen.get("position_batch") != per:
-            self._struct.position_batch = per
-            self._seen["position_batch"] = per
-        return t
+        return t, per
 
 
 @dataclasses.dataclass
@@ -460,87 +473,84 @@ def mosaic_bsa_rotation_init(rotary_dim: int, axes: int = 1, layout: int = ROTAT
 
 
 def _heads_forward(params, rotation, positions, q, k, q_out, k_out, v, v_out, rows):
-    params._c()
     h, kv, n = params.heads, params.kv_heads or params.heads, params.tokens
     m = n if rows is None else params.cache_tokens
-    pos = None if positions is None else params._positions(rotation, positions)
+    pos, per = params._positions(rotation, positions)
     rows = None if rows is None else _vector("rows", rows, params.batch * n, "int32")
     if v is None and v_out is None:
-        q, k, q_out, k_out = params._tensors(("q", q, h, n), ("k", k, kv, n), ("q_out", q_out, h, n),
-                                             ("k_out", k_out, kv, m))
+        _, ref, (q, k, q_out, k_out) = params._call(
+            "fwd", ("q", q, h, n), ("k", k, kv, n), ("q_out", q_out, h, n), ("k_out", k_out, kv, m),
+            position_batch=per)
     else:
-        q, k, q_out, k_out, v, v_out = params._tensors(
-            ("q", q, h, n), ("k", k, kv, n), ("q_out", q_out, h, n), ("k_out", k_out, kv, m),
-            ("v", v, kv, n), ("v_out", v_out, kv, m))
-    return pos, q, k, v, rows, q_out, k_out, v_out
+        _, ref, (q, k, q_out, k_out, v, v_out) = params._call(
+            "cached", ("q", q, h, n), ("k", k, kv, n), ("q_out", q_out, h, n), ("k_out", k_out, kv, m),
+            ("v", v, kv, n), ("v_out", v_out, kv, m), position_batch=per)
+    return ref, pos, q, k, v, rows, q_out, k_out, v_out
 
 
 def mosaic_bsa_rope_fwd(params: HeadsParams, rotation: Rotation, positions, q, k, q_out, k_out,
                         v=None, v_out=None, rows=None, stream=None) -> None:
-    pos, q, k, v, rows, q_out, k_out, v_out = _heads_forward(
+    ref, pos, q, k, v, rows, q_out, k_out, v_out = _heads_forward(
         params, rotation, positions, q, k, q_out, k_out, v, v_out, rows)
-    _check(load_library().mosaic_bsa_rope_fwd(params._ref, rotation.ref, pos, q, k, v, rows, q_out,
-                                              k_out, v_out, _stream(stream)))
+    _check(load_library().mosaic_bsa_rope_fwd(ref, rotation.ref, pos, q, k, v, rows, q_out, k_out, v_out,
+                                              _stream(stream)))
 
 
 def mosaic_bsa_rope_bwd(params: HeadsParams, rotation: Rotation, positions, dq_out, dk_out, dq, dk,
                         stream=None) -> None:
-    params._c()
     h, kv, n = params.heads, params.kv_heads or params.heads, params.tokens
-    pos = None if positions is None else params._positions(rotation, positions)
-    dq_out, dk_out, dq, dk = params._tensors(("q_out", dq_out, h, n), ("k_out", dk_out, kv, n),
-                                             ("q", dq, h, n), ("k", dk, kv, n))
-    _check(load_library().mosaic_bsa_rope_bwd(params._ref, rotation.ref, pos, dq_out, dk_out, dq,
-                                              dk, _stream(stream)))
+    pos, per = params._positions(rotation, positions)
+    _, ref, (dq_out, dk_out, dq, dk) = params._call(
+        "rope_bwd", ("q_out", dq_out, h, n), ("k_out", dk_out, kv, n), ("q", dq, h, n), ("k", dk, kv, n),
+        position_batch=per)
+    _check(load_library().mosaic_bsa_rope_bwd(ref, rotation.ref, pos, dq_out, dk_out, dq, dk,
+                                              _stream(stream)))
 
 
 def mosaic_bsa_qk_norm_rope_fwd(params: HeadsParams, rotation: Rotation, positions, q, k, q_weight,
                                 k_weight, q_out, k_out, v=None, v_out=None, rows=None,
                                 stream=None) -> None:
-    pos, q, k, v, rows, q_out, k_out, v_out = _heads_forward(
+    ref, pos, q, k, v, rows, q_out, k_out, v_out = _heads_forward(
         params, rotation, positions, q, k, q_out, k_out, v, v_out, rows)
     d = params.head_dim
     _check(load_library().mosaic_bsa_qk_norm_rope_fwd(
-        params._ref, rotation.ref, pos, q, k, v, _vector("q_weight", q_weight, d, "float32"),
+        ref, rotation.ref, pos, q, k, v, _vector("q_weight", q_weight, d, "float32"),
         _vector("k_weight", k_weight, d, "float32"), rows, q_out, k_out, v_out, _stream(stream)))
 
 
 def mosaic_bsa_qk_norm_rope_workspace_bytes(params: HeadsParams) -> int:
-    params._c()
-    return int(load_library().mosaic_bsa_qk_norm_rope_workspace_bytes(params._ref))
+    return int(load_library().mosaic_bsa_qk_norm_rope_workspace_bytes(ctypes.byref(params._c())))
 
 
 def mosaic_bsa_qk_norm_rope_bwd(params: HeadsParams, rotation: Rotation, positions, q, k, q_weight,
                                 k_weight, dq_out, dk_out, dq, dk, dq_weight, dk_weight, workspace,
                                 stream=None, workspace_bytes=None) -> None:
-    c = params._c()
     h, kv, n, d = params.heads, params.kv_heads or params.heads, params.tokens, params.head_dim
-    pos = None if positions is None else params._positions(rotation, positions)
+    pos, per = params._positions(rotation, positions)
     # the strides of dq and dk are arguments of their own: the fields of v and v_out hold them
-    q, k, dq_out, dk_out, dq, dk = params._tensors(
-        ("q", q, h, n), ("k", k, kv, n), ("q_out", dq_out, h, n), ("k_out", dk_out, kv, n),
-        ("v", dq, h, n), ("v_out", dk, kv, n))
+    c, ref, (q, k, dq_out, dk_out, dq, dk) = params._call(
+        "norm_bwd", ("q", q, h, n), ("k", k, kv, n), ("q_out", dq_out, h, n), ("k_out", dk_out, kv, n),
+        ("v", dq, h, n), ("v_out", dk, kv, n), position_batch=per)
     wb = _nbytes(workspace) if workspace_bytes is None else workspace_bytes
     _check(load_library().mosaic_bsa_qk_norm_rope_bwd(
-        params._ref, rotation.ref, pos, q, k, _vector("q_weight", q_weight, d, "float32"),
+        ref, rotation.ref, pos, q, k, _vector("q_weight", q_weight, d, "float32"),
         _vector("k_weight", k_weight, d, "float32"), dq_out, dk_out, ctypes.byref(c.v),
         ctypes.byref(c.v_out), dq, dk, _vector("dq_weight", dq_weight, d, "float32"),
         _vector("dk_weight", dk_weight, d, "float32"), _ptr(workspace), wb, _stream(stream)))
 
 
 def mosaic_bsa_window_workspace_bytes(params: WindowParams, op: int) -> int:
-    params._c()
-    return int(load_library().mosaic_bsa_window_workspace_bytes(params._ref, int(op)))
+    return int(load_library().mosaic_bsa_window_workspace_bytes(ctypes.byref(params._c()), int(op)))
 
 
 def mosaic_bsa_window_fwd(params: WindowParams, q, k, v, out, lse=None, q_lens=None, k_lens=None,
                           workspace=None, stream=None, workspace_bytes=None) -> None:
-    params._c()
     h, kv, nq, nk = params.heads, params.kv_heads or params.heads, params.q_tokens, params.k_tokens
     wb = _nbytes(workspace) if workspace_bytes is None else workspace_bytes
-    q, k, v, out = params._tensors(("q", q, h, nq), ("k", k, kv, nk), ("v", v, kv, nk), ("out", out, h, nq))
+    _, ref, (q, k, v, out) = params._call("fwd", ("q", q, h, nq), ("k", k, kv, nk), ("v", v, kv, nk),
+                                          ("out", out, h, nq))
     _check(load_library().mosaic_bsa_window_fwd(
-        params._ref, q, k, v, _vector("q_lens", q_lens, params.batch, "int32"),
+        ref, q, k, v, _vector("q_lens", q_lens, params.batch, "int32"),
         _vector("k_lens", k_lens, params.batch, "int32"), out,
         _vector("lse", lse, params.batch * h * nq, "float32"), _ptr(workspace), wb,
         _stream(stream)))
@@ -549,14 +559,13 @@ def mosaic_bsa_window_fwd(params: WindowParams, q, k, v, out, lse=None, q_lens=N
 def mosaic_bsa_window_bwd(params: WindowParams, q, k, v, out, lse, dout, dq, dk, dv,
                           workspace=None, q_lens=None, k_lens=None, stream=None,
                           workspace_bytes=None) -> None:
-    params._c()
     h, kv, nq, nk = params.heads, params.kv_heads or params.heads, params.q_tokens, params.k_tokens
     wb = _nbytes(workspace) if workspace_bytes is None else workspace_bytes
-    q, k, v, out, dout, dq, dk, dv = params._tensors(
-        ("q", q, h, nq), ("k", k, kv, nk), ("v", v, kv, nk), ("out", out, h, nq),
+    _, ref, (q, k, v, out, dout, dq, dk, dv) = params._call(
+        "bwd", ("q", q, h, nq), ("k", k, kv, nk), ("v", v, kv, nk), ("out", out, h, nq),
         ("dout", dout, h, nq), ("dq", dq, h, nq), ("dk", dk, kv, nk), ("dv", dv, kv, nk))
     _check(load_library().mosaic_bsa_window_bwd(
-        params._ref, q, k, v, out, _vector("lse", lse, params.batch * h * nq, "float32"), dout,
+        ref, q, k, v, out, _vector("lse", lse, params.batch * h * nq, "float32"), dout,
         _vector("q_lens", q_lens, params.batch, "int32"),
         _vector("k_lens", k_lens, params.batch, "int32"), dq, dk, dv, _ptr(workspace), wb,
         _stream(stream)))
