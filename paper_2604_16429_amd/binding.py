@@ -120,6 +120,14 @@ class Rotation:
             beta_slow, freq, ctypes.byref(self.c)))
         self.ref = ctypes.byref(self.c)
 
+    def __getstate__(self):
+        return self.axes, bytes(self.c)
+
+    def __setstate__(self, state):
+        self.axes = state[0]
+        self.c = _CRotation.from_buffer_copy(state[1])
+        self.ref = ctypes.byref(self.c)
+
 
 class _StridedParams:
     """Parameters whose C struct also carries the tensors' strides.  A call has a struct of its own for
@@ -134,10 +142,11 @@ class _StridedParams:
         self.__dict__[name] = value
         self.__dict__.update(_struct=None, _ref=None, _kept={})
 
-    def __copy__(self):
-        other = object.__new__(type(self))
-        other.__dict__.update(self.__dict__, _struct=None, _ref=None, _kept={})
-        return other
+    def __getstate__(self):
+        return {k: v for k, v in self.__dict__.items() if k not in ("_struct", "_ref", "_kept")}
+
+    def __setstate__(self, state):
+        self.__dict__.update(state, _struct=None, _ref=None, _kept={})
 
     def _new_struct(self):
         c = self._C()

@@ -1,5 +1,7 @@
 """What objects with a call's parameters keep between calls, threads and copies (CPU)."""
 import copy
+import dataclasses
+import pickle
 import threading
 
 import pytest
@@ -153,3 +155,32 @@ def test_many_layouts_of_one_object(monkeypatch):
         M.mosaic_bsa_window_fwd(p, q, q, q, q, stream=0)
     assert stub.seen == tokens
     assert all(len(x) <= 64 for x in p.__dict__.values() if isinstance(x, dict))
+
+
+COPIES = pytest.mark.parametrize("copied", [copy.copy, copy.deepcopy, lambda x: pickle.loads(pickle.dumps(x))],
+                                 ids=["copy", "deepcopy", "pickle"])
+
+
+@COPIES
+@pytest.mark.parametrize("used", [False, True])
+def test_copies_of_parameters(copied, used):
+    """Also after a call, which leaves a struct in the object."""
+    for p in (M.HeadsParams(2, 8, 4, 64, kv_heads=2, norm_eps=1e-5), M.WindowParams(2, 4, 8, 64, 64, n_sink=3)):
+        size = (M.mosaic_bsa_qk_norm_rope_workspace_bytes if isinstance(p, M.HeadsParams) else
+                lambda x: M.mosaic_bsa_window_workspace_bytes(x, binding.OP_BWD))
+        want = size(p) if used else size(dataclasses.replace(p))
+        c = copied(p)
+        assert c == p and type(c) is type(p) and size(c) == want
+        c.batch = 1
+        assert p.batch == 2 and size(p) == want
+
+
+@COPIES
+def test_copies_of_rotations(copied):
+    a = M.Rotation(64, axes=2, layout=binding.ROTATE_PAIRS, theta=500.0)
+    b = copied(a)
+    assert bytes(a.c) == bytes(b.c) and b.axes == 2
+    b.c.turns[0] = 5
+    b.c.rotary_dim = 32
+    assert a.c.turns[0] != 5 and a.c.rotary_dim == 64          # memory of its own
+    assert b.ref._obj is b.c
