@@ -429,6 +429,11 @@ int mosaic_bsa_qk_norm_rope_bwd(const mosaic_bsa_heads_params *params,
  * (a negative window_left or window_right: no bound on that side; window_right = 0 is causal).
  * A query that sees no key, and the rows i >= q_lens[b], give zeros and a log-sum-exp of
  * -infinity; their gradients are zeros, as are those of keys that no query sees.
+ *
+ * Sizes: with g = heads / kv_heads, fewer than 2^22 slices (batch x kv_heads), 2^29 keys and
+ * 2^29 rows (q_tokens x g) of a slice, and 2^24 tiles of 128 rows in all slices together;
+ * in the backward also 2^24 tiles of 128 keys and 2^23 groups of 32 sinks; q_tokens below
+ * 2^28 on a ring.
  */
 typedef struct {
     int32_t batch, heads, kv_heads;    /* kv_heads: 0 = heads; divides heads */

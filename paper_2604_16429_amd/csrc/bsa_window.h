@@ -21,9 +21,9 @@ constexpr float kLn2 = 0.6931471805599453f;
 // against it
 constexpr float kNoRef = -3.0e38f;
 constexpr int32_t kUnbounded = 1 << 30;
-// Longest sequence that a ring cache may have held: positions with a right bound (at most q_tokens,
-// fewer than 2^28) added stay below 2^31.
-constexpr int32_t kMostRingLength = 3 << 29;
+// Longest sequence that a ring cache may have held, and the bound on a chunk of queries on it: positions
+// with a right bound (at most q_tokens) added stay below 2^31.
+constexpr int32_t kMostRingLength = 3 << 29, kMostRingChunk = 1 << 28;
 
 struct Shape {
     int32_t batch, heads, kv_heads, group;

@@ -8,7 +8,9 @@
 
 namespace {
 
+using bsa::win::kMostRingChunk;
 using bsa::win::kUnbounded;
+constexpr int32_t kMostTokens = 1 << 29;
 
 struct Checked {
     bsa::win::Shape s;
@@ -18,20 +20,25 @@ struct Checked {
 
 int32_t bound(int32_t x) { return x < 0 || x > kUnbounded ? kUnbounded : x; }
 
-int check_params(const mosaic_bsa_window_params* p, Checked* c)
+int check_params(const mosaic_bsa_window_params* p, bool backward, Checked* c)
 {
     if (!p) return MOSAIC_BSA_ERR_NULL;
-    if (p->batch <= 0 || p->heads <= 0 || p->kv_heads < 0 || p->q_tokens <= 0 || p->k_tokens <= 0 ||
-        p->k_tokens >= kUnbounded)
+    if (p->batch <= 0 || p->heads <= 0 || p->kv_heads < 0 || p->q_tokens <= 0 || p->k_tokens <= 0)
         return MOSAIC_BSA_ERR_SHAPE;
     const int kv_heads = p->kv_heads == 0 ? p->heads : p->kv_heads;
     if (kv_heads > p->heads || p->heads % kv_heads) return MOSAIC_BSA_ERR_SHAPE;
     const int group = p->heads / kv_heads;
     const int64_t rows = (int64_t)p->q_tokens * group;
     const int64_t slices = (int64_t)p->batch * kv_heads;
-    // workgroups of 256 work items: fewer than 2^24 of them in a launch
-    if (rows >= kUnbounded || slices >= (1 << 23) ||
-        slices * ((rows + 31) / 32 + ((int64_t)p->k_tokens + 31) / 32) >= (int64_t)1 << 23)
+    // sums of positions and lengths stay below 2^31, launches below 2^32 work items: 256 of them to a tile
+    // of 128 rows, up to 1,024 to a slice of few rows
+    if (rows >= kMostTokens || p->k_tokens >= kMostTokens || slices >= (int64_t)1 << 22 ||
+        slices * ((rows + 127) / 128) >= (int64_t)1 << 24)
+        return MOSAIC_BSA_ERR_SHAPE;
+    if (p->ring > 0 && p->q_tokens >= kMostRingChunk) return MOSAIC_BSA_ERR_SHAPE;
+    // backward: 256 to a tile of 128 keys, 512 to a group of 32 that holds sinks
+    if (backward && (slices * (((int64_t)p->k_tokens + 127) / 128) >= (int64_t)1 << 24 ||
+                     slices * (((int64_t)std::min(p->n_sink, p->k_tokens) + 31) / 32) >= (int64_t)1 << 23))
         return MOSAIC_BSA_ERR_SHAPE;
     if (p->head_dim != 32 && p->head_dim != 64 && p->head_dim != 128) return MOSAIC_BSA_ERR_HEAD_DIM;
     if (p->dtype != MOSAIC_BSA_F32 && p->dtype != MOSAIC_BSA_BF16) return MOSAIC_BSA_ERR_DTYPE;
@@ -82,7 +89,7 @@ bool unaligned4(const void* p) { return ((uintptr_t)p & 3u) != 0; }
 extern "C" size_t mosaic_bsa_window_workspace_bytes(const mosaic_bsa_window_params* params, int op)
 {
     Checked c;
-    if (check_params(params, &c) != MOSAIC_BSA_OK) return 0;
+    if (check_params(params, op == MOSAIC_BSA_OP_BWD, &c) != MOSAIC_BSA_OK) return 0;
     if (op == MOSAIC_BSA_OP_FWD) return bsa::window_fwd_workspace(c.is_bf16, c.D, c.s);
     if (op == MOSAIC_BSA_OP_BWD && !c.s.ring) return bsa::window_bwd_workspace(c.is_bf16, c.D, c.s);
     return 0;
@@ -94,7 +101,7 @@ extern "C" int mosaic_bsa_window_fwd(const mosaic_bsa_window_params* params, con
                                      size_t workspace_bytes, void* hip_stream)
 {
     Checked c;
-    if (int rc = check_params(params, &c)) return rc;
+    if (int rc = check_params(params, false, &c)) return rc;
     const mosaic_bsa_window_params& p = *params;
     bsa::win::Shape& s = c.s;
     if (int rc = check_tensor(c, q, p.q, s.heads, s.q_tokens, false, &s.q)) return rc;
@@ -121,7 +128,7 @@ extern "C" int mosaic_bsa_window_bwd(const mosaic_bsa_window_params* params, con
                                      void* workspace, size_t workspace_bytes, void* hip_stream)
 {
     Checked c;
-    if (int rc = check_params(params, &c)) return rc;
+    if (int rc = check_params(params, true, &c)) return rc;
     const mosaic_bsa_window_params& p = *params;
     bsa::win::Shape& s = c.s;
     if (s.ring) return MOSAIC_BSA_ERR_WINDOW;
