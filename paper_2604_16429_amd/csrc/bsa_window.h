@@ -317,8 +317,7 @@ __device__ __forceinline__ int64_t part_of(const Shape& s, const Parts& p, uint3
 inline int64_t most_keys(const Shape& s, int rows)
 {
     const int64_t tokens = ((int64_t)rows + s.group - 1) / s.group + 1;
-    const int64_t right = s.right < tokens ? s.right : tokens;
-    const int64_t span = (int64_t)s.left + right + tokens + s.sinks;
+    const int64_t span = (int64_t)s.left + s.right + tokens + s.sinks;
     const int64_t all = s.ring ? (int64_t)s.ring + s.sinks : (int64_t)s.k_tokens;
     return span < all ? span : all;
 }

@@ -215,7 +215,9 @@ bool is_step(bool is_bf16, int D, const Shape& s)
 // least to each.  Joining costs a launch, so that few keys stay whole, and two or three parts come from 1,280
 // keys on.  us, whole | split: bf16, head dim 64, 300 keys 11 | 17, 600 16 | 12, 2,255 45 | 17, 210
 // workgroups of 304 10 | 20, of 819 16 | 24, 160 of 1,700, head dim 128, 43 | 35; fp32, head dim 64, 215
-// keys 16 | 23, 411 17 | 13.  Parts of 128 keys: 9,830 keys, one token, 18 us instead of 14.
+// keys 16 | 23, 411 17 | 13.  Parts of 128 keys: 9,830 keys, one token, 18 us instead of 14.  Keys count on both
+// sides of a tile: bf16, head dim 64, one head of 3,000 tokens, 63 to the left and all to the right 43 | 19;
+// near the borders of the rule up to a third slower (16 slices of 952, head dim 128, 152 and 238 18 | 23).
 int splits_of(bool is_bf16, int D, const Shape& s)
 {
     const bool step = is_step(is_bf16, D, s);

@@ -3,7 +3,7 @@ matrix-core path, large launches of strided tensors, gradients of large scores."
 import pytest
 import torch
 
-from tests.test_gpu_window import BF16, DTYPES
+from tests.test_gpu_window import BF16, DTYPES, run
 from tests.window_reference import attention, visible
 
 pytestmark = pytest.mark.gpu
@@ -101,3 +101,12 @@ def test_training_of_many_long_slices():
     assert bool(((one[0][0, 0, :300].cpu().double() - r["out"]).abs() <= r["out_tol"](BF16)).all())
     del one, all_, x, y
     torch.cuda.empty_cache()                       # (75 GB)
+
+
+@DTYPES
+@pytest.mark.parametrize("D", [32, 64, 128])
+@pytest.mark.parametrize("left,right,sinks", [(63, -1, 0), (10, 900, 4), (300, 700, 33)])
+def test_few_rows_with_keys_to_the_right(dtype, D, left, right, sinks):
+    """Forward and backward of launches whose keys are shared out on both sides of a tile."""
+    run(dtype, 1, 2, 1, 1500, 1500, D, left, right, sinks, train=True, seed=D + left)
+    run(dtype, 2, 1, 1, 40, 1300, D, left, right, sinks, k_lens=[1300, 900], q_lens=[40, 33], seed=D)

@@ -63,3 +63,15 @@ def test_chunks_on_rings():
     p = dict(batch=1, heads=1, head_dim=32, window_left=15)
     assert forward(M.WindowParams(q_tokens=1 << 28, k_tokens=1 << 28 | 16, ring=1 << 28 | 16, **p)) == -2
     assert forward(M.WindowParams(q_tokens=(1 << 28) - 1, k_tokens=1 << 28 | 16, ring=1 << 28 | 16, **p)) == -1
+
+
+@pytest.mark.parametrize("kw,split", [
+    (dict(heads=1, q_tokens=3000, k_tokens=3000, window_left=63, window_right=-1), True),
+    (dict(heads=1, q_tokens=3000, k_tokens=3000, window_left=63, window_right=2000), True),
+    (dict(heads=1, q_tokens=3000, k_tokens=3000, window_left=63, window_right=0), False),
+])
+def test_keys_to_the_right_count(kw, split):
+    """Few workgroups with many keys share them out (which takes a workspace), on whichever side they are."""
+    p = M.WindowParams(batch=1, k_tokens=kw["k_tokens"], head_dim=64, dtype=binding.BF16,
+                       **{k: v for k, v in kw.items() if k != "k_tokens"})
+    assert (M.mosaic_bsa_window_workspace_bytes(p, binding.OP_FWD) > 0) == split
