@@ -70,3 +70,63 @@ def test_far_positions_against_exact_angles(first, transpose):
     a, b = q64[0, 0].chunk(2, -1)
     ref = torch.cat([a * c - b * s, b * c + a * s], -1).view(1, 1, N, D)
     check(out, ref, rotation_tol(ref, pair_size(q64), FP32), "q")
+
+
+@DTYPES
+@pytest.mark.parametrize("D,rd,memory", [(32, 32, "tokens"), (64, 24, "heads"), (128, 128, "tokens"), (64, 62, 3)])
+def test_norm_gradients_over_their_inputs(dtype, D, rd, memory):
+    """dq and dk may be q and k: the same bits as in memory of their own."""
+    M, binding = lib()
+    B, h, kv, N = 2, 5, 2, 70
+    gen = torch.Generator().manual_seed(D)
+    q, k = (tensor((B, x, N, D), dtype, gen, memory)[0] for x in (h, kv))
+    gq, gk = (tensor((B, x, N, D), dtype, gen, "heads")[0] for x in (h, kv))
+    qw, kw = (1.0 + 0.3 * torch.randn(D, generator=gen).cuda() for _ in range(2))
+    p = M.HeadsParams(B, N, h, D, binding.BF16 if dtype is BF16 else binding.F32, kv_heads=kv)
+    rot = M.Rotation(rd)
+    ws = torch.empty(M.mosaic_bsa_qk_norm_rope_workspace_bytes(p), dtype=torch.uint8, device="cuda")
+    results = []
+    for over in (False, True):
+        dq, dk = (q, k) if over else (nan_like(q), nan_like(k))
+        dw = torch.full((2, D), float("nan"), device="cuda")
+        M.mosaic_bsa_qk_norm_rope_bwd(p, rot, None, q, k, qw, kw, gq, gk, dq, dk, dw[0], dw[1], ws)
+        results.append([t.clone() for t in (dq, dk, dw)])
+    for a, b in zip(*results):
+        assert bool(torch.isfinite(a).all()) and torch.equal(a, b)
+
+
+@DTYPES
+def test_rotated_heads_go_into_the_selection(dtype, oracle):
+    """Queries and keys rotated by their grid positions, then block selection and attention on them, against
+    the oracle on the rotated values."""
+    import dataclasses
+
+    from inputs.fields import make_problem, round_to_bf16
+    from tests import gpu_util
+    M, binding = lib()
+    prob = make_problem(1)
+    cfg = dataclasses.replace(prob.cfg, dtype="bf16" if dtype is BF16 else "fp32")
+    q, k, v = (round_to_bf16(x) if dtype is BF16 else x for x in (prob.q, prob.k, prob.v))
+    qd, kd = gpu_util.to_dev(q, cfg), gpu_util.to_dev(k, cfg)
+    N = cfg.grid_h * cfg.grid_w
+    t = torch.arange(N, dtype=torch.int32)
+    pos = torch.stack([t // cfg.grid_w, t % cfg.grid_w], -1)
+    qr, kr = torch.full_like(qd, float("nan")), torch.full_like(kd, float("nan"))
+    M.mosaic_bsa_rope_fwd(
+        M.HeadsParams(cfg.batch, N, cfg.heads, cfg.head_dim, binding.BF16 if dtype is BF16 else binding.F32,
+                      kv_heads=kd.shape[1]),
+        M.Rotation(cfg.head_dim, axes=2), pos.cuda(), qd, kd, qr, kr)
+    for got, x in ((qr, qd), (kr, kd)):
+        x64 = x.cpu().double()
+        ref = rotate(x64, pos.unsqueeze(0), frequencies(cfg.head_dim // 2), 1.0, cfg.head_dim, 2, False)
+        check(got, ref, rotation_tol(ref, pair_size(x64), dtype), "rotated")
+    idx = gpu_util.select_dev(cfg, qr, kr)
+    out, _ = gpu_util.fwd_dev(cfg, qr, kr, gpu_util.to_dev(v, cfg), idx)
+    rotated = [x.float().cpu().numpy() for x in (qr, kr)]
+    s = oracle.shape_of(cfg)
+    want = oracle.select(s, *rotated)
+    assert (idx.cpu().numpy() == want).all()
+    ref, _ = oracle.fwd(s, *rotated, v, want)
+    off = abs(out.float().cpu().numpy() - ref).max()
+    # bf16: a weight's and the result's rounding, 2^-8 each of the largest value; fp32: as elsewhere
+    assert off <= (2.0 ** -7 if dtype is BF16 else 1e-5) * abs(v).max()
