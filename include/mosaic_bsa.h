@@ -343,7 +343,8 @@ typedef struct {
  * Fills *out.  rotary_dim: 0 .. 128, a multiple of 2 * axes.  theta > 0 (10000 in the
  * paper).  scaling: MOSAIC_BSA_SCALE_*; factor >= 1; original_tokens > 0 and beta_fast >
  * beta_slow > 0 for RAMP (0, 0: 32 and 1).  inv_freq: NULL, or d / 2 frequencies in radians
- * per position that replace theta and the scaling (the magnitude is 1 then).
+ * per position that replace theta and the scaling (out->magnitude is 1 then; the caller may
+ * set it to what belongs to those frequencies).
  */
 int mosaic_bsa_rotation_init(int32_t rotary_dim, int32_t axes, int32_t layout, double theta,
                              int32_t scaling, double factor, double original_tokens,

@@ -101,7 +101,8 @@ class _CWindowParams(ctypes.Structure):
 class Rotation:
     """A mosaic_bsa_rotation, filled by mosaic_bsa_rotation_init (see there): the frequencies
     of a rotation of heads by their positions, made once and used by every call.  inv_freq:
-    frequencies in radians per position that replace theta and the scaling."""
+    frequencies in radians per position that replace theta and the scaling; `c.magnitude`, 1 then, may
+    be set to what belongs to them."""
 
     def __init__(self, rotary_dim: int, axes: int = 1, layout: int = ROTATE_HALVES,
                  theta: float = 10000.0, scaling: int = SCALE_NONE, factor: float = 1.0,

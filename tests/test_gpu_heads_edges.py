@@ -130,3 +130,18 @@ def test_rotated_heads_go_into_the_selection(dtype, oracle):
     off = abs(out.float().cpu().numpy() - ref).max()
     # bf16: a weight's and the result's rounding, 2^-8 each of the largest value; fp32: as elsewhere
     assert off <= (2.0 ** -7 if dtype is BF16 else 1e-5) * abs(v).max()
+
+
+def test_given_frequencies_with_a_magnitude():
+    M, binding = lib()
+    N, D = 50, 64
+    gen = torch.Generator().manual_seed(8)
+    q, q64 = tensor((1, 2, N, D), FP32, gen, "heads")
+    freq = [0.5 / (1 + i) for i in range(D // 2)]
+    rot = M.Rotation(D, inv_freq=freq)
+    assert rot.c.magnitude == 1.0
+    rot.c.magnitude = 1.25
+    out = nan_like(q)
+    M.mosaic_bsa_rope_fwd(M.HeadsParams(1, N, 2, D, binding.F32), rot, None, q, None, out, None)
+    ref = rotate(q64, torch.arange(N).view(1, N, 1), freq, 1.25, D, 1, False)
+    check(out, ref, rotation_tol(ref, pair_size(q64) * 1.25, FP32), "q")
