@@ -401,7 +401,8 @@ int mosaic_bsa_qk_norm_rope_fwd(const mosaic_bsa_heads_params *params,
                                 const float *q_weight, const float *k_weight, const int32_t *rows,
                                 void *q_out, void *k_out, void *v_out, void *hip_stream);
 /*
- * Its gradient (without rows and v).
+ * Its gradient (without rows and v).  The sums of dq_weight and dk_weight run in fp32 inside a
+ * workgroup, in 64 bits over the workgroups.
  *   q, k                  in   device, the forward's inputs (params->q, k)
  *   dq_out, dk_out        in   device (params->q_out, k_out)
  *   dq, dk                out  device, strides dq_strides, dk_strides; may be dq_out and dk_out, or
@@ -453,7 +454,9 @@ typedef struct {
     mosaic_bsa_strides q, k, v, out, dout, dq, dk, dv;
 } mosaic_bsa_window_params;
 
-/* Bytes of workspace for op MOSAIC_BSA_OP_FWD or _BWD; 0 if none or params is invalid. */
+/* Bytes of workspace for op MOSAIC_BSA_OP_FWD or _BWD; 0 if none or params is invalid.  Forward: up to
+ * 34 MB.  Backward: 8 bytes per query head and token; up to 2 MB x head_dim where few workgroups have
+ * long walks; sums of the sinks' keys. */
 size_t mosaic_bsa_window_workspace_bytes(const mosaic_bsa_window_params *params, int op);
 
 /*

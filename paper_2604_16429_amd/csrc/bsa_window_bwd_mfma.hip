@@ -311,7 +311,7 @@ __global__ __launch_bounds__(256, 2) void window_dkdv_mfma_kernel(
 
 // delta_i = sum_j P_ij dP_ij of 128 rows, and lse in base 2, for the kernels of dQ, dK and dV: the tiles and
 // the two products of the dQ kernel below.  Little but two operands in registers: four wavefronts per SIMD, at head dim
-// 128 with tiles of 32 keys.  1.5 degrees, head dim 128, window 1,024: 1,140 us, two wavefronts and tiles of 64 1,180.
+// 128 with tiles of 32 keys.  1.5 degrees, head dim 128, window 1,024: 1,120 us, two wavefronts and tiles of 64 1,180.
 template <int D>
 __global__ __launch_bounds__(256, 4) void window_delta_mfma_kernel(
     const uint16_t* __restrict__ q, const uint16_t* __restrict__ k, const uint16_t* __restrict__ v,
