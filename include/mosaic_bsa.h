@@ -83,8 +83,10 @@ enum {
     MOSAIC_BSA_ERR_ROTATION = -10, /* rotation: rotary_dim, axes, layout or scaling */
     MOSAIC_BSA_ERR_STRIDE = -11,   /* a stride that is negative or too large, or rows of an
                                       output that share memory */
-    MOSAIC_BSA_ERR_WINDOW = -12    /* window: negative sinks, ring too small for the
+    MOSAIC_BSA_ERR_WINDOW = -12,   /* window: negative sinks, ring too small for the
                                       window, or a ring in a backward pass */
+    MOSAIC_BSA_ERR_PAGES = -13     /* pages: none, page_tokens no power of two up to 65536,
+                                      or more tokens than a sequence may have */
 };
 
 enum { MOSAIC_BSA_F32 = 0, MOSAIC_BSA_BF16 = 1 };
@@ -485,6 +487,91 @@ int mosaic_bsa_window_bwd(const mosaic_bsa_window_params *params, const void *q,
                           const void *v, const void *out, const float *lse, const void *dout,
                           const int32_t *q_lens, const int32_t *k_lens, void *dq, void *dk,
                           void *dv, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * A key/value cache in pages, and attention over it for a batch that may share a prefix.
+ *
+ * The cache is a pool of pages, k_pages and v_pages [pages, kv_heads, page_tokens, D] (strides:
+ * `batch` steps from page to page).  Sequence b is made of
+ *   P tokens that all sequences share: token j < P is row j % page_tokens of page
+ *     prefix_table[j / page_tokens]; P = *prefix_len, or prefix_tokens where that is NULL;
+ *   k_lens[b] tokens of its own, with pages from the beginning of its row of the table: token P + o is row
+ *     o % page_tokens of page page_table[b, o / page_tokens].
+ * Its q_lens[b] queries stand at its end: query i is token P + k_lens[b] - q_lens[b] + i.
+ * Lengths live in device memory, so that a captured graph replays with other ones; values are
+ * held to [0, prefix_tokens], [0, table_pages * page_tokens] and [0, q_tokens].  Table entries behind
+ * a sequence's last page are not read.  An entry outside [0, pages) names no page: nothing is
+ * written there, and its tokens are seen by no query.
+ * To fill the prefix, call mosaic_bsa_paged_append with batch 1, prefix_tokens 0 and the
+ * prefix's table as page_table.
+ *
+ * Sizes: with g = heads / kv_heads, prefix_tokens, table_pages x page_tokens and q_tokens x g below
+ * 2^29, batch x kv_heads below 2^22, and (append) batch x q_tokens up to 2^30, (attention) fewer than
+ * 2^23 tiles of 32 rows (q_tokens x g of each batch x kv_heads) in all.
+ */
+typedef struct {
+    int32_t batch, heads, kv_heads;    /* kv_heads: 0 = heads; divides heads */
+    int32_t q_tokens;                  /* new tokens of a sequence: rows of q, k, v and out */
+    int32_t head_dim;                  /* 32, 64 or 128 */
+    int32_t dtype;                     /* MOSAIC_BSA_F32 or _BF16 */
+    int32_t pages, page_tokens;        /* page_tokens: a power of two up to 65536 */
+    int32_t table_pages;               /* entries of a sequence's row of page_table */
+    int32_t prefix_tokens;             /* 0: no prefix */
+    int32_t window_left, n_sink;       /* attention: as in mosaic_bsa_window_params */
+    int32_t position_batch;            /* append: as in mosaic_bsa_heads_params */
+    float norm_eps;                    /* append: likewise */
+    float softmax_scale;               /* attention: <= 0 selects 1/sqrt(head_dim) */
+    mosaic_bsa_strides q, k, v;        /* [batch, heads or kv_heads, q_tokens, D] */
+    mosaic_bsa_strides out;            /* append: of q_out */
+    mosaic_bsa_strides k_pages, v_pages;
+} mosaic_bsa_paged_params;
+
+/*
+ * Appends new tokens to the cache: with n the norm of mosaic_bsa_qk_norm_rope_fwd (without weights: none)
+ * and R the rotation of mosaic_bsa_rope_fwd,
+ *   q_out = R n(q),  k_pages <- R n(k),  v_pages <- v
+ * for the tokens i < q_lens[b] of every sequence, whose lengths count them already.
+ *   positions           in   device, int32 [q_tokens, axes] or [B, q_tokens, axes]; NULL (axes 1): the
+ *                            tokens' places in their sequences, P + k_lens[b] - q_lens[b] + i
+ *   q, k, v             in   device, the new tokens
+ *   q_weight, k_weight  in   device, fp32 [D]; both NULL: no norms
+ *   q_lens              in   device, int32 [B], or NULL: q_tokens
+ *   k_lens              in   device, int32 [B]
+ *   page_table          in   device, int32 [B, table_pages]
+ *   prefix_len          in   device, int32 [1], or NULL
+ *   q_out               out  device; may be q (same strides).  Rows i >= q_lens[b] are left as they are
+ *   k_pages, v_pages    out  device: rows of tokens i < q_lens[b] of their own (a token before those,
+ *                            where q_lens[b] > k_lens[b], belongs to the prefix and is not written);
+ *                            no two tokens may name the same row of the same page
+ * Base pointers and strides need the element's alignment only; 16 bytes are fastest.
+ */
+int mosaic_bsa_paged_append(const mosaic_bsa_paged_params *params,
+                            const mosaic_bsa_rotation *rotation, const int32_t *positions,
+                            const void *q, const void *k, const void *v, const float *q_weight,
+                            const float *k_weight, const int32_t *q_lens, const int32_t *k_lens,
+                            const int32_t *page_table, const int32_t *prefix_len, void *q_out,
+                            void *k_pages, void *v_pages, void *hip_stream);
+
+/* Bytes of workspace of mosaic_bsa_paged_fwd; 0 if none or params is invalid. */
+size_t mosaic_bsa_paged_workspace_bytes(const mosaic_bsa_paged_params *params);
+/*
+ * Attention over the cache: query i at token p of its sequence sees token j where
+ *   j <= p  and  (j >= p - window_left or j < n_sink)     (window_left < 0: all j <= p)
+ * A query that sees no token, and the rows i >= q_lens[b], give zeros and a log-sum-exp of -infinity.
+ *   q                   in   device; bases and strides of all tensors multiples of 16 bytes
+ *   k_pages, v_pages    in   device; tokens within the lengths must be finite, the rest may be anything
+ *   q_lens, k_lens, page_table, prefix_len   as above
+ *   prefix_table        in   device, int32 [ceil(prefix_tokens / page_tokens)]; NULL if there is none
+ *   out                 out  device, must not alias an input
+ *   lse                 out  device, fp32 [batch, heads, q_tokens], natural log; may be NULL
+ *   workspace                mosaic_bsa_paged_workspace_bytes(..) bytes (may be 0)
+ * Sums run in a fixed order: the same call gives the same bits.
+ */
+int mosaic_bsa_paged_fwd(const mosaic_bsa_paged_params *params, const void *q, const void *k_pages,
+                         const void *v_pages, const int32_t *q_lens, const int32_t *k_lens,
+                         const int32_t *page_table, const int32_t *prefix_table,
+                         const int32_t *prefix_len, void *out, float *lse, void *workspace,
+                         size_t workspace_bytes, void *hip_stream);
 
 /*
  * Checker for selections that were not produced by mosaic_bsa_select: the

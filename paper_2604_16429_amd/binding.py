@@ -98,6 +98,15 @@ class _CWindowParams(ctypes.Structure):
                 [(n, _CStrides) for n in ("q", "k", "v", "out", "dout", "dq", "dk", "dv")])
 
 
+class _CPagedParams(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in
+                 ("batch", "heads", "kv_heads", "q_tokens", "head_dim", "dtype", "pages",
+                  "page_tokens", "table_pages", "prefix_tokens", "window_left", "n_sink",
+                  "position_batch")] +
+                [("norm_eps", ctypes.c_float), ("softmax_scale", ctypes.c_float)] +
+                [(n, _CStrides) for n in ("q", "k", "v", "out", "k_pages", "v_pages")])
+
+
 class Rotation:
     """A mosaic_bsa_rotation, filled by mosaic_bsa_rotation_init (see there): the frequencies
     of a rotation of heads by their positions, made once and used by every call.  inv_freq:
@@ -187,8 +196,13 @@ class _StridedParams:
             last = kept[entry] = looks, c, ctypes.byref(c)
         return last[1], last[2], pointers
 
+    def _entries(self, field):
+        """First dimension of a field's tensor."""
+        return self.batch
+
     def _strides(self, field, t, heads, tokens):
-        wanted, strides = (self.batch, heads, tokens, self.head_dim), t.stride()
+        entries = self._entries(field)
+        wanted, strides = (entries, heads, tokens, self.head_dim), t.stride()
         if t.shape != wanted:
             raise ValueError(f"{field}: shape {tuple(t.shape)} instead of {wanted}")
         if t.dtype is not _named_dtype(self.dtype) or not t.is_cuda:
@@ -201,7 +215,7 @@ class _StridedParams:
         # a dimension of one entry may carry any stride: the contiguous one is taken
         token = strides[2] if tokens > 1 else self.head_dim
         head = strides[1] if heads > 1 else token * tokens
-        batch = strides[0] if self.batch > 1 else head * heads
+        batch = strides[0] if entries > 1 else head * heads
         return _CStrides(batch, head, token)
 
 
@@ -226,8 +240,26 @@ def _vector(name, t, size, dtype_name):
     return t.data_ptr()
 
 
+class _Positions:
+    """Positions of [batch, n] tokens."""
+
+    def _positions_of(self, rotation, t, n):
+        """Pointer and values from one batch entry's positions to the next's."""
+        per = 0
+        if t is not None and not isinstance(t, int):
+            axes = rotation.axes
+            if t.dtype is not _named_dtype("int32") or not t.is_cuda or not t.is_contiguous():
+                raise ValueError("positions: contiguous int32 on a GPU expected")
+            if t.shape == (self.batch, n, axes) or (axes == 1 and t.shape == (self.batch, n)):
+                per = n * axes
+            elif t.shape != (n, axes) and not (axes == 1 and t.shape == (n,)):
+                raise ValueError(f"positions: shape {tuple(t.shape)}")
+            t = t.data_ptr()
+        return t, per
+
+
 @dataclasses.dataclass
-class HeadsParams(_StridedParams):
+class HeadsParams(_Positions, _StridedParams):
     """Mirror of the C struct mosaic_bsa_heads_params (the strides come from the tensors)."""
     batch: int
     tokens: int
@@ -243,18 +275,7 @@ class HeadsParams(_StridedParams):
                 "norm_eps")
 
     def _positions(self, rotation, t):
-        """Pointer and values from one batch entry's positions to the next's."""
-        per = 0
-        if t is not None and not isinstance(t, int):
-            n, axes = self.tokens, rotation.axes
-            if t.dtype is not _named_dtype("int32") or not t.is_cuda or not t.is_contiguous():
-                raise ValueError("positions: contiguous int32 on a GPU expected")
-            if t.shape == (self.batch, n, axes) or (axes == 1 and t.shape == (self.batch, n)):
-                per = n * axes
-            elif t.shape != (n, axes) and not (axes == 1 and t.shape == (n,)):
-                raise ValueError(f"positions: shape {tuple(t.shape)}")
-            t = t.data_ptr()
-        return t, per
+        return self._positions_of(rotation, t, self.tokens)
 
 
 @dataclasses.dataclass
@@ -276,6 +297,33 @@ class WindowParams(_StridedParams):
     _C = _CWindowParams
     _SCALARS = ("batch", "heads", "q_tokens", "k_tokens", "head_dim", "dtype", "kv_heads",
                 "window_left", "window_right", "n_sink", "ring", "softmax_scale")
+
+
+@dataclasses.dataclass
+class PagedParams(_Positions, _StridedParams):
+    """Mirror of the C struct mosaic_bsa_paged_params (the strides come from the tensors)."""
+    batch: int
+    heads: int
+    q_tokens: int
+    head_dim: int
+    pages: int
+    page_tokens: int
+    table_pages: int
+    dtype: int = BF16
+    kv_heads: int = 0
+    prefix_tokens: int = 0
+    window_left: int = -1
+    n_sink: int = 0
+    norm_eps: float = 1e-6
+    softmax_scale: float = 0.0
+
+    _C = _CPagedParams
+    _SCALARS = ("batch", "heads", "q_tokens", "head_dim", "pages", "page_tokens", "table_pages",
+                "dtype", "kv_heads", "prefix_tokens", "window_left", "n_sink", "norm_eps",
+                "softmax_scale")
+
+    def _entries(self, field):
+        return self.pages if field in ("k_pages", "v_pages") else self.batch
 
 
 def library_path() -> str:
@@ -339,6 +387,13 @@ def load_library() -> ctypes.CDLL:
         lib.mosaic_bsa_window_fwd.argtypes = [wp] + [vp] * 8 + [sz, vp]
         lib.mosaic_bsa_window_bwd.restype = i32
         lib.mosaic_bsa_window_bwd.argtypes = [wp] + [vp] * 12 + [sz, vp]
+        gp = ctypes.POINTER(_CPagedParams)
+        lib.mosaic_bsa_paged_append.restype = i32
+        lib.mosaic_bsa_paged_append.argtypes = [gp, rp] + [vp] * 14
+        lib.mosaic_bsa_paged_workspace_bytes.restype = sz
+        lib.mosaic_bsa_paged_workspace_bytes.argtypes = [gp]
+        lib.mosaic_bsa_paged_fwd.restype = i32
+        lib.mosaic_bsa_paged_fwd.argtypes = [gp] + [vp] * 11 + [sz, vp]
         lib.mosaic_bsa_strerror.restype = ctypes.c_char_p
         lib.mosaic_bsa_strerror.argtypes = [i32]
         _lib = lib
@@ -579,3 +634,47 @@ def mosaic_bsa_window_bwd(params: WindowParams, q, k, v, out, lse, dout, dq, dk,
         _vector("q_lens", q_lens, params.batch, "int32"),
         _vector("k_lens", k_lens, params.batch, "int32"), dq, dk, dv, _ptr(workspace), wb,
         _stream(stream)))
+
+
+# ---- a cache in pages: k_pages and v_pages of shape [pages, kv_heads, page_tokens, head_dim] with any
+# strides of the first three dimensions
+
+def mosaic_bsa_paged_append(params: PagedParams, rotation: Rotation, positions, q, k, v, q_weight,
+                            k_weight, q_lens, k_lens, page_table, prefix_len, q_out, k_pages, v_pages,
+                            stream=None) -> None:
+    h, kv, n, d = params.heads, params.kv_heads or params.heads, params.q_tokens, params.head_dim
+    b, t = params.batch, params.page_tokens
+    pos, per = params._positions_of(rotation, positions, n)
+    _, ref, (q, k, v, q_out, k_pages, v_pages) = params._call(
+        "append", ("q", q, h, n), ("k", k, kv, n), ("v", v, kv, n), ("out", q_out, h, n),
+        ("k_pages", k_pages, kv, t), ("v_pages", v_pages, kv, t), position_batch=per)
+    _check(load_library().mosaic_bsa_paged_append(
+        ref, rotation.ref, pos, q, k, v, _vector("q_weight", q_weight, d, "float32"),
+        _vector("k_weight", k_weight, d, "float32"), _vector("q_lens", q_lens, b, "int32"),
+        _vector("k_lens", k_lens, b, "int32"),
+        _vector("page_table", page_table, b * params.table_pages, "int32"),
+        _vector("prefix_len", prefix_len, 1, "int32"), q_out, k_pages, v_pages, _stream(stream)))
+
+
+def mosaic_bsa_paged_workspace_bytes(params: PagedParams) -> int:
+    return int(load_library().mosaic_bsa_paged_workspace_bytes(ctypes.byref(params._c())))
+
+
+def mosaic_bsa_paged_fwd(params: PagedParams, q, k_pages, v_pages, q_lens, k_lens, page_table,
+                         prefix_table, prefix_len, out, lse=None, workspace=None, stream=None,
+                         workspace_bytes=None) -> None:
+    h, kv, n, b = params.heads, params.kv_heads or params.heads, params.q_tokens, params.batch
+    t = params.page_tokens
+    wb = _nbytes(workspace) if workspace_bytes is None else workspace_bytes
+    _, ref, (q, k_pages, v_pages, out) = params._call(
+        "fwd", ("q", q, h, n), ("k_pages", k_pages, kv, t), ("v_pages", v_pages, kv, t),
+        ("out", out, h, n))
+    if params.prefix_tokens <= 0:
+        prefix_table = None
+    _check(load_library().mosaic_bsa_paged_fwd(
+        ref, q, k_pages, v_pages, _vector("q_lens", q_lens, b, "int32"),
+        _vector("k_lens", k_lens, b, "int32"),
+        _vector("page_table", page_table, b * params.table_pages, "int32"),
+        _vector("prefix_table", prefix_table, -(-params.prefix_tokens // max(t, 1)), "int32"),
+        _vector("prefix_len", prefix_len, 1, "int32"), out,
+        _vector("lse", lse, b * h * n, "float32"), _ptr(workspace), wb, _stream(stream)))

@@ -562,6 +562,9 @@ extern "C" const char* mosaic_bsa_strerror(int code)
     case MOSAIC_BSA_ERR_WINDOW:
         return "invalid window: n_sink must not be negative; a ring is for the forward only, takes "
                "k_lens and k_tokens = n_sink + ring, and needs 0 <= window_left <= ring - q_tokens";
+    case MOSAIC_BSA_ERR_PAGES:
+        return "invalid pages: there must be some, page_tokens a power of two up to 65536, prefix_tokens "
+               "not negative and table_pages * page_tokens positive, both below 2^29";
     }
     return "unknown error code";
 }

@@ -51,4 +51,19 @@ inline bool rows_meet(const mosaic_bsa_strides& s, int64_t batch, int64_t heads,
     return false;
 }
 
+// Pages and lengths of a paged cache: what both of its entry points need.
+inline int check_pages(const mosaic_bsa_paged_params& p)
+{
+    constexpr int64_t most = (int64_t)1 << 29;
+    if (p.pages <= 0 || p.page_tokens <= 0 || p.page_tokens > 65536 ||
+        (p.page_tokens & (p.page_tokens - 1)) || p.table_pages <= 0 ||
+        (int64_t)p.table_pages * p.page_tokens >= most || p.prefix_tokens < 0 || p.prefix_tokens >= most)
+        return MOSAIC_BSA_ERR_PAGES;
+    const int kv_heads = p.kv_heads == 0 ? p.heads : p.kv_heads;
+    if (kv_heads > p.heads || p.heads % kv_heads ||
+        (int64_t)p.q_tokens * (p.heads / kv_heads) >= most || (int64_t)p.batch * kv_heads >= 1 << 22)
+        return MOSAIC_BSA_ERR_SHAPE;
+    return MOSAIC_BSA_OK;
+}
+
 }  // namespace bsa

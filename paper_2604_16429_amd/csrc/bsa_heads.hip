@@ -39,6 +39,12 @@ struct Segment {
     int32_t to_rows;          // y's rows are looked up
 };
 
+// Where new tokens of a cache in pages go, and which tokens there are: q_lens and k_lens by sequence.
+struct Pages {
+    const int32_t *q_lens, *k_lens, *table, *prefix_len;
+    int32_t pages, page_shift, table_pages, prefix_tokens;
+};
+
 struct Args {
     Segment seg[3];           // q, k, v (v: copied)
     const int32_t* positions;
@@ -50,6 +56,7 @@ struct Args {
     int32_t all_heads, head_chunk, chunks;
     float eps, magnitude, sin_magnitude;     // (the transpose turns the other way)
     uint64_t turns[MOSAIC_BSA_MAX_PAIRS];
+    Pages paged;
 };
 
 // V channels of a row, as they lie in memory (32-bit words; V = 1 in bf16: one in a word).
@@ -155,7 +162,9 @@ __device__ __forceinline__ float row_sum(float x, int P)
     return x;
 }
 
-template <typename T, int V, bool PAIRS, int MODE>
+// PAGED (kRotate, kNorm): a token is the q_lens[b] - n-th from the end of its sequence, which gives its
+// position, where none are given, and the page and row that keys and values go to.
+template <typename T, int V, bool PAIRS, int MODE, bool PAGED>
 __global__ __launch_bounds__(256, 3) void heads_kernel(const Args a, const int D, const int P)
 {
     constexpr int E = 2 * V;
@@ -192,9 +201,21 @@ __global__ __launch_bounds__(256, 3) void heads_kernel(const Args a, const int D
         const int head0 = (int)(item - group * a.chunks) * a.head_chunk;
         const int head1 = min(a.all_heads, head0 + a.head_chunk);
         const uint32_t tok = group * per_group + wave * per_wave + slot;
-        const bool here = active && tok < (uint32_t)a.all_tokens;
+        bool here = active && tok < (uint32_t)a.all_tokens;
         const uint32_t tk = tok < (uint32_t)a.all_tokens ? tok : 0u;
         const int b = (int)(tk / (uint32_t)a.tokens), n = (int)(tk - (uint32_t)b * a.tokens);
+        int place = 0, page = -1, prefix = 0;         // PAGED: index among the sequence's own tokens; its page
+        if constexpr (PAGED) {
+            const Pages& pg = a.paged;
+            const int ql = pg.q_lens ? min(max(pg.q_lens[b], 0), a.tokens) : a.tokens;
+            const int kl = min(max(pg.k_lens[b], 0), pg.table_pages << pg.page_shift);
+            if (pg.prefix_len) prefix = min(max(*pg.prefix_len, 0), pg.prefix_tokens);
+            else prefix = pg.prefix_tokens;
+            place = kl - ql + n;
+            here = here && n < ql;
+            if (here && place >= 0)
+                page = pg.table[(int64_t)b * pg.table_pages + (place >> pg.page_shift)];
+        }
 
         float cs[V], sn[V];
 #pragma unroll
@@ -202,7 +223,7 @@ __global__ __launch_bounds__(256, 3) void heads_kernel(const Args a, const int D
         if (rotated) {
             const int32_t pos = a.positions
                                     ? a.positions[(int64_t)b * a.position_batch + (int64_t)n * a.axes + axis]
-                                    : n;
+                                    : PAGED ? prefix + place : n;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const uint64_t turn = (uint64_t)(int64_t)pos * a.turns[pair0 + i];
@@ -221,13 +242,20 @@ __global__ __launch_bounds__(256, 3) void heads_kernel(const Args a, const int D
             const bool copy = si == 2;
             bool write = here;
             int64_t row = n;
-            if (sg.to_rows) {
+            int64_t block = b;
+            if constexpr (PAGED) {
+                if (si > 0) {
+                    row = place & ((1 << a.paged.page_shift) - 1);
+                    block = page;
+                    write = here && (uint32_t)page < (uint32_t)a.paged.pages;
+                }
+            } else if (sg.to_rows) {
                 row = a.rows[tk];
                 write = here && row >= 0 && row < a.cache_tokens;
             }
             const T* x = (const T*)sg.x + (int64_t)b * sg.xs.batch + (int64_t)n * sg.xs.token;
             const T* g = (const T*)sg.g + (int64_t)b * sg.gs.batch + (int64_t)n * sg.gs.token;
-            T* y = (T*)sg.y + (int64_t)b * sg.ys.batch + row * sg.ys.token;
+            T* y = (T*)sg.y + block * sg.ys.batch + row * sg.ys.token;
             float w[MODE >= kNorm ? E : 1];
             if constexpr (MODE >= kNorm) {
                 if (!copy) {
@@ -372,11 +400,18 @@ constexpr int kGradWorkgroups = 768;
 template <typename T, int V, bool PAIRS>
 hipError_t launch_mode(const Args& a, int mode, int D, int P, unsigned grid, hipStream_t stream)
 {
-    switch (mode) {
-    case kRotate: heads_kernel<T, V, PAIRS, kRotate><<<grid, 256, 0, stream>>>(a, D, P); break;
-    case kNorm: heads_kernel<T, V, PAIRS, kNorm><<<grid, 256, 0, stream>>>(a, D, P); break;
-    default: heads_kernel<T, V, PAIRS, kNormGrad><<<grid, 256, 0, stream>>>(a, D, P); break;
+#define BSA_HEADS(MODE, PAGED) heads_kernel<T, V, PAIRS, MODE, PAGED><<<grid, 256, 0, stream>>>(a, D, P)
+    if (a.paged.k_lens) {
+        if (mode == kRotate) BSA_HEADS(kRotate, true);
+        else BSA_HEADS(kNorm, true);
+    } else {
+        switch (mode) {
+        case kRotate: BSA_HEADS(kRotate, false); break;
+        case kNorm: BSA_HEADS(kNorm, false); break;
+        default: BSA_HEADS(kNormGrad, false); break;
+        }
     }
+#undef BSA_HEADS
     return hipGetLastError();
 }
 
@@ -625,6 +660,64 @@ extern "C" int mosaic_bsa_qk_norm_rope_fwd(const mosaic_bsa_heads_params* params
 {
     return forward(params, rotation, positions, q, k, v, q_weight, k_weight, rows, q_out, k_out,
                    v_out, true, (hipStream_t)hip_stream);
+}
+
+extern "C" int mosaic_bsa_paged_append(const mosaic_bsa_paged_params* params,
+                                       const mosaic_bsa_rotation* rotation,
+                                       const int32_t* positions, const void* q, const void* k,
+                                       const void* v, const float* q_weight, const float* k_weight,
+                                       const int32_t* q_lens, const int32_t* k_lens,
+                                       const int32_t* page_table, const int32_t* prefix_len,
+                                       void* q_out, void* k_pages, void* v_pages, void* hip_stream)
+{
+    if (!params) return MOSAIC_BSA_ERR_NULL;
+    const mosaic_bsa_paged_params& p = *params;
+    mosaic_bsa_heads_params h = {};
+    h.batch = p.batch;
+    h.tokens = p.q_tokens;
+    h.heads = p.heads;
+    h.kv_heads = p.kv_heads;
+    h.head_dim = p.head_dim;
+    h.dtype = p.dtype;
+    h.position_batch = p.position_batch;
+    h.norm_eps = p.norm_eps;
+    Checked c;
+    if (int rc = check_params(&h, &c)) return rc;
+    if (int rc = check_pages(p)) return rc;
+    if (int rc = check_rotation(rotation, c, positions)) return rc;
+    if (!q || !k || !v || !q_out || !k_pages || !v_pages || !k_lens || !page_table ||
+        !q_weight != !k_weight)
+        return MOSAIC_BSA_ERR_NULL;
+    const int64_t B = p.batch, N = p.q_tokens, T = p.page_tokens;
+    const int kv = c.kv_heads, D = c.D;
+    if (int rc = check_pair(q, q_out, true, p.q, p.out, B, p.heads, N, N, c)) return rc;
+    const struct { const void* x; const mosaic_bsa_strides* s; int64_t n, rows; bool output; } rest[] = {
+        {k, &p.k, B, N, false}, {v, &p.v, B, N, false},
+        {k_pages, &p.k_pages, p.pages, T, true}, {v_pages, &p.v_pages, p.pages, T, true}};
+    for (const auto& r : rest) {
+        if (unaligned(r.x, c.is_bf16 ? 2 : 4)) return MOSAIC_BSA_ERR_ALIGN;
+        if (bad_strides(*r.s, r.n, kv, r.rows, D, r.output) ||
+            (r.output && rows_meet(*r.s, r.n, kv, r.rows, D)))
+            return MOSAIC_BSA_ERR_STRIDE;
+    }
+    if (unaligned(positions, 4) || unaligned(q_weight, 4) || unaligned(k_weight, 4) ||
+        unaligned(q_lens, 4) || unaligned(k_lens, 4) || unaligned(page_table, 4) ||
+        unaligned(prefix_len, 4))
+        return MOSAIC_BSA_ERR_ALIGN;
+    Args a = {};
+    const mosaic_bsa_strides none = {0, 0, 0};
+    a.seg[0] = {q, nullptr, q_out, q_weight, strides_of(p.q, p.heads, N, D), none,
+                strides_of(p.out, p.heads, N, D), p.heads, 0};
+    a.seg[1] = {k, nullptr, k_pages, k_weight, strides_of(p.k, kv, N, D), none,
+                strides_of(p.k_pages, kv, T, D), kv, 0};
+    a.seg[2] = {v, nullptr, v_pages, nullptr, strides_of(p.v, kv, N, D), none,
+                strides_of(p.v_pages, kv, T, D), kv, 0};
+    a.positions = positions;
+    a.eps = p.norm_eps;
+    a.paged = {q_lens, k_lens, page_table, prefix_len, p.pages, __builtin_ctz((unsigned)p.page_tokens),
+               p.table_pages, p.prefix_tokens};
+    return launch(a, &h, c, rotation, q_weight ? kNorm : kRotate, false, kMostWorkgroups, nullptr,
+                  (hipStream_t)hip_stream);
 }
 
 extern "C" int mosaic_bsa_rope_bwd(const mosaic_bsa_heads_params* params,

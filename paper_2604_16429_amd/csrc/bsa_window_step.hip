@@ -14,45 +14,6 @@ namespace bsa {
 
 namespace win {
 
-// 16 x 16 products over 32 channels or keys: lane l holds 8 of them, from 8 (l / 16) on in the
-// order that both operands agree on, for row (column) l % 16.
-template <typename T> struct Mma16;
-template <> struct Mma16<uint16_t> {
-    static __device__ __forceinline__ f32x4 mul(bf16x8 a, bf16x8 b, f32x4 c)
-    {
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-    }
-    static __device__ __forceinline__ bf16x8 pack(const f32x4& x, const f32x4& y)
-    {
-        return __builtin_bit_cast(bf16x8, make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]),
-                                                     pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])));
-    }
-};
-template <> struct Mma16<float> {
-    static __device__ __forceinline__ f32x4 mul(f32x8 a, f32x8 b, f32x4 c)
-    {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
-        return c;
-    }
-    static __device__ __forceinline__ f32x8 pack(const f32x4& x, const f32x4& y)
-    {
-        return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
-    }
-};
-
-// Sum and maximum over the four lanes that hold one row.
-__device__ __forceinline__ float row_sum16(float x)
-{
-    x += __shfl_xor(x, 16);
-    return x + swap32(x);
-}
-__device__ __forceinline__ float row_max16(float x)
-{
-    x = fmaxf(x, __shfl_xor(x, 16));
-    return fmaxf(x, swap32(x));
-}
-
 // NR: 16-row tiles.  W: wavefronts.
 template <typename T, int D, int NR, int W>
 __global__ __launch_bounds__(64 * W) void window_step_kernel(
