@@ -507,7 +507,7 @@ int mosaic_bsa_window_bwd(const mosaic_bsa_window_params *params, const void *q,
  *
  * Sizes: with g = heads / kv_heads, prefix_tokens, table_pages x page_tokens and q_tokens x g below
  * 2^29, batch x kv_heads below 2^22, and (append) batch x q_tokens up to 2^30, (attention) fewer than
- * 2^23 tiles of 32 rows (q_tokens x g of each batch x kv_heads) in all.
+ * 2^21 tiles of 32 rows (q_tokens x g of each batch x kv_heads) in all.
  */
 typedef struct {
     int32_t batch, heads, kv_heads;    /* kv_heads: 0 = heads; divides heads */

@@ -19,19 +19,143 @@ using win::kLog2e;
 using win::kNoRef;
 using win::put4;
 
-// The same for all lanes, in scalar registers.
+template <typename T>
+struct Args {
+    const T *q, *k, *v;
+    T* out;
+    float* lse;
+    Shape s;
+    Plan plan;
+};
+
 __device__ __forceinline__ int prefix_of(const Shape& s)
 {
-    const int p = s.prefix_len ? min(max(*s.prefix_len, 0), s.prefix_tokens) : s.prefix_tokens;
-    return __builtin_amdgcn_readfirstlane(p);
+    return s.prefix_len ? min(max(*s.prefix_len, 0), s.prefix_tokens) : s.prefix_tokens;
 }
 __device__ __forceinline__ Sequence sequence(const Shape& s, int b)
 {
     Sequence q;
-    q.ql = __builtin_amdgcn_readfirstlane(s.q_lens ? min(max(s.q_lens[b], 0), s.q_tokens) : s.q_tokens);
-    q.kl = __builtin_amdgcn_readfirstlane(min(max(s.k_lens[b], 0), s.table_pages << s.page_shift));
+    q.ql = s.q_lens ? min(max(s.q_lens[b], 0), s.q_tokens) : s.q_tokens;
+    q.kl = min(max(s.k_lens[b], 0), s.table_pages << s.page_shift);
     q.prefix = prefix_of(s);
     return q;
+}
+// The same for all lanes, in scalar registers.
+__device__ __forceinline__ Sequence uniform(const Sequence& q)
+{
+    return Sequence{__builtin_amdgcn_readfirstlane(q.ql), __builtin_amdgcn_readfirstlane(q.kl),
+                    __builtin_amdgcn_readfirstlane(q.prefix)};
+}
+
+// The rows that a workgroup owns, from row0 on: of sequence b, or of all sequences one after the other.
+struct Rows {
+    int row0, n;
+    int a, b;                              // key/value head; sequence, or -1: all
+};
+struct Row {
+    int b, tok, head;
+    int place;                             // of its query; -1 - tokens: there is no such query
+    bool query;
+};
+// Row `r` of them (r < n); seq: of sequence b.
+__device__ __forceinline__ Row row_at(const Shape& s, const Rows& rows, const Sequence& seq, int r)
+{
+    Row x;
+    int row = rows.row0 + r;
+    Sequence own = seq;
+    x.b = rows.b;
+    if (rows.b < 0) {
+        x.b = row / s.rows;
+        row -= x.b * s.rows;
+        own = sequence(s, x.b);
+    }
+    x.tok = row / s.group;
+    x.head = rows.a * s.group + (row - x.tok * s.group);
+    x.query = x.tok < own.ql;
+    x.place = x.query ? own.prefix + own.kl - own.ql + x.tok : -1;
+    return x;
+}
+
+__device__ __forceinline__ int wave_sum(int x)
+{
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o);
+    return x;
+}
+// Sum over this lane and those before it.
+__device__ __forceinline__ int wave_scan(int x, int lane)
+{
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(x, o);
+        x += lane >= o ? y : 0;
+    }
+    return x;
+}
+
+// Chunk w of a call: sequence, its chunks and the first of them; b = -1: none.  All lanes of a wavefront
+// call it with the same w and get the same.
+struct Chunk {
+    int b, first, chunks;
+};
+template <class Hit>
+__device__ __forceinline__ Chunk scan_chunks(const Shape& s, const Plan& plan, int lane, Hit hit_of)
+{
+    int units[2] = {0, 0}, all = 0;                    // (of up to 128 sequences they are kept)
+    for (int base = 0; base < s.batch; base += 64) {
+        const int b = base + lane;
+        const int u = b < s.batch ? units_of(s, plan, sequence(s, b)) : 0;
+        if (base < 128) units[base >> 6] = u;
+        all += u;
+    }
+    const int per = chunk_units(s, plan, wave_sum(all));
+    int run = 0;
+    for (int base = 0; base < s.batch; base += 64) {
+        const int b = base + lane;
+        int n = 0;
+        if (b < s.batch)
+            n = chunks_of(plan, base == 0 ? units[0] : base == 64 ? units[1] : units_of(s, plan, sequence(s, b)), per);
+        const int end = run + wave_scan(n, lane), first = end - n;
+        const uint64_t hit = __builtin_amdgcn_ballot_w64(hit_of(b, first, end));
+        if (hit) {
+            const int l = __builtin_ctzll(hit);
+            return Chunk{base + l, __builtin_amdgcn_readlane(first, l), __builtin_amdgcn_readlane(n, l)};
+        }
+        run = __builtin_amdgcn_readlane(end, 63);
+    }
+    return Chunk{-1, 0, 0};
+}
+__device__ __forceinline__ Chunk chunk_at(const Shape& s, const Plan& plan, int w, int lane)
+{
+    if (!plan.scanned) return Chunk{w, w, 1};
+    return scan_chunks(s, plan, lane, [&](int, int first, int end) { return w >= first && w < end; });
+}
+// The chunks of sequence b.
+__device__ __forceinline__ Chunk chunks_at(const Shape& s, const Plan& plan, int b, int lane)
+{
+    if (!plan.scanned) return Chunk{b, b, 1};
+    return scan_chunks(s, plan, lane, [&](int x, int, int) { return x == b; });
+}
+
+// Four channels of a row's sum against reference `top`: the result, or a part of it.
+template <typename T, int D>
+__device__ __forceinline__ void store_row(const Args<T>& g, const Row& x, int c, const f32x4& sum, float top, float l)
+{
+    const Shape& s = g.s;
+    const bool none = !x.query || l == 0.0f;
+    const float f = 1.0f / l;
+    put4(g.out + (int64_t)x.b * s.out.batch + (int64_t)x.head * s.out.head + (int64_t)x.tok * s.out.token + c,
+         none ? 0.0f : sum[0] * f, none ? 0.0f : sum[1] * f, none ? 0.0f : sum[2] * f,
+         none ? 0.0f : sum[3] * f);
+    if (g.lse && c == 0)
+        g.lse[((int64_t)x.b * s.heads + x.head) * s.q_tokens + x.tok] =
+            none ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * kLn2;
+}
+template <int D>
+__device__ __forceinline__ void store_part(const Plan& plan, int64_t part, int c, const f32x4& sum, float top, float l)
+{
+    *(f32x4*)(plan.acc + part * D + c) = sum;
+    if (c == 0) plan.ml[part] = make_float2(top, l);
 }
 
 }  // namespace paged

@@ -38,8 +38,8 @@ int check_params(const mosaic_bsa_paged_params* p, Checked* c)
                                                                            : p->window_left;
     s.sinks = p->n_sink;
     s.scale = p->softmax_scale > 0.0f ? p->softmax_scale : 1.0f / sqrtf((float)p->head_dim);
-    // launches of at most 2^23 workgroups
-    if ((int64_t)s.batch * s.kv_heads * ((s.rows + 31) / 32) >= 1 << 23) return MOSAIC_BSA_ERR_SHAPE;
+    // launches of less than 2^32 work items: 256 to a tile and, where sums are joined, to 8 rows
+    if ((int64_t)s.batch * s.kv_heads * ((s.rows + 31) / 32) >= 1 << 21) return MOSAIC_BSA_ERR_SHAPE;
     return MOSAIC_BSA_OK;
 }
 

@@ -36,6 +36,32 @@ extern "C" int walk_of(int kt, int prefix, int ql, int kl, int left, int sinks, 
     return kt == 32 ? walk<32>(prefix, ql, kl, left, sinks, first, last, out)
                     : walk<64>(prefix, ql, kl, left, sinks, first, last, out);
 }
+// what: 0 batch, rows, kv_heads, own, prefix (a power of two of pages), left, q_tokens -> chunks, scanned, stacked,
+// splits, parts, least; then the chunks of every sequence of the given lengths
+extern "C" int64_t plan_of(const int32_t* shape, const int32_t* lens, int32_t* out, int32_t* chunks)
+{
+    Shape s = {};
+    s.batch = shape[0];
+    s.group = shape[1];
+    s.q_tokens = shape[2];
+    s.rows = s.group * s.q_tokens;
+    s.kv_heads = shape[3];
+    s.table_pages = shape[4];
+    s.prefix_tokens = shape[5];
+    s.left = shape[6];
+    s.sinks = shape[7];
+    const Plan p = make_plan(s);
+    const int32_t v[] = {p.chunks, p.scanned, p.stacked, p.shared_splits, p.parts, p.least, p.all_rows};
+    for (int i = 0; i < 7; ++i) out[i] = v[i];
+    if (p.scanned) {
+        int all = 0;
+        for (int b = 0; b < s.batch; ++b) all += units_of(s, p, Sequence{lens[3 * b], lens[3 * b + 1], lens[3 * b + 2]});
+        const int per = chunk_units(s, p, all);
+        for (int b = 0; b < s.batch; ++b)
+            chunks[b] = chunks_of(p, units_of(s, p, Sequence{lens[3 * b], lens[3 * b + 1], lens[3 * b + 2]}), per);
+    }
+    return p.all_parts(s);
+}
 extern "C" int page(int pages, int shift, const int32_t* table, int at, int count)
 {
     Shape s = {};
@@ -58,6 +84,37 @@ def plan(tmp_path_factory):
 
 
 UNBOUNDED = 1 << 30
+
+
+def test_chunks_fit(plan):
+    """Whatever the lengths, all chunks have a place, and each sequence that needs one has one."""
+    plan.plan_of.restype = ctypes.c_int64
+    rng = random.Random(0)
+    seen = {"scanned": 0, "stacked": 0}
+    for _ in range(3000):
+        B, q_tokens = rng.choice([1, 2, 7, 64, 300, 1024, 1500]), rng.choice([1, 1, 1, 5, 40, 1000])
+        shape = [B, rng.choice([1, 2, 4, 8, 16]), q_tokens, rng.choice([1, 2, 8]),
+                 rng.choice([1, 100, 1000, 30000, 1 << 20, (1 << 29) - 1]), rng.choice([0, 0, 300, 20000, (1 << 29) - 1]),
+                 rng.choice([UNBOUNDED, UNBOUNDED, 1000]), rng.choice([0, 4])]
+        own, prefix = shape[4], shape[5]
+        lens = np.array([[rng.choice([0, 1, q_tokens]), rng.choice([0, 1, own, rng.randint(0, own)]), prefix]
+                         for _ in range(B)], dtype=np.int32)
+        out, chunks = np.zeros(7, np.int32), np.zeros(B, np.int32)
+        n = plan.plan_of(np.array(shape, np.int32).ctypes.data_as(ctypes.c_void_p),
+                         lens.ctypes.data_as(ctypes.c_void_p), out.ctypes.data_as(ctypes.c_void_p),
+                         chunks.ctypes.data_as(ctypes.c_void_p))
+        total, scanned, stacked, splits, parts, least, all_rows = out.tolist()
+        rows = shape[1] * q_tokens
+        assert total >= B and least >= 1 and parts == (stacked or scanned)
+        assert n == shape[3] * (total * rows + splits * all_rows) and n < 1 << 40
+        assert all_rows == (B * rows if stacked else 1) and (splits >= 1) == bool(stacked)
+        if scanned:
+            assert total > B and int(chunks.sum()) <= total and int(chunks.min()) >= (0 if stacked else 1)
+        else:
+            assert total == B
+        seen["scanned"] += scanned
+        seen["stacked"] += stacked
+    assert min(seen.values()) > 100
 
 
 @pytest.mark.parametrize("seed", range(8))
