@@ -76,65 +76,63 @@ __device__ __forceinline__ Row row_at(const Shape& s, const Rows& rows, const Se
     return x;
 }
 
-__device__ __forceinline__ int wave_sum(int x)
+// Sum over this lane and those before it, by data-parallel moves: within 16 lanes, then the last of each 16
+// (32) lanes into those behind.
+__device__ __forceinline__ int wave_scan(int x)
 {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o);
-    return x;
-}
-// Sum over this lane and those before it.
-__device__ __forceinline__ int wave_scan(int x, int lane)
-{
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int y = __shfl_up(x, o);
-        x += lane >= o ? y : 0;
-    }
+#define BSA_SCAN_STEP(CTRL, ROWS) x += __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false)
+    BSA_SCAN_STEP(0x111, 0xf);
+    BSA_SCAN_STEP(0x112, 0xf);
+    BSA_SCAN_STEP(0x114, 0xf);
+    BSA_SCAN_STEP(0x118, 0xf);
+    BSA_SCAN_STEP(0x142, 0xa);
+    BSA_SCAN_STEP(0x143, 0xc);
+#undef BSA_SCAN_STEP
     return x;
 }
 
-// Chunk w of a call: sequence, its chunks and the first of them; b = -1: none.  All lanes of a wavefront
-// call it with the same w and get the same.
+// Chunk w of a call: its entry, the entry's chunks and the first of them; entry -1: none.  All lanes of a
+// wavefront call it with the same w and get the same.  record: entries are written down for the joining.
 struct Chunk {
-    int b, first, chunks;
+    int entry, first, chunks;
 };
-template <class Hit>
-__device__ __forceinline__ Chunk scan_chunks(const Shape& s, const Plan& plan, int lane, Hit hit_of)
+__device__ __forceinline__ Chunk chunk_at(const Shape& s, const Plan& plan, int w, int lane, bool record)
 {
-    int units[2] = {0, 0}, all = 0;                    // (of up to 128 sequences they are kept)
-    for (int base = 0; base < s.batch; base += 64) {
-        const int b = base + lane;
-        const int u = b < s.batch ? units_of(s, plan, sequence(s, b)) : 0;
-        if (base < 128) units[base >> 6] = u;
+    const auto units = [&](int e) -> int {
+        return e < plan.entries ? units_of(s, plan, sequence(s, plan.sequence_of(s, e)), plan.tile_of(s, e)) : 0;
+    };
+    if (!plan.scanned) {
+        const int n = plan.stacked ? min(__builtin_amdgcn_readfirstlane(units(w)), 1) : 1;
+        if (record && lane == 0) plan.found[w] = Entry{w, n};
+        return Chunk{n > 0 ? w : -1, w, 1};
+    }
+    int kept[2] = {0, 0}, all = 0;                     // units of up to 128 entries
+    for (int base = 0; base < plan.entries; base += 64) {
+        const int u = units(base + lane);
+        if (base < 128) kept[base >> 6] = u;
         all += u;
     }
-    const int per = chunk_units(s, plan, wave_sum(all));
+    const auto sum = [&](int x) { return __builtin_amdgcn_readlane(wave_scan(x), 63); };
+    const auto chunks = [&](int e, int u, int per) { return e < plan.entries ? chunks_of(plan, u, per) : 0; };
+    const int per = chunk_units(plan, sum(all), plan.entries <= 128, [&](int c) {
+        return sum(chunks(lane, kept[0], c) + chunks(lane + 64, kept[1], c));
+    });
+    Chunk found = {-1, 0, 0};
     int run = 0;
-    for (int base = 0; base < s.batch; base += 64) {
-        const int b = base + lane;
-        int n = 0;
-        if (b < s.batch)
-            n = chunks_of(plan, base == 0 ? units[0] : base == 64 ? units[1] : units_of(s, plan, sequence(s, b)), per);
-        const int end = run + wave_scan(n, lane), first = end - n;
-        const uint64_t hit = __builtin_amdgcn_ballot_w64(hit_of(b, first, end));
+    for (int base = 0; base < plan.entries; base += 64) {
+        const int e = base + lane;
+        const int n = chunks(e, base == 0 ? kept[0] : base == 64 ? kept[1] : units(e), per);
+        const int end = run + wave_scan(n), first = end - n;
+        const uint64_t hit = __builtin_amdgcn_ballot_w64(w >= first && w < end);
+        if (record && e < plan.entries) plan.found[e] = Entry{first, n};
         if (hit) {
             const int l = __builtin_ctzll(hit);
-            return Chunk{base + l, __builtin_amdgcn_readlane(first, l), __builtin_amdgcn_readlane(n, l)};
+            found = Chunk{base + l, __builtin_amdgcn_readlane(first, l), __builtin_amdgcn_readlane(n, l)};
+            if (!record) break;
         }
         run = __builtin_amdgcn_readlane(end, 63);
     }
-    return Chunk{-1, 0, 0};
-}
-__device__ __forceinline__ Chunk chunk_at(const Shape& s, const Plan& plan, int w, int lane)
-{
-    if (!plan.scanned) return Chunk{w, w, 1};
-    return scan_chunks(s, plan, lane, [&](int, int first, int end) { return w >= first && w < end; });
-}
-// The chunks of sequence b.
-__device__ __forceinline__ Chunk chunks_at(const Shape& s, const Plan& plan, int b, int lane)
-{
-    if (!plan.scanned) return Chunk{b, b, 1};
-    return scan_chunks(s, plan, lane, [&](int x, int, int) { return x == b; });
+    return found;
 }
 
 // Four channels of a row's sum against reference `top`: the result, or a part of it.

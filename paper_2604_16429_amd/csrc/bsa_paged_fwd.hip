@@ -1,6 +1,7 @@
 // Attention over a cache in pages: launches.  Which rows and tokens a workgroup takes is in
 // bsa_paged_plan.h.
 #include "bsa_paged_step.h"
+#include "bsa_paged_tile.h"
 
 namespace bsa {
 
@@ -8,12 +9,29 @@ namespace paged {
 
 constexpr int most_of(int a, int b) { return a > b ? a : b; }
 
-// OWN, SHARED: 16-row tiles of a workgroup that takes a sequence's rows, and the rows of all (0: none do).
-template <typename T, int D, int OWN, int SHARED, int W>
-__global__ __launch_bounds__(64 * W) void paged_kernel(const Args<T> g, uint32_t shared_items)
+// What works on tiles of ROWS rows.
+template <typename T, int D, int ROWS, int W, bool ONE>
+struct WalkOf {
+    using Type = Step<T, D, ROWS / 16, W>;
+};
+template <int D, int W, bool ONE>
+struct WalkOf<uint16_t, D, 128, W, ONE> {
+    using Type = WideTile<D, ONE>;
+};
+// Workgroups that a CU is to hold: as many as the registers of each kernel allow.
+template <typename T, int D, int ROWS, int W>
+constexpr int held_by_cu()
 {
-    using Own = Step<T, D, OWN, W>;
-    using Shared = Step<T, D, most_of(SHARED, 1), W>;
+    return W > 4 || sizeof(T) == 4 ? 1 : ROWS == 128 && D == 64 ? 3 : 2;
+}
+
+// OWN, SHARED: rows of a workgroup that takes a sequence's, and of one that takes those of all (0: none does).
+template <typename T, int D, int OWN, int SHARED, int W, bool ONE = false>
+__global__ __launch_bounds__(64 * W, (held_by_cu<T, D, most_of(OWN, SHARED), W>())) void paged_kernel(
+    const Args<T> g, uint32_t shared_items)
+{
+    using Own = typename WalkOf<T, D, OWN, W, ONE>::Type;
+    using Shared = typename WalkOf<T, D, SHARED ? SHARED : 16, W, ONE>::Type;
     __shared__ __attribute__((aligned(1024))) unsigned char
         lds[SHARED ? most_of(Own::LDS_BYTES, Shared::LDS_BYTES) : Own::LDS_BYTES];
     const Shape& s = g.s;
@@ -21,135 +39,148 @@ __global__ __launch_bounds__(64 * W) void paged_kernel(const Args<T> g, uint32_t
     const int lane = threadIdx.x & 63;
 
     if (SHARED && blockIdx.x < shared_items) {
-        const uint32_t rest = blockIdx.x / (uint32_t)plan.shared_splits;
-        const int split = (int)(blockIdx.x - rest * (uint32_t)plan.shared_splits);
+        const uint32_t item = blockIdx.x, rest = item / (uint32_t)plan.shared_splits;
+        const int split = (int)(item - rest * (uint32_t)plan.shared_splits);
         const int tile = (int)(rest / (uint32_t)s.kv_heads);
         Rows rows;
         rows.a = (int)(rest - (uint32_t)tile * s.kv_heads);
         rows.b = -1;
-        rows.row0 = tile * 16 * SHARED;
-        rows.n = min(16 * SHARED, plan.all_rows - rows.row0);
+        rows.row0 = tile * SHARED;
+        rows.n = min(SHARED, plan.all_rows - rows.row0);
         Sequence seq = {0, 0, 0};
         seq.prefix = __builtin_amdgcn_readfirstlane(prefix_of(s));
-        const Tiles<32> tiles(s, seq, 0, seq.prefix - 1, kShared);
-        const Row x = row_at(s, rows, seq, min(lane, rows.n - 1));
-        int first = x.query ? x.place : 1 << 30;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) first = min(first, __shfl_xor(first, o));
+        const Tiles<Shared::KT> tiles(s, seq, 0, seq.prefix - 1, kShared);
         const int per = (tiles.count + plan.shared_splits - 1) / plan.shared_splits;
         const int t_a = min(split * per, tiles.count);
-        Shared::walk(lds, g, rows, seq, tiles, t_a, min(t_a + per, tiles.count), first, 0,
-                     [&](int r, int c, const f32x4& sum, float top, float l) {
-                         store_part<D>(plan, plan.shared_part(s, rows.a, split, rows.row0 + r), c, sum, top, l);
-                     });
+        Shared::walk(lds, g, rows, seq, tiles, t_a, min(t_a + per, tiles.count),
+                     plan.shared_part(s, rows.a, split, rows.row0));
         return;
     }
-    const uint32_t item = blockIdx.x - (SHARED ? shared_items : 0u), rest = item / (uint32_t)plan.chunks;
-    const int w = (int)(item - rest * (uint32_t)plan.chunks);
-    const int tile = (int)(rest / (uint32_t)s.kv_heads);
-    const Chunk chunk = chunk_at(s, plan, w, lane);
-    if (chunk.b < 0) return;
+    const uint32_t item = blockIdx.x - (SHARED ? shared_items : 0u);
+    const int w = (int)(item / (uint32_t)s.kv_heads);
     Rows rows;
-    rows.a = (int)(rest - (uint32_t)tile * s.kv_heads);
-    rows.b = chunk.b;
-    rows.row0 = tile * 16 * OWN;
-    rows.n = min(16 * OWN, s.rows - rows.row0);
-    const Sequence seq = uniform(sequence(s, chunk.b));
-    const int p0 = seq.prefix + seq.kl - seq.ql;
-    const int first = p0 + rows.row0 / s.group;
-    const int last = p0 + min((rows.row0 + rows.n - 1) / s.group, seq.ql - 1);
-    const Tiles<32> tiles(s, seq, first, last, SHARED ? kOwn : kAll);
+    rows.a = (int)(item - (uint32_t)w * s.kv_heads);
+    Chunk chunk = chunk_at(s, plan, w, lane,
+                           plan.parts && rows.a == 0 && (w == 0 || !plan.scanned) && threadIdx.x < 64);
+    chunk.entry = __builtin_amdgcn_readfirstlane(chunk.entry);
+    chunk.first = __builtin_amdgcn_readfirstlane(chunk.first);
+    chunk.chunks = __builtin_amdgcn_readfirstlane(chunk.chunks);
+    if (chunk.entry < 0) return;
+    rows.b = plan.sequence_of(s, chunk.entry);
+    const int tile = plan.tile_of(s, chunk.entry);
+    rows.row0 = tile * OWN;
+    rows.n = min(OWN, s.rows - rows.row0);
+    const Sequence seq = uniform(sequence(s, rows.b));
+    const auto tiles = tiles_of<Own::KT>(s, plan, seq, tile);
     const int per = (tiles.count + chunk.chunks - 1) / chunk.chunks;
     const int t_a = min((w - chunk.first) * per, tiles.count);
     const bool direct = !SHARED && chunk.chunks == 1;
-    Own::walk(lds, g, rows, seq, tiles, t_a, min(t_a + per, tiles.count), first, last,
-              [&](int r, int c, const f32x4& sum, float top, float l) {
-                  if (direct) store_row<T, D>(g, row_at(s, rows, seq, r), c, sum, top, l);
-                  else store_part<D>(plan, plan.own_part(s, rows.a, w, rows.row0 + r), c, sum, top, l);
-              });
+    Own::walk(lds, g, rows, seq, tiles, t_a, min(t_a + per, tiles.count), direct ? -1 : plan.own_part(rows.a, w));
 }
 
-// The parts of a row in their order, the prefix's first: out = sum 2^(m - M) acc / sum 2^(m - M) l.  A
+// The parts of a row, each group's in their order, the prefix's first: out = sum 2^(m - M) acc / sum 2^(m - M) l.  A
 // workgroup has rows of one sequence; D / 4 lanes have a row, PG groups of them take its parts in turn.
 template <typename T, int D, int PG>
 __global__ __launch_bounds__(256) void paged_join_kernel(const Args<T> g, uint32_t row_groups)
 {
     constexpr int LANES = D / 4, PER = 256 / (LANES * PG);     // rows of a workgroup
     __shared__ f32x4 sum_s[PG][PER * LANES];
-    __shared__ float l_s[PG][PER * LANES];
+    __shared__ float2 ml_s[PG][PER * LANES];
     const Shape& s = g.s;
     const Plan& plan = g.plan;
-    const int b = (int)(blockIdx.x / row_groups), tid = threadIdx.x, lane = tid & 63;
+    const int b = (int)(blockIdx.x / row_groups), tid = threadIdx.x;
     const int at = tid % LANES, slot = tid / LANES % PER, pg = tid / (LANES * PER);
-    Chunk chunk = chunks_at(s, plan, b, lane);
-    if (!plan.stacked && chunk.chunks == 1) return;            // stored by its workgroup
-    const int slice_row = (int)(blockIdx.x % row_groups) * PER + slot;     // (key/value head, row)
-    const bool there = slice_row < s.kv_heads * s.rows;
-    const int a = there ? slice_row / s.rows : 0, row = there ? slice_row - a * s.rows : 0;
+    const int slice_row = (int)(blockIdx.x - (uint32_t)b * row_groups) * PER + slot;     // (key/value head, row)
+    const int a = min(slice_row / s.rows, s.kv_heads - 1), row = slice_row - a * s.rows;
+    const int tile = min(row, s.rows - 1) / plan.tile;
+    const Row x = row_at(s, Rows{row, 1, a, b}, sequence(s, b), 0);
+    const Entry entry = plan.found[plan.entry_of(s, b, tile)];
+    // (one chunk and nothing else: stored by its workgroup)
+    const bool there = row < s.rows && (plan.stacked || entry.chunks != 1);
     const int shared = plan.stacked ? plan.shared_splits : 0;
-    if (plan.stacked && !plan.scanned) {                       // (a sequence may have nothing of its own)
-        const Sequence seq = uniform(sequence(s, b));
-        if (units_of(s, plan, seq) == 0) chunk.chunks = 0;
-    }
-    const int parts = shared + chunk.chunks;
+    const int parts = there ? shared + entry.chunks : 0;
+    const int64_t shared0 = plan.shared_part(s, a, 0, b * s.rows + row);
+    const int64_t own0 = plan.own_part(a, entry.first) + row - tile * plan.tile;
     auto part = [&](int i) -> int64_t {
-        return i < shared ? plan.shared_part(s, a, i, b * s.rows + row)
-                          : plan.own_part(s, a, chunk.first + i - shared, row);
+        return i < shared ? shared0 + (int64_t)i * plan.all_rows : own0 + (int64_t)(i - shared) * plan.tile_rows;
     };
-    float top = kNoRef;
-    for (int i = at; i < parts; i += LANES) top = fmaxf(top, plan.ml[part(i)].x);
-#pragma unroll
-    for (int o = 1; o < LANES; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+    float top = kNoRef, l = 0.0f;
     f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-    float l = 0.0f;
-#pragma unroll 4
-    for (int i = pg; i < parts; i += PG) {
-        const int64_t x = part(i);
-        const float2 ml = plan.ml[x];
-        const float f = __builtin_amdgcn_exp2f(ml.x - top);
-        const f32x4 v = *(const f32x4*)(plan.acc + x * D + 4 * at);
-        l = fmaf(f, ml.y, l);
+    const auto add = [&](float m, float l_part, const f32x4& v) {
+        const float most = fmaxf(top, m);
+        const float f0 = __builtin_amdgcn_exp2f(top - most), f = __builtin_amdgcn_exp2f(m - most);
+        top = most;
+        l = fmaf(f, l_part, l * f0);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum[e] = fmaf(f, v[e], sum[e]);
+        for (int e = 0; e < 4; ++e) sum[e] = fmaf(f, v[e], sum[e] * f0);
+    };
+    constexpr int AHEAD = 8;                           // parts asked for at once
+    for (int i0 = pg; i0 < parts; i0 += PG * AHEAD) {
+        float2 ml[AHEAD];
+        f32x4 v[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int64_t x = part(min(i0 + PG * u, parts - 1));
+            ml[u] = plan.ml[x];
+            v[u] = *(const f32x4*)(plan.acc + x * D + 4 * at);
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+            if (i0 + PG * u < parts) add(ml[u].x, ml[u].y, v[u]);
     }
     if constexpr (PG > 1) {
         sum_s[pg][slot * LANES + at] = sum;
-        l_s[pg][slot * LANES + at] = l;
+        ml_s[pg][slot * LANES + at] = make_float2(top, l);
         __syncthreads();
         if (pg > 0) return;
 #pragma unroll
         for (int i = 1; i < PG; ++i) {
-            sum += sum_s[i][slot * LANES + at];
-            l += l_s[i][slot * LANES + at];
+            const float2 ml = ml_s[i][slot * LANES + at];
+            add(ml.x, ml.y, sum_s[i][slot * LANES + at]);
         }
     }
     if (!there) return;
-    const Sequence seq = uniform(sequence(s, b));
-    store_row<T, D>(g, row_at(s, Rows{row, 1, a, b}, seq, 0), 4 * at, sum, top, l);
+    store_row<T, D>(g, x, 4 * at, sum, top, l);
 }
 
 template <typename T, int D>
 hipError_t launch(const Shape& s, const void* q, const void* k, const void* v, void* out, float* lse,
                   void* workspace, hipStream_t stream)
 {
-    Args<T> g = {(const T*)q, (const T*)k, (const T*)v, (T*)out, lse, s, make_plan(s)};
+    Kind kind = kind_of(sizeof(T) == 2, D, s);
+    kind.wide = kind.wide && strides_fit(s);
+    Args<T> g = {(const T*)q, (const T*)k, (const T*)v, (T*)out, lse, s, make_plan(s, D, kind)};
     Plan& plan = g.plan;
     if (plan.parts) {
+        const int64_t n = plan.all_parts(s);
         plan.acc = (float*)workspace;
-        plan.ml = (float2*)(plan.acc + plan.all_parts(s) * D);
+        plan.ml = (float2*)(plan.acc + n * D);
+        plan.found = (Entry*)(plan.ml + n);
     }
-    const int own = tile_rows(s.rows) / 16, shared = plan.stacked ? tile_rows(plan.all_rows) / 16 : 0;
-    const uint32_t own_items = (uint32_t)plan.chunks * s.kv_heads * ((s.rows + 16 * own - 1) / (16 * own));
+    const int own = plan.tile, shared = plan.shared_tile;
+    const uint32_t own_items = (uint32_t)plan.chunks * s.kv_heads;
     const uint32_t shared_items =
-        shared ? (uint32_t)plan.shared_splits * s.kv_heads * ((plan.all_rows + 16 * shared - 1) / (16 * shared)) : 0u;
-    auto kernel = shared == 0   ? own == 1 ? paged_kernel<T, D, 1, 0, 4> : paged_kernel<T, D, 2, 0, 4>
-                  : shared == 1 ? paged_kernel<T, D, 1, 1, 4>
-                  : own == 1    ? paged_kernel<T, D, 1, 2, 4>
-                                : paged_kernel<T, D, 2, 2, 4>;
-    kernel<<<own_items + shared_items, 256, 0, stream>>>(g, shared_items);
+        shared ? (uint32_t)plan.shared_splits * s.kv_heads * ((plan.all_rows + shared - 1) / shared) : 0u;
+    constexpr int WAVES = win::step_waves(sizeof(T), D);
+    void (*kernel)(const Args<T>, uint32_t) = nullptr;
+    if (plan.waves > 4) kernel = paged_kernel<T, D, 16, 0, WAVES>;
+    else if (shared == 0) kernel = own == 16 ? paged_kernel<T, D, 16, 0, 4> : paged_kernel<T, D, 32, 0, 4>;
+    else if (shared == 16) kernel = paged_kernel<T, D, 16, 16, 4>;
+    else kernel = own == 16 ? paged_kernel<T, D, 16, 32, 4> : paged_kernel<T, D, 32, 32, 4>;
+    if constexpr (sizeof(T) == 2 && D >= 64) {
+        const bool one = s.page_shift >= 6;
+#define BSA_PAGED_WIDE(OWN, SHARED) (one ? paged_kernel<T, D, OWN, SHARED, 4, true> : paged_kernel<T, D, OWN, SHARED, 4>)
+        if (shared == 0 && own == 128) kernel = BSA_PAGED_WIDE(128, 0);
+        if (shared == 128)
+            kernel = own == 16   ? BSA_PAGED_WIDE(16, 128)
+                     : own == 32 ? BSA_PAGED_WIDE(32, 128)
+                                 : BSA_PAGED_WIDE(128, 128);
+#undef BSA_PAGED_WIDE
+    }
+    kernel<<<own_items + shared_items, 64 * plan.waves, 0, stream>>>(g, shared_items);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !plan.parts) return e;
-    const bool many = plan.shared_splits + plan.chunks / s.batch > 8;
+    const bool many = plan.shared_splits + plan.chunks / plan.entries > 8;
     const int per = many ? 256 / (D / 4 * 8) : 256 / (D / 4);
     const uint32_t row_groups = (uint32_t)((s.kv_heads * s.rows + per - 1) / per);
     auto join = many ? paged_join_kernel<T, D, 8> : paged_join_kernel<T, D, 1>;
@@ -161,8 +192,16 @@ hipError_t launch(const Shape& s, const void* q, const void* k, const void* v, v
 
 size_t paged_fwd_workspace(bool is_bf16, int D, const paged::Shape& s)
 {
-    const paged::Plan p = paged::make_plan(s);
-    return p.parts ? (size_t)p.all_parts(s) * (D + 2) * sizeof(float) : 0;
+    using namespace paged;
+    // (which kernels run depends on strides as well: enough for both)
+    Kind kind = kind_of(is_bf16, D, s);
+    size_t most = 0;
+    for (int i = 0; i < 2; ++i, kind.wide = false) {
+        const Plan p = make_plan(s, D, kind);
+        const size_t n = p.parts ? (size_t)p.all_parts(s) * (D + 2) * sizeof(float) + p.entries * sizeof(Entry) : 0;
+        if (n > most) most = n;
+    }
+    return most;
 }
 
 hipError_t launch_paged_fwd(bool is_bf16, int D, const paged::Shape& s, const void* q, const void* k,

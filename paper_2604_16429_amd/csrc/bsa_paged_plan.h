@@ -82,59 +82,98 @@ struct Tiles {
     }
 };
 
-// How a call is dealt out.  Tokens of few rows are split over workgroups, whose sums a second launch joins.
+// How a call is dealt out.  Workgroups own tiles of a sequence's rows ("entries", all sequences' last tiles
+// first: they see most) and walk the tokens that these see; few rows see many tokens, which are then
+// split over workgroups, whose sums a second launch joins.
 //
 // The prefix's part of rows that are too few to fill a tile by themselves is worked on for the rows of all
 // sequences together ("stacked"), in `shared_splits` shares of its tokens; without that the prefix
-// is the beginning of every sequence.  What is left of a sequence, u units of 128 tokens, is cut into
+// is the beginning of every sequence.  What is left of an entry, u units of 128 tokens, is cut into
 // max(1, ceil(u / c)) chunks (stacked: maybe none), c the same for all and large enough that there are
-// at most `chunks` of them, and at least `least`: with U the sum of all u, c = max(least, ceil(U / (chunks -
-// batch))).  Lengths are in device memory: workgroups find their chunk by a sum over the batch.
-constexpr int kUnit = 128;
-constexpr int kMostScanned = 1024;         // sequences; a larger batch has a chunk for each
+// at most `chunks` of them.  Lengths are in device memory: workgroups find c and their chunk by sums over
+// the entries.
+constexpr int kUnit = 128, kLeast = 2;     // c is kLeast at least
+constexpr int kMostScanned = 2048;         // entries; more have a chunk each
+struct Entry {
+    int32_t first, chunks;
+};
 struct Plan {
     bool stacked, parts;                   // parts: there may be several sums of one row
-    bool scanned;                          // chunks are looked up; else chunk i is sequence i
-    int32_t chunks, least, shared_splits;
-    int32_t all_rows;                      // batch x rows
-    float* acc;                            // sums of weight x value against a reference: [kv_heads][chunks][rows][D],
+    bool scanned;                          // chunks are looked up; else chunk i is entry i
+    int32_t waves;                         // of a workgroup
+    int32_t tile, tile_rows;               // rows of a workgroup at most, and those that there are
+    int32_t row_tiles, entries, chunks;
+    int32_t shared_tile, shared_splits, all_rows;      // all_rows = batch x rows
+    float* acc;                            // sums of weight x value against a reference: [kv_heads][chunks][tile_rows][D],
     float2* ml;                            // then [kv_heads][shared_splits][all_rows][D]; (reference in base 2, sum
                                            // of weights) likewise
-    // index of a row's sums
-    __host__ __device__ inline int64_t own_part(const Shape& s, int a, int chunk, int row) const
+    Entry* found;                          // [entries]: what the first launch found, for the second
+    // index of the sums of a chunk's first row
+    __host__ __device__ inline int64_t own_part(int a, int chunk) const
     {
-        return ((int64_t)a * chunks + chunk) * s.rows + row;
+        return ((int64_t)a * chunks + chunk) * tile_rows;
     }
     __host__ __device__ inline int64_t shared_part(const Shape& s, int a, int split, int row) const
     {
-        return (int64_t)s.kv_heads * chunks * s.rows +
-               ((int64_t)a * shared_splits + split) * all_rows + row;
+        return (int64_t)s.kv_heads * chunks * tile_rows + ((int64_t)a * shared_splits + split) * all_rows + row;
     }
     __host__ __device__ inline int64_t all_parts(const Shape& s) const
     {
-        return (int64_t)s.kv_heads * ((int64_t)chunks * s.rows + (int64_t)shared_splits * all_rows);
+        return (int64_t)s.kv_heads * ((int64_t)chunks * tile_rows + (int64_t)shared_splits * all_rows);
+    }
+    __host__ __device__ inline int sequence_of(const Shape& s, int entry) const { return entry % s.batch; }
+    __host__ __device__ inline int tile_of(const Shape& s, int entry) const { return row_tiles - 1 - entry / s.batch; }
+    __host__ __device__ inline int entry_of(const Shape& s, int b, int tile_at) const
+    {
+        return (row_tiles - 1 - tile_at) * s.batch + b;
     }
 };
-// Units of a sequence and the chunks that they make.
-__host__ __device__ inline int units_of(const Shape& s, const Plan& plan, const Sequence& q)
+// The tokens that an entry's chunks hold.
+template <int KT>
+__host__ __device__ inline Tiles<KT> tiles_of(const Shape& s, const Plan& plan, const Sequence& q, int tile_at)
 {
+    const int row0 = tile_at * plan.tile, end = row0 + plan.tile < s.rows ? row0 + plan.tile : s.rows;
+    const int last = (end - 1) / s.group < q.ql - 1 ? (end - 1) / s.group : q.ql - 1;
     const int p0 = q.prefix + q.kl - q.ql;
-    const Tiles<32> tiles(s, q, p0, p0 + q.ql - 1, plan.stacked ? kOwn : kAll);
-    return (tiles.count + kUnit / 32 - 1) / (kUnit / 32);
+    return Tiles<KT>(s, q, p0 + row0 / s.group, p0 + last, plan.stacked ? kOwn : kAll);
 }
-__host__ __device__ inline int chunk_units(const Shape& s, const Plan& plan, int all_units)
+__host__ __device__ inline int units_of(const Shape& s, const Plan& plan, const Sequence& q, int tile_at)
 {
-    const int room = plan.chunks - s.batch, c = (all_units + room - 1) / room;
-    return c > plan.least ? c : plan.least;
+    return (tiles_of<32>(s, plan, q, tile_at).count + kUnit / 32 - 1) / (kUnit / 32);
 }
 __host__ __device__ inline int chunks_of(const Plan& plan, int units, int per_chunk)
 {
-    const int n = (units + per_chunk - 1) / per_chunk;
+    const int n = (int)((uint32_t)(units + per_chunk - 1) / (uint32_t)per_chunk);
     return n > 0 || plan.stacked ? n : 1;
 }
+// The least c for which `all` units make no more chunks than there is room for: total(c) of them.  Without
+// `exact` a c that is large enough.
+template <class Total>
+__host__ __device__ inline int chunk_units(const Plan& plan, int all, bool exact, Total total)
+{
+    const int room = plan.chunks - plan.entries;       // (each entry's last chunk may be short)
+    int lo = (all + plan.chunks - 1) / plan.chunks, hi = (all + room - 1) / room;
+    lo = lo > kLeast ? lo : kLeast;
+    hi = hi > kLeast ? hi : kLeast;
+    while (exact && lo < hi) {
+        const int mid = (lo + hi) / 2;
+        if (total(mid) <= plan.chunks) hi = mid;
+        else lo = mid + 1;
+    }
+    return hi;
+}
 
+// What decides beside the shape: whether bsa_paged_tile.h takes more than 32 rows, and how many wavefronts a
+// workgroup has that takes all of up to `few` tokens of up to 16 rows.
+struct Kind {
+    bool wide;
+    int waves, few;
+};
 // Rows of a workgroup's tile, by how many there are.
-inline int tile_rows(int64_t rows) { return rows <= 16 ? 16 : 32; }
+inline int tile_rows_of(int64_t rows, const Kind& kind)
+{
+    return rows <= 16 ? 16 : rows <= 32 || !kind.wide ? 32 : 128;
+}
 // Most tokens that a sequence's list can hold.
 inline int64_t most_tokens(const Shape& s, bool stacked)
 {
@@ -143,32 +182,45 @@ inline int64_t most_tokens(const Shape& s, bool stacked)
     return seen < all ? seen : all;
 }
 // Nothing here may depend on strides, which the size of the workspace is asked for without.
-inline Plan make_plan(const Shape& s)
+inline Plan make_plan(const Shape& s, int D, const Kind& kind)
 {
     Plan p = {};
+    p.waves = 4;
+    p.tile = tile_rows_of(s.rows, kind);
+    p.tile_rows = p.tile < s.rows ? p.tile : s.rows;
+    p.row_tiles = (s.rows + p.tile - 1) / p.tile;
+    p.entries = p.chunks = s.batch * p.row_tiles;
     p.all_rows = 1;
-    const int64_t own = (int64_t)s.table_pages << s.page_shift;
-    p.stacked = s.batch > 1 && s.prefix_tokens >= 256 && s.rows < 128 && s.left >= s.prefix_tokens + own;
+    const int64_t own = (int64_t)s.table_pages << s.page_shift, slices = (int64_t)s.batch * s.kv_heads;
+    const bool shares = s.batch > 1 && s.prefix_tokens >= 256 && s.rows < 128 && s.left >= s.prefix_tokens + own;
+    if (s.rows <= 16 && kind.waves > 4 && most_tokens(s, false) <= kind.few && (!shares || slices <= 256)) {
+        p.waves = kind.waves;
+        return p;
+    }
+    // Workgroups that the chip holds at once.
+    const int64_t wide_held = D == 64 ? 768 : 512;
+    int64_t shared_items = 0;
+    p.stacked = shares;
     if (p.stacked) {
         p.all_rows = s.batch * s.rows;
-        const int tile = tile_rows(p.all_rows);
-        const int64_t items = (int64_t)s.kv_heads * ((p.all_rows + tile - 1) / tile);
-        int64_t n = 512 / items;
-        if (n > s.prefix_tokens / 256) n = s.prefix_tokens / 256;
+        p.shared_tile = tile_rows_of(p.all_rows, kind);
+        const int tokens = p.shared_tile == 128 ? 384 : 256;
+        const int64_t items = (int64_t)s.kv_heads * ((p.all_rows + p.shared_tile - 1) / p.shared_tile);
+        int64_t n = wide_held / items;
+        if (n > s.prefix_tokens / tokens) n = s.prefix_tokens / tokens;
         p.shared_splits = n < 1 ? 1 : n >= 8 ? (int)n & ~7 : (int)n;
+        shared_items = items * p.shared_splits;
     }
     const int64_t tokens = most_tokens(s, p.stacked), units = (tokens + 31) / 32 / (kUnit / 32) + 2;
-    const int tile = tile_rows(s.rows);
-    const int64_t tiles = (int64_t)s.kv_heads * ((s.rows + tile - 1) / tile);
-    p.least = 2;
-    int64_t n = 1024 / tiles;
-    if (n < 2 * (int64_t)s.batch) n = 2 * (int64_t)s.batch;
-    const int64_t most = s.batch * ((units + p.least - 1) / p.least);
-    if (n > most) n = most;
-    if (s.batch > kMostScanned || s.batch * units >= 1 << 30 || s.batch * tiles >= 4096 || tokens < 640)
-        n = s.batch;
-    p.scanned = n > s.batch;
-    p.chunks = (int)n;
+    const int64_t held = p.tile == 128 || p.shared_tile == 128 ? wide_held : p.tile == 16 ? 1024 : 512;
+    if (p.entries <= kMostScanned && p.entries * units < 1 << 30 && (int64_t)p.entries * s.kv_heads < held &&
+        tokens >= 640) {
+        int64_t n = (held - shared_items) / s.kv_heads;
+        if (n < 2 * (int64_t)p.entries) n = 2 * (int64_t)p.entries;
+        const int64_t most = p.entries * ((units + kLeast - 1) / kLeast);
+        p.chunks = (int)(n < most ? n : most);
+    }
+    p.scanned = p.chunks > p.entries;
     p.parts = p.stacked || p.scanned;
     return p;
 }

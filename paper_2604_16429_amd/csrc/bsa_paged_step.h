@@ -37,19 +37,18 @@ struct Step {
         return row * ROW + ((chunk ^ ((((row & 3) << 1) | ((row >> 2) & 1)) & (CHUNKS - 1))) << 4);
     }
 
-    // Tiles t_a .. t_e - 1 for the given rows, whose queries are at places first .. last; store(row, its
-    // index, channel, four sums, reference, sum of weights).
-    template <class Store>
+    // Tiles t_a .. t_e - 1 for the given rows.  part: index of the first row's sums; negative: these are
+    // all of them, the rows are stored.
     static __device__ __forceinline__ void walk(unsigned char* lds, const Args<T>& g, const Rows& rows,
                                                 const Sequence& seq, const Tiles<KT>& tiles, int t_a, int t_e,
-                                                int first, int last, Store store)
+                                                int64_t part)
     {
         const Shape& s = g.s;
         const int tid = threadIdx.x, lane = tid & 63;
         const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
         const int l16 = lane & 15, grp = lane >> 4;
         unsigned char* const mine = lds + wave * REGION;
-        float* const m_s = (float*)(lds + SUMS);       // [W][NR * 16]
+        float* const m_s = (float*)(lds + SUMS);       // [NR * 16][W]
         float* const l_s = m_s + W * NR * 16;
 
         const T* kb = g.k + (int64_t)rows.a * s.k.head;
@@ -59,16 +58,37 @@ struct Step {
 
         Frag qf[NR][KS];
         int place[NR];                                 // of this lane's rows; -1: no query
+        // the least and the largest place of a query
+        int first = 1 << 30, last = -(1 << 30);
+        if (rows.b >= 0) {
+            const int p0 = seq.prefix + seq.kl - seq.ql;
+            first = p0 + rows.row0 / s.group;
+            last = p0 + min((rows.row0 + rows.n - 1) / s.group, seq.ql - 1);
+        }
 #pragma unroll
         for (int nr = 0; nr < NR; ++nr) {
             const int r = 16 * nr + l16;
             Row x = row_at(s, rows, seq, min(r, rows.n - 1));
             const bool valid = r < rows.n && x.query;
             place[nr] = valid ? x.place : -1;
+            if (rows.b < 0) {
+                first = valid ? min(first, x.place) : first;
+                last = valid ? max(last, x.place) : last;
+            }
             const T* p = g.q + (int64_t)x.b * s.q.batch + (int64_t)x.head * s.q.head + (int64_t)x.tok * s.q.token;
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks)
                 qf[nr][ks] = valid ? Mma<T>::load(p + 32 * ks + 8 * grp) : Frag{};
+        }
+
+        if (rows.b < 0) {
+#pragma unroll
+            for (int o = 1; o < 16; o <<= 1) {
+                first = min(first, __shfl_xor(first, o));
+                last = max(last, __shfl_xor(last, o));
+            }
+            first = __builtin_amdgcn_readfirstlane(first);
+            last = __builtin_amdgcn_readfirstlane(last);
         }
 
         const float c2 = s.scale * kLog2e;
@@ -237,21 +257,30 @@ struct Step {
         }
 
         // ---- the wavefronts' sums, each against the largest reference, in their order
+        auto of_row = [&](const float* at, int r, float (&x)[W]) {
 #pragma unroll
-        for (int nr = 0; nr < NR; ++nr) {
-            const float l = win::row_sum16(l_run[nr]);
-            if (grp == 0) {
-                m_s[wave * NR * 16 + 16 * nr + l16] = m_ref[nr];
-                l_s[wave * NR * 16 + 16 * nr + l16] = l;
+            for (int w = 0; w < W; w += 4) {
+                const f32x4 v = *(const f32x4*)(at + r * W + w);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[w + e] = v[e];
             }
-        }
+        };
+        auto top_of = [&](int r) -> float {
+            float m[W], top = kNoRef;
+            of_row(m_s, r, m);
+#pragma unroll
+            for (int w = 0; w < W; ++w) top = fmaxf(top, m[w]);
+            return top;
+        };
+#pragma unroll
+        for (int nr = 0; nr < NR; ++nr)
+            if (grp == 0) m_s[(16 * nr + l16) * W + wave] = m_ref[nr];
         __syncthreads();                               // (the V tiles are used up as well)
 #pragma unroll
         for (int nr = 0; nr < NR; ++nr) {
-            float top = kNoRef;
-#pragma unroll
-            for (int w = 0; w < W; ++w) top = fmaxf(top, m_s[w * NR * 16 + 16 * nr + l16]);
-            const float f = __builtin_amdgcn_exp2f(m_ref[nr] - top);
+            const float f = __builtin_amdgcn_exp2f(m_ref[nr] - top_of(16 * nr + l16));
+            const float l = win::row_sum16(l_run[nr]) * f;
+            if (grp == 0) l_s[(16 * nr + l16) * W + wave] = l;
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt)
                 *(f32x4*)(mine + ((16 * nr + l16) * D + 16 * dt + 4 * grp) * 4) = acc[nr][dt] * f;
@@ -260,16 +289,17 @@ struct Step {
         const int quads = rows.n * (D / 4);
         for (int at = tid; at < quads; at += 64 * W) {
             const int r = at / (D / 4), c = at % (D / 4) * 4;
-            float top = kNoRef, l = 0.0f;
-#pragma unroll
-            for (int w = 0; w < W; ++w) top = fmaxf(top, m_s[w * NR * 16 + r]);
+            const float top = top_of(r);
+            float ls[W], l = 0.0f;
+            of_row(l_s, r, ls);
             f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int w = 0; w < W; ++w) {
-                l = fmaf(__builtin_amdgcn_exp2f(m_s[w * NR * 16 + r] - top), l_s[w * NR * 16 + r], l);
+                l += ls[w];
                 sum += *(const f32x4*)(lds + w * REGION + (r * D + c) * 4);
             }
-            store(r, c, sum, top, l);
+            if (part < 0) store_row<T, D>(g, row_at(s, rows, seq, r), c, sum, top, l);
+            else store_part<D>(g.plan, part + r, c, sum, top, l);
         }
     }
 };

@@ -157,8 +157,8 @@ __device__ __forceinline__ f32x16 start_of(const Sight& see, int slot0, int half
 // a row in the two lanes of its number, times f: through 4 KiB of LDS of its own, 64 channels at a
 // time, so that a store instruction writes runs of 128 bytes.  `to`: the batch entry's rows of the first
 // head of the group.
-template <int D>
-__device__ __forceinline__ void store_wave_rows(uint16_t* to, const mosaic_bsa_strides& st, const Shape& s,
+template <int D, class S>
+__device__ __forceinline__ void store_wave_rows(uint16_t* to, const mosaic_bsa_strides& st, const S& s,
                                                 int row0, const f32x16 (&acc)[D / 32], float f,
                                                 unsigned char* lds, int lane)
 {

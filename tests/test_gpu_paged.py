@@ -87,6 +87,14 @@ def test_prefixes(dtype, B, N, h, kv, D, P, own):
     run(dtype, B, h, kv, N, D, 16, own, prefix=P, seed=B + P)
 
 
+@pytest.mark.parametrize("B,most,prefix", [(65, 1500, 0), (70, 900, 300), (130, 1000, 0), (200, 700, 0), (1030, 40, 260)])
+def test_large_batches(B, most, prefix):
+    """Chunks are found by a sum over the batch."""
+    own = [(37 * b * b + 11 * b) % most if b % 5 else 0 for b in range(B)]
+    own[-1] = most
+    run(BF16, B, 2, 1, 1, 32, 64, own, prefix=prefix, q_lens=[1 if b % 7 else 0 for b in range(B)], seed=B)
+
+
 @TYPES
 @pytest.mark.parametrize("N,q_lens,own,prefix", [
     (6, [6, 0, 3, 1, 5], [6, 9, 0, 1, 2], 20),           # no queries; queries that reach into the prefix

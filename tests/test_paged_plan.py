@@ -36,8 +36,6 @@ extern "C" int walk_of(int kt, int prefix, int ql, int kl, int left, int sinks, 
     return kt == 32 ? walk<32>(prefix, ql, kl, left, sinks, first, last, out)
                     : walk<64>(prefix, ql, kl, left, sinks, first, last, out);
 }
-// what: 0 batch, rows, kv_heads, own, prefix (a power of two of pages), left, q_tokens -> chunks, scanned, stacked,
-// splits, parts, least; then the chunks of every sequence of the given lengths
 extern "C" int64_t plan_of(const int32_t* shape, const int32_t* lens, int32_t* out, int32_t* chunks)
 {
     Shape s = {};
@@ -50,16 +48,29 @@ extern "C" int64_t plan_of(const int32_t* shape, const int32_t* lens, int32_t* o
     s.prefix_tokens = shape[5];
     s.left = shape[6];
     s.sinks = shape[7];
-    const Plan p = make_plan(s);
-    const int32_t v[] = {p.chunks, p.scanned, p.stacked, p.shared_splits, p.parts, p.least, p.all_rows};
-    for (int i = 0; i < 7; ++i) out[i] = v[i];
+    const Plan p = make_plan(s, shape[10], Kind{shape[8] != 0, shape[9], 128 * shape[9]});
+    const int32_t v[] = {p.chunks, p.scanned, p.stacked, p.shared_splits, p.parts, p.entries, p.all_rows, p.tile_rows,
+                         p.tile, p.row_tiles};
+    for (int i = 0; i < 10; ++i) out[i] = v[i];
     if (p.scanned) {
+        auto units = [&](int e) {
+            const int32_t* l = lens + 3 * p.sequence_of(s, e);
+            return units_of(s, p, Sequence{l[0], l[1], l[2]}, p.tile_of(s, e));
+        };
         int all = 0;
-        for (int b = 0; b < s.batch; ++b) all += units_of(s, p, Sequence{lens[3 * b], lens[3 * b + 1], lens[3 * b + 2]});
-        const int per = chunk_units(s, p, all);
-        for (int b = 0; b < s.batch; ++b)
-            chunks[b] = chunks_of(p, units_of(s, p, Sequence{lens[3 * b], lens[3 * b + 1], lens[3 * b + 2]}), per);
+        for (int e = 0; e < p.entries; ++e) all += units(e);
+        auto total = [&](int c) {
+            int n = 0;
+            for (int e = 0; e < p.entries; ++e) n += chunks_of(p, units(e), c);
+            return n;
+        };
+        const int per = chunk_units(p, all, p.entries <= 128, total);
+        out[10] = per;
+        out[11] = per > kLeast ? total(per - 1) : -1;
+        for (int e = 0; e < p.entries; ++e) chunks[e] = chunks_of(p, units(e), per);
     }
+    for (int e = 0; e < p.entries && e < 5000; ++e)
+        if (p.entry_of(s, p.sequence_of(s, e), p.tile_of(s, e)) != e) return -1;
     return p.all_parts(s);
 }
 extern "C" int page(int pages, int shift, const int32_t* table, int at, int count)
@@ -87,31 +98,37 @@ UNBOUNDED = 1 << 30
 
 
 def test_chunks_fit(plan):
-    """Whatever the lengths, all chunks have a place, and each sequence that needs one has one."""
+    """Whatever the lengths, all chunks have a place, and each tile of rows that needs one has one."""
     plan.plan_of.restype = ctypes.c_int64
     rng = random.Random(0)
-    seen = {"scanned": 0, "stacked": 0}
-    for _ in range(3000):
-        B, q_tokens = rng.choice([1, 2, 7, 64, 300, 1024, 1500]), rng.choice([1, 1, 1, 5, 40, 1000])
+    seen = {"scanned": 0, "stacked": 0, "exact": 0}
+    for _ in range(1500):
+        B, q_tokens = rng.choice([1, 2, 7, 64, 300, 1024, 2500]), rng.choice([1, 1, 1, 5, 40, 1000])
         shape = [B, rng.choice([1, 2, 4, 8, 16]), q_tokens, rng.choice([1, 2, 8]),
                  rng.choice([1, 100, 1000, 30000, 1 << 20, (1 << 29) - 1]), rng.choice([0, 0, 300, 20000, (1 << 29) - 1]),
-                 rng.choice([UNBOUNDED, UNBOUNDED, 1000]), rng.choice([0, 4])]
+                 rng.choice([UNBOUNDED, UNBOUNDED, 1000]), rng.choice([0, 4]), rng.randint(0, 1),
+                 rng.choice([4, 8, 16]), rng.choice([32, 64, 128])]
         own, prefix = shape[4], shape[5]
         lens = np.array([[rng.choice([0, 1, q_tokens]), rng.choice([0, 1, own, rng.randint(0, own)]), prefix]
                          for _ in range(B)], dtype=np.int32)
-        out, chunks = np.zeros(7, np.int32), np.zeros(B, np.int32)
+        out, chunks = np.zeros(12, np.int32), np.zeros(1 << 19, np.int32)
         n = plan.plan_of(np.array(shape, np.int32).ctypes.data_as(ctypes.c_void_p),
                          lens.ctypes.data_as(ctypes.c_void_p), out.ctypes.data_as(ctypes.c_void_p),
                          chunks.ctypes.data_as(ctypes.c_void_p))
-        total, scanned, stacked, splits, parts, least, all_rows = out.tolist()
+        total, scanned, stacked, splits, parts, entries, all_rows, tile_rows, tile, row_tiles, per, below = out.tolist()
         rows = shape[1] * q_tokens
-        assert total >= B and least >= 1 and parts == (stacked or scanned)
-        assert n == shape[3] * (total * rows + splits * all_rows) and n < 1 << 40
+        assert row_tiles == -(-rows // tile) and tile_rows == min(tile, rows) and entries == B * row_tiles
+        assert total >= entries and parts == (stacked or scanned)
+        assert n == shape[3] * (total * tile_rows + splits * all_rows) and n < 1 << 40
         assert all_rows == (B * rows if stacked else 1) and (splits >= 1) == bool(stacked)
         if scanned:
-            assert total > B and int(chunks.sum()) <= total and int(chunks.min()) >= (0 if stacked else 1)
+            assert total > entries and int(chunks.sum()) <= total
+            assert int(chunks[:entries].min()) >= (0 if stacked else 1)
+            if entries <= 128:
+                assert below == -1 or below > total        # no smaller chunk would do
+                seen["exact"] += 1
         else:
-            assert total == B
+            assert total == entries
         seen["scanned"] += scanned
         seen["stacked"] += stacked
     assert min(seen.values()) > 100
