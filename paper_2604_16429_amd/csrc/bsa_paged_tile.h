@@ -51,18 +51,24 @@ struct WideTile {
         const int32_t* own_table = s.table + (int64_t)max(rows.b, 0) * s.table_pages;
         const int in_page = (1 << s.page_shift) - 1;
 
-        // The page of token `lane` of a tile: -1 if it names none, the last token's behind the list's end.
-        auto ask = [&](int t) -> int {
-            if (t >= t_e) return -1;
-            const Tile tile = list[t];
-            const int32_t* table = tile.shared ? s.prefix_table : own_table;
-            return page_of(s, table, min(tile.at + lane, tile.count - 1), tile.count);
+        // A tile and, in every lane, the page of token `lane` of it: -1 if it names none, the last token's behind
+        // the list's end.  n: its tokens, at most KT of them count; 0: no tile.
+        struct Ahead {
+            int at, n, token, id;
         };
-        auto hidden_of = [&](int t, int id) -> uint64_t {
-            if (t >= t_e) return 0;
-            const Tile tile = list[t];
-            return __builtin_amdgcn_ballot_w64(id < 0 || lane >= tile.count - tile.at);
+        auto ask = [&](int t) -> Ahead {
+            Ahead x = {0, 0, 0, -1};
+            if (t < t_e) {
+                const Tile tile = list[t];
+                const int32_t* table = tile.shared ? s.prefix_table : own_table;
+                x.at = tile.at;
+                x.n = tile.count - tile.at;
+                x.token = tile.token;
+                x.id = page_of(s, table, min(tile.at + lane, tile.count - 1), tile.count);
+            }
+            return x;
         };
+        auto hidden_of = [&](const Ahead& x) -> uint64_t { return __builtin_amdgcn_ballot_w64(x.id < 0 || lane >= x.n); };
         const int row_of = lane / R::CHUNKS;           // of this lane in a load
         const uint32_t chunk = (uint32_t)R::swizzled(row_of, lane % R::CHUNKS) * 16;
         // (strides_fit: 32-bit strides)
@@ -70,11 +76,10 @@ struct WideTile {
             return pool + (uint64_t)(uint32_t)page * (uint32_t)st.batch +
                    (uint64_t)(uint32_t)(at & in_page) * (uint32_t)st.token;
         };
-        auto gather = [&](const uint16_t* pool, const mosaic_bsa_strides& st, int t, int id, uint64_t hidden,
+        auto gather = [&](const uint16_t* pool, const mosaic_bsa_strides& st, const Ahead& x, uint64_t hidden,
                           unsigned char* to) {
-            if (t >= t_e) return;
-            const Tile tile = list[t];
-            const int n = tile.count - tile.at;
+            const int n = x.n, id = x.id;
+            if (n <= 0) return;
             const uint32_t stride = (uint32_t)st.token * 2u, to0 = lds_address(to) + (uint32_t)(wave * R::SLAB);
             auto nothing = [&](int i) { *(uint4*)(to + (wave + 4 * i) * R::SLAB + 16 * lane) = make_uint4(0, 0, 0, 0); };
             if constexpr (ONE) {
@@ -84,7 +89,7 @@ struct WideTile {
                     for (int i = 0; i < MINE; ++i) nothing(i);
                     return;
                 }
-                const i32x4 rsrc = buffer_desc(row_at_page(pool, st, page, tile.at), (KT - 1) * stride + R::ROW_BYTES);
+                const i32x4 rsrc = buffer_desc(row_at_page(pool, st, page, x.at), (KT - 1) * stride + R::ROW_BYTES);
                 const int row = R::PER_SLAB * wave + row_of;
                 if (n >= KT) {
                     const uint32_t from = (uint32_t)row * stride + chunk;
@@ -102,7 +107,7 @@ struct WideTile {
 #pragma unroll
                 for (int i = 0; i < MINE; ++i) {
                     const int r0 = R::PER_SLAB * (wave + 4 * i);
-                    const uint16_t* p = row_at_page(pool, st, __builtin_amdgcn_readlane(id, r0), tile.at + r0);
+                    const uint16_t* p = row_at_page(pool, st, __builtin_amdgcn_readlane(id, r0), x.at + r0);
                     load_lds_16(buffer_desc(p, (R::PER_SLAB - 1) * stride + R::ROW_BYTES), from, 0,
                                 to0 + (uint32_t)(4 * i * R::SLAB));
                 }
@@ -116,21 +121,22 @@ struct WideTile {
                         continue;
                     }
                     const uint32_t r = (uint32_t)min(row_of, n - 1 - r0);
-                    load_lds_16(buffer_desc(row_at_page(pool, st, page, tile.at + r0), (R::PER_SLAB - 1) * stride + R::ROW_BYTES),
+                    load_lds_16(buffer_desc(row_at_page(pool, st, page, x.at + r0), (R::PER_SLAB - 1) * stride + R::ROW_BYTES),
                                 r * stride + chunk, 0, to0 + (uint32_t)(4 * i * R::SLAB));
                 }
             }
         };
         auto k_to = [&](int t) { return tiles_s[0][(t - t_a) & 1]; };
         auto v_to = [&](int t) { return tiles_s[1][(t - t_a) & 1]; };
-        // pages of the next two tiles, hidden tokens of this one and the next (by parity)
-        int id1 = ask(t_a), id2 = ask(t_a + 1);
-        uint64_t hidden[2] = {hidden_of(t_a, id1), hidden_of(t_a + 1, id2)};
-        gather(kb, s.k, t_a, id1, hidden[0], k_to(t_a));
-        gather(vb, s.v, t_a, id1, hidden[0], v_to(t_a));
-        gather(kb, s.k, t_a + 1, id2, hidden[1], k_to(t_a + 1));
-        id1 = id2;
-        id2 = ask(t_a + 2);
+        // the next two tiles, with their hidden tokens, and what masks of the present one take
+        Ahead next = ask(t_a), after = ask(t_a + 1);
+        uint64_t hidden = hidden_of(next), next_hidden = hidden_of(after);
+        int token = next.token;
+        gather(kb, s.k, next, hidden, k_to(t_a));
+        gather(vb, s.v, next, hidden, v_to(t_a));
+        gather(kb, s.k, after, next_hidden, k_to(t_a + 1));
+        next = after;
+        after = ask(t_a + 2);
 
         const Row x = row_at(s, rows, seq, min(32 * wave + l32, rows.n - 1));
         const bool exists = 32 * wave + l32 < rows.n, query = exists && x.query;
@@ -155,16 +161,16 @@ struct WideTile {
         for (int dt = 0; dt < DT; ++dt) acc[dt] = win::splat(0.0f);
         float m_ref = kNoRef, l_run = 0.0f;
 
-        // (rows that are no query may see what they like: nothing is kept of them)
-        auto full = [&](int t, int h) -> bool {
-            if (t >= t_e) return true;
-            const int j = list[t].token + 32 * h;
-            return (uint32_t)(hidden[(t - t_a) & 1] >> (32 * h)) == 0 && j + 31 <= first &&
-                   (j >= last - s.left || j + 32 <= s.sinks);
+        // (rows that are no query may see what they like: nothing is kept of them; behind the last tile there is
+        // nothing to keep either)
+        const int lo_all = last - s.left;
+        auto full = [&](int, int h) -> bool {
+            const int j = token + 32 * h;
+            return (uint32_t)(hidden >> (32 * h)) == 0 && j + 31 <= first && (j >= lo_all || j + 32 <= s.sinks);
         };
-        auto start = [&](int t, int h) -> f32x16 {
-            const int j = list[t].token + 32 * h + 4 * half;
-            const uint32_t mask = (uint32_t)(hidden[(t - t_a) & 1] >> (32 * h)) >> (4 * half);
+        auto start = [&](int, int h) -> f32x16 {
+            const int j = token + 32 * h + 4 * half;
+            const uint32_t mask = (uint32_t)(hidden >> (32 * h)) >> (4 * half);
             const uint32_t lo = (uint32_t)(j - (place - s.left));
             const int sinks = min(s.sinks, place + 1) - j;
             f32x16 st;
@@ -176,12 +182,15 @@ struct WideTile {
             }
             return st;
         };
+        // (in the middle of a tile: its masks are done, those of the next one follow)
         win::walk_tiles<D>(tiles_s, t_a, t_e, qf, s.scale * kLog2e, acc, m_ref, l_run, lane, full, start, [&](int t) {
-            hidden[(t - t_a) & 1] = hidden_of(t + 2, id2);
-            gather(kb, s.k, t + 2, id2, hidden[(t - t_a) & 1], k_to(t + 2));
-            gather(vb, s.v, t + 1, id1, hidden[(t + 1 - t_a) & 1], v_to(t + 1));
-            id1 = id2;
-            id2 = ask(t + 3);
+            token = next.token;
+            hidden = next_hidden;
+            next_hidden = hidden_of(after);
+            gather(kb, s.k, after, next_hidden, k_to(t + 2));
+            gather(vb, s.v, next, hidden, v_to(t + 1));
+            next = after;
+            after = ask(t + 3);
         });
 
         const float l = l_run + swap32(l_run);

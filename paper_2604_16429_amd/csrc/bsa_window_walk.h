@@ -30,7 +30,8 @@ struct Walk {
 
 // Tiles c_a .. c_e - 1; K of the first two and V of the first have been asked for.  full(c, h): whether all of the
 // wavefront's rows see all of half h of tile c (also asked for tile c_e); start(c, h): what its S^T starts
-// from otherwise (start_of); issue(c): asks for K of tile c + 2 and V of tile c + 1, as far as there are any.
+// from otherwise (start_of); issue(c): asks for K of tile c + 2 and V of tile c + 1, as far as there are any.  The
+// order of calls: full and start of (c, 1), issue(c), full and start of (c + 1, 0).
 template <int D, class Full, class Start, class Issue>
 __device__ __forceinline__ void walk_tiles(typename Walk<D>::Tiles& tiles, int c_a, int c_e,
                                            const bf16x8 (&qf)[D / 16], float c2, f32x16 (&acc)[D / 32],
