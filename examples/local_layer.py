@@ -7,7 +7,9 @@ rotated by position in one pass, attention runs inside a sliding window with a f
 tokens that stay visible, and a second projection closes the layer.  Gradients go back the
 same way, into one tensor beside the projection's output.  Then the layer reads the same
 tokens one at a time: a single call norms, rotates and writes keys and values into a ring
-cache that holds the window and the first tokens, and the attention reads it.
+cache that holds the window and the first tokens, and the attention reads it.  Members of an
+ensemble that go on from one beginning read it once, into pages that all of them share, and keep
+pages of their own for what follows.
 """
 from __future__ import annotations
 
@@ -122,6 +124,54 @@ class Server:
         return self.out.view(self.batch, -1) @ lay.w_out.t()
 
 
+class MemberServer:
+    """Members that go on from one common beginning, which is read and kept once: pages of a pool, those
+    of the beginning in `prefix_table`, each member's own in its row of `table`."""
+
+    def __init__(self, layer, members, shared, own, page=64):
+        self.layer, self.members, self.shared, self.page = layer, members, shared, page
+        n, each = -(-shared // page), -(-own // page)
+        self.pages = n + members * each
+        ids = torch.arange(self.pages, dtype=torch.int32, device="cuda")
+        self.prefix_table, self.table = ids[:n].contiguous(), ids[n:].view(members, each).contiguous()
+        self.k_pages, self.v_pages = (
+            torch.zeros(self.pages, layer.kv_heads, page, layer.head_dim, dtype=torch.bfloat16,
+                        device="cuda") for _ in range(2))
+        self.length = torch.zeros(members, dtype=torch.int32, device="cuda")
+        self.steps = self._params(members, 1, each, shared)
+        self.ws = _space(bsa.mosaic_bsa_paged_workspace_bytes(self.steps))
+
+    def _params(self, batch, tokens, table_pages, prefix):
+        lay = self.layer
+        return bsa.PagedParams(batch, lay.heads, tokens, lay.head_dim, self.pages, self.page,
+                               table_pages, binding.BF16, kv_heads=lay.kv_heads, prefix_tokens=prefix,
+                               window_left=lay.window - 1, n_sink=lay.sinks)
+
+    def _run(self, p, x, lengths, table, prefix_table, ws):
+        """x [batch, tokens, width], counted in `lengths` already."""
+        lay, (B, N, _) = self.layer, x.shape
+        q, k, v = lay._split((x.reshape(B * N, -1) @ lay.w_in.t()).view(B, N, -1))
+        qr = torch.empty(B, lay.heads, N, lay.head_dim, dtype=x.dtype, device="cuda")
+        bsa.mosaic_bsa_paged_append(p, lay.rotation, None, q, k, v, lay.q_norm, lay.k_norm, None,
+                                    lengths, table, None, qr, self.k_pages, self.v_pages)
+        out = torch.empty(B, N, lay.heads, lay.head_dim, dtype=x.dtype, device="cuda")
+        bsa.mosaic_bsa_paged_fwd(p, qr, self.k_pages, self.v_pages, None, lengths, table,
+                                 prefix_table, None, out.transpose(1, 2), workspace=ws)
+        return (out.view(B * N, -1) @ lay.w_out.t()).view(B, N, -1)
+
+    def begin(self, x):
+        """x [shared, width], the common beginning -> y [shared, width]."""
+        p = self._params(1, self.shared, self.prefix_table.numel(), 0)
+        lengths = torch.full((1,), self.shared, dtype=torch.int32, device="cuda")
+        ws = _space(bsa.mosaic_bsa_paged_workspace_bytes(p))
+        return self._run(p, x.unsqueeze(0), lengths, self.prefix_table.view(1, -1), None, ws)[0]
+
+    def step(self, x):
+        """x [members, width] -> y [members, width]."""
+        self.length += 1
+        return self._run(self.steps, x.unsqueeze(1), self.length, self.table, self.prefix_table, self.ws)[:, 0]
+
+
 def _space(n):
     return torch.empty(max(n, 256), dtype=torch.uint8, device="cuda")
 
@@ -151,6 +201,23 @@ def run(batch=2, tokens=600, width=256, heads=8, kv_heads=2, head_dim=64, window
     return losses, apart
 
 
+def run_members(members=3, shared=300, own=40, width=256, heads=8, kv_heads=2, head_dim=64, window=128,
+                sinks=4, page=64):
+    """Members that go on from a common beginning, token by token from pages, against whole sequences:
+    the largest difference relative to the largest output."""
+    layer = LocalLayer(width, heads, kv_heads, head_dim, window, sinks)
+    gen = torch.Generator().manual_seed(2)
+    start = torch.randn(shared, width, generator=gen).to(torch.bfloat16).cuda()
+    rest = torch.randn(members, own, width, generator=gen).to(torch.bfloat16).cuda()
+    whole, _ = layer.forward(torch.cat([start.expand(members, -1, -1), rest], dim=1))
+    server = MemberServer(layer, members, shared, own, page)
+    y = server.begin(start)
+    steps = torch.stack([server.step(rest[:, t]) for t in range(own)], dim=1)
+    apart = torch.cat([(whole[0, :shared].float() - y.float()).abs().flatten(),
+                       (whole[:, shared:].float() - steps.float()).abs().flatten()])
+    return float(apart.max() / whole.float().abs().max())
+
+
 if __name__ == "__main__":
     p = argparse.ArgumentParser(description=__doc__.splitlines()[0])
     for name, value in (("batch", 2), ("tokens", 600), ("width", 256), ("heads", 8), ("kv-heads", 2),
@@ -161,3 +228,5 @@ if __name__ == "__main__":
                         a.steps)
     print("loss by step:", " ".join(f"{x:.4f}" for x in losses))
     print(f"whole sequence against single tokens: {apart:.2e} of the largest output")
+    apart = run_members(3, a.tokens, 40, a.width, a.heads, a.kv_heads, a.head_dim, a.window, a.sinks)
+    print(f"members on a common beginning, from pages: {apart:.2e} of the largest output")

@@ -172,17 +172,18 @@ class _StridedParams:
             self.__dict__.update(_struct=c, _ref=ctypes.byref(c))
         return c
 
-    def _call(self, entry, *args, position_batch=None):
+    def _call(self, entry, *args, position_batch=None, device=None):
         """(struct, its reference, device pointers) of a call of `entry` on [batch, heads, tokens, head_dim]
         tensors, given as (field of the struct, tensor, heads, tokens) one after the other.  Integers and
-        None are taken as they are (contiguous)."""
+        None are taken as they are (contiguous).  device: the GPU that all of them have to be on."""
         looks, pointers = [position_batch], []
         for _, t, heads, tokens in args:
             if t is None or isinstance(t, int):
                 looks.append(None)
                 pointers.append(t)
             else:
-                looks.append((t.shape, t.stride(), t.dtype, t.is_cuda, heads, tokens))
+                looks.append((t.shape, t.stride(), t.dtype,
+                              t.is_cuda if device is None else t.get_device() == device, heads, tokens))
                 pointers.append(t.data_ptr())
         kept = self._kept
         last = kept.get(entry)
@@ -192,6 +193,8 @@ class _StridedParams:
                 c.position_batch = position_batch
             for field, t, heads, tokens in args:
                 if t is not None and not isinstance(t, int):
+                    if device is not None and t.get_device() != device:
+                        raise ValueError(f"{field}: on {t.device} instead of the first tensor's GPU")
                     setattr(c, field, self._strides(field, t, heads, tokens))
             last = kept[entry] = looks, c, ctypes.byref(c)
         return last[1], last[2], pointers
@@ -639,21 +642,50 @@ def mosaic_bsa_window_bwd(params: WindowParams, q, k, v, out, lse, dout, dq, dk,
 # ---- a cache in pages: k_pages and v_pages of shape [pages, kv_heads, page_tokens, head_dim] with any
 # strides of the first three dimensions
 
+def _device_of(t):
+    """The GPU of a call's first tensor; None for an address."""
+    return None if t is None or isinstance(t, int) else t.get_device()
+
+
+def _vector_on(device, name, t, size, dtype_name):
+    """_vector on one GPU."""
+    if t is None or isinstance(t, int):
+        return t
+    if (t.numel() != size or t.dtype is not _named_dtype(dtype_name) or not t.is_contiguous() or
+            (t.get_device() != device if device is not None else not t.is_cuda)):
+        raise ValueError(f"{name}: {size} contiguous {dtype_name} values on the tensors' GPU expected")
+    return t.data_ptr()
+
+
+def _stream_on(device, stream):
+    """_stream, which has to belong to the tensors' GPU."""
+    handle = _stream(stream)
+    if device is not None:
+        there = (_raw_stream[1]() if stream is None else
+                 device if isinstance(stream, int) else stream.device_index)
+        if there != device:
+            raise ValueError(f"tensors on cuda:{device}, stream on cuda:{there}")
+    return handle
+
+
 def mosaic_bsa_paged_append(params: PagedParams, rotation: Rotation, positions, q, k, v, q_weight,
                             k_weight, q_lens, k_lens, page_table, prefix_len, q_out, k_pages, v_pages,
                             stream=None) -> None:
     h, kv, n, d = params.heads, params.kv_heads or params.heads, params.q_tokens, params.head_dim
-    b, t = params.batch, params.page_tokens
+    b, t, on = params.batch, params.page_tokens, _device_of(q)
     pos, per = params._positions_of(rotation, positions, n)
+    if pos is not positions and on is not None and positions.get_device() != on:
+        raise ValueError("positions: on another GPU")
     _, ref, (q, k, v, q_out, k_pages, v_pages) = params._call(
         "append", ("q", q, h, n), ("k", k, kv, n), ("v", v, kv, n), ("out", q_out, h, n),
-        ("k_pages", k_pages, kv, t), ("v_pages", v_pages, kv, t), position_batch=per)
+        ("k_pages", k_pages, kv, t), ("v_pages", v_pages, kv, t), position_batch=per, device=on)
     _check(load_library().mosaic_bsa_paged_append(
-        ref, rotation.ref, pos, q, k, v, _vector("q_weight", q_weight, d, "float32"),
-        _vector("k_weight", k_weight, d, "float32"), _vector("q_lens", q_lens, b, "int32"),
-        _vector("k_lens", k_lens, b, "int32"),
-        _vector("page_table", page_table, b * params.table_pages, "int32"),
-        _vector("prefix_len", prefix_len, 1, "int32"), q_out, k_pages, v_pages, _stream(stream)))
+        ref, rotation.ref, pos, q, k, v, _vector_on(on, "q_weight", q_weight, d, "float32"),
+        _vector_on(on, "k_weight", k_weight, d, "float32"), _vector_on(on, "q_lens", q_lens, b, "int32"),
+        _vector_on(on, "k_lens", k_lens, b, "int32"),
+        _vector_on(on, "page_table", page_table, b * params.table_pages, "int32"),
+        _vector_on(on, "prefix_len", prefix_len, 1, "int32"), q_out, k_pages, v_pages,
+        _stream_on(on, stream)))
 
 
 def mosaic_bsa_paged_workspace_bytes(params: PagedParams) -> int:
@@ -664,17 +696,19 @@ def mosaic_bsa_paged_fwd(params: PagedParams, q, k_pages, v_pages, q_lens, k_len
                          prefix_table, prefix_len, out, lse=None, workspace=None, stream=None,
                          workspace_bytes=None) -> None:
     h, kv, n, b = params.heads, params.kv_heads or params.heads, params.q_tokens, params.batch
-    t = params.page_tokens
+    t, on = params.page_tokens, _device_of(q)
     wb = _nbytes(workspace) if workspace_bytes is None else workspace_bytes
+    if on is not None and _device_of(workspace) not in (None, on):
+        raise ValueError("workspace: on another device than the tensors")
     _, ref, (q, k_pages, v_pages, out) = params._call(
         "fwd", ("q", q, h, n), ("k_pages", k_pages, kv, t), ("v_pages", v_pages, kv, t),
-        ("out", out, h, n))
+        ("out", out, h, n), device=on)
     if params.prefix_tokens <= 0:
         prefix_table = None
     _check(load_library().mosaic_bsa_paged_fwd(
-        ref, q, k_pages, v_pages, _vector("q_lens", q_lens, b, "int32"),
-        _vector("k_lens", k_lens, b, "int32"),
-        _vector("page_table", page_table, b * params.table_pages, "int32"),
-        _vector("prefix_table", prefix_table, -(-params.prefix_tokens // max(t, 1)), "int32"),
-        _vector("prefix_len", prefix_len, 1, "int32"), out,
-        _vector("lse", lse, b * h * n, "float32"), _ptr(workspace), wb, _stream(stream)))
+        ref, q, k_pages, v_pages, _vector_on(on, "q_lens", q_lens, b, "int32"),
+        _vector_on(on, "k_lens", k_lens, b, "int32"),
+        _vector_on(on, "page_table", page_table, b * params.table_pages, "int32"),
+        _vector_on(on, "prefix_table", prefix_table, -(-params.prefix_tokens // max(t, 1)), "int32"),
+        _vector_on(on, "prefix_len", prefix_len, 1, "int32"), out,
+        _vector_on(on, "lse", lse, b * h * n, "float32"), _ptr(workspace), wb, _stream_on(on, stream)))

@@ -208,6 +208,7 @@ inline Plan make_plan(const Shape& s, int D, const Kind& kind)
         const int64_t items = (int64_t)s.kv_heads * ((p.all_rows + p.shared_tile - 1) / p.shared_tile);
         int64_t n = wide_held / items;
         if (n > s.prefix_tokens / tokens) n = s.prefix_tokens / tokens;
+        if (n > 64) n = 64;
         p.shared_splits = n < 1 ? 1 : n >= 8 ? (int)n & ~7 : (int)n;
         shared_items = items * p.shared_splits;
     }

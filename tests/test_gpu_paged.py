@@ -274,3 +274,44 @@ def test_another_stream_and_graphs_that_share_a_workspace():
             call(i, want, other)
             torch.cuda.synchronize()
             assert torch.equal(out[i], want)
+
+
+def test_token_strides_past_32_bits_of_a_tile():
+    """Rows 2^24 elements apart: the kernels for any stride take over, with the same workspace."""
+    import paper_2604_16429_amd as M
+    T, kv, D, B, h = 8, 1, 64, 2, 4
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    far = [torch.zeros(T << 24, dtype=BF16, device="cuda").as_strided((40, kv, T, D), (D, 0, 1 << 24, 1))
+           for _ in range(2)]
+    near = [torch.randn(40, kv, T, D, generator=gen, device="cuda").to(BF16) for _ in range(2)]
+    for a, b in zip(far, near):
+        a.copy_(b)
+    table = torch.randperm(40, generator=gen, device="cuda")[:36].to(torch.int32)
+    for N, prefix in ((50, 0), (50, 60), (1, 60)):
+        q = torch.randn(B, h, N, D, generator=gen, device="cuda").to(BF16)
+        p = M.PagedParams(B, h, N, D, 40, T, 14, kv_heads=kv, prefix_tokens=prefix)
+        lens = torch.tensor([112, 51], dtype=torch.int32, device="cuda")
+        n = M.mosaic_bsa_paged_workspace_bytes(p)
+        outs = []
+        for k, v in (far, near):
+            ws, out = torch.empty(max(n, 256), dtype=torch.uint8, device="cuda"), torch.empty_like(q)
+            M.mosaic_bsa_paged_fwd(p, q, k, v, None, lens, table[:28].contiguous().view(2, 14), table[28:].contiguous(),
+                                   None, out, workspace=ws)
+            outs.append(out.float())
+        # each within its roundings of the definition: weights and result, a half step each
+        assert float((outs[0] - outs[1]).abs().max()) <= 2 * 2 * 2.0 ** -8 * float(near[1].abs().max())
+
+
+def test_streams_as_objects():
+    import paper_2604_16429_amd as M
+    k, v, table, prefix_table = cache_on_the_gpu(2, 2, 16, 64, 100, 40)
+    q = torch.randn(2, 4, 1, 64, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)).to(BF16)
+    p = M.PagedParams(2, 4, 1, 64, k.shape[0], 16, table.shape[1], kv_heads=2, prefix_tokens=40)
+    lens = torch.full((2,), 100, dtype=torch.int32, device="cuda")
+    outs = [torch.empty_like(q) for _ in range(2)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for out, stream in zip(outs, (None, side)):
+        M.mosaic_bsa_paged_fwd(p, q, k, v, None, lens, table, prefix_table, None, out, stream=stream)
+    torch.cuda.synchronize()
+    assert torch.equal(*outs)

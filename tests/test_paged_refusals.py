@@ -144,6 +144,90 @@ def test_tensors_of_another_shape_or_place():
         append(p, prefix_len=torch.zeros(1, dtype=torch.int64))
 
 
+class OnGpu:
+    """A tensor of some GPU: shape, strides and an address, nothing behind it."""
+
+    def __init__(self, device, *shape, dtype=torch.bfloat16):
+        self.t, self.index = torch.empty(shape, dtype=dtype, device="meta"), device
+        self.shape, self.dtype, self.is_cuda, self.device = self.t.shape, dtype, True, f"cuda:{device}"
+
+    def stride(self):
+        return self.t.stride()
+
+    def numel(self):
+        return self.t.numel()
+
+    def is_contiguous(self):
+        return True
+
+    def element_size(self):
+        return self.t.element_size()
+
+    def get_device(self):
+        return self.index
+
+    def data_ptr(self):
+        return FAKE
+
+
+class Library:
+    """Takes every call."""
+
+    def __init__(self):
+        self.calls = 0
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls += 1
+            return 0
+        return call
+
+
+def tensors(device):
+    i32 = torch.int32
+    return dict(q=OnGpu(device, 2, 4, 8, 64), k_pages=OnGpu(device, 16, 2, 16, 64),
+                v_pages=OnGpu(device, 16, 2, 16, 64), q_lens=OnGpu(device, 2, dtype=i32),
+                k_lens=OnGpu(device, 2, dtype=i32), page_table=OnGpu(device, 2, 4, dtype=i32),
+                prefix_table=OnGpu(device, 2, dtype=i32), prefix_len=OnGpu(device, 1, dtype=i32),
+                out=OnGpu(device, 2, 4, 8, 64), lse=OnGpu(device, 2, 4, 8, dtype=torch.float32),
+                workspace=OnGpu(device, 1 << 20, dtype=torch.uint8))
+
+
+def append_tensors(device):
+    t = tensors(device)
+    new = {n: OnGpu(device, 2, c, 8, 64) for n, c in (("q", 4), ("k", 2), ("v", 2), ("q_out", 4))}
+    w = {n: OnGpu(device, 64, dtype=torch.float32) for n in ("q_weight", "k_weight")}
+    return {**new, **w, **{n: t[n] for n in ("q_lens", "k_lens", "page_table", "prefix_len", "k_pages", "v_pages")}}
+
+
+@pytest.mark.parametrize("call,make", [(attend, tensors), (append, append_tensors)], ids=["attend", "append"])
+def test_tensors_of_two_gpus(monkeypatch, call, make):
+    lib, p = Library(), params()
+    rot = M.Rotation(64)
+    monkeypatch.setattr(binding, "_lib", lib)
+    extra = {"rot": rot} if call is append else {}
+    call(p, **extra, **make(1))
+    call(p, **extra, **make(0))
+    assert lib.calls == 2
+    for name in make(0):
+        with pytest.raises(ValueError):
+            call(p, **extra, **{**make(0), name: make(1)[name]})
+    assert lib.calls == 2
+    monkeypatch.setattr(binding, "_raw_stream", (lambda device: 0, lambda: 1))     # GPU 1 is the current one
+    t = make(0)
+    if call is attend:
+        with pytest.raises(ValueError):
+            M.mosaic_bsa_paged_fwd(p, *t.values())
+        M.mosaic_bsa_paged_fwd(p, *make(1).values())
+    else:
+        order = ("q", "k", "v", "q_weight", "k_weight", "q_lens", "k_lens", "page_table", "prefix_len", "q_out",
+                 "k_pages", "v_pages")
+        with pytest.raises(ValueError):
+            M.mosaic_bsa_paged_append(p, rot, None, *(t[n] for n in order))
+        M.mosaic_bsa_paged_append(p, rot, None, *(make(1)[n] for n in order))
+    assert lib.calls == 3
+
+
 @pytest.mark.parametrize("copied", [copy.copy, copy.deepcopy, lambda x: pickle.loads(pickle.dumps(x))])
 def test_copies_of_parameters(copied):
     p = params()
