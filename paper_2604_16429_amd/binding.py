@@ -647,13 +647,13 @@ def _device_of(t):
     return None if t is None or isinstance(t, int) else t.get_device()
 
 
-def _vector_on(device, name, t, size, dtype_name):
-    """_vector on one GPU."""
+def _vector_on(device, name, t, size, dtype):
+    """_vector on one GPU, of a torch dtype."""
     if t is None or isinstance(t, int):
         return t
-    if (t.numel() != size or t.dtype is not _named_dtype(dtype_name) or not t.is_contiguous() or
+    if (t.numel() != size or t.dtype is not dtype or not t.is_contiguous() or
             (t.get_device() != device if device is not None else not t.is_cuda)):
-        raise ValueError(f"{name}: {size} contiguous {dtype_name} values on the tensors' GPU expected")
+        raise ValueError(f"{name}: {size} contiguous {dtype} values on the tensors' GPU expected")
     return t.data_ptr()
 
 
@@ -673,6 +673,7 @@ def mosaic_bsa_paged_append(params: PagedParams, rotation: Rotation, positions, 
                             stream=None) -> None:
     h, kv, n, d = params.heads, params.kv_heads or params.heads, params.q_tokens, params.head_dim
     b, t, on = params.batch, params.page_tokens, _device_of(q)
+    i32, f32 = _named_dtype("int32"), _named_dtype("float32")
     pos, per = params._positions_of(rotation, positions, n)
     if pos is not positions and on is not None and positions.get_device() != on:
         raise ValueError("positions: on another GPU")
@@ -680,11 +681,11 @@ def mosaic_bsa_paged_append(params: PagedParams, rotation: Rotation, positions, 
         "append", ("q", q, h, n), ("k", k, kv, n), ("v", v, kv, n), ("out", q_out, h, n),
         ("k_pages", k_pages, kv, t), ("v_pages", v_pages, kv, t), position_batch=per, device=on)
     _check(load_library().mosaic_bsa_paged_append(
-        ref, rotation.ref, pos, q, k, v, _vector_on(on, "q_weight", q_weight, d, "float32"),
-        _vector_on(on, "k_weight", k_weight, d, "float32"), _vector_on(on, "q_lens", q_lens, b, "int32"),
-        _vector_on(on, "k_lens", k_lens, b, "int32"),
-        _vector_on(on, "page_table", page_table, b * params.table_pages, "int32"),
-        _vector_on(on, "prefix_len", prefix_len, 1, "int32"), q_out, k_pages, v_pages,
+        ref, rotation.ref, pos, q, k, v, _vector_on(on, "q_weight", q_weight, d, f32),
+        _vector_on(on, "k_weight", k_weight, d, f32), _vector_on(on, "q_lens", q_lens, b, i32),
+        _vector_on(on, "k_lens", k_lens, b, i32),
+        _vector_on(on, "page_table", page_table, b * params.table_pages, i32),
+        _vector_on(on, "prefix_len", prefix_len, 1, i32), q_out, k_pages, v_pages,
         _stream_on(on, stream)))
 
 
@@ -697,6 +698,7 @@ def mosaic_bsa_paged_fwd(params: PagedParams, q, k_pages, v_pages, q_lens, k_len
                          workspace_bytes=None) -> None:
     h, kv, n, b = params.heads, params.kv_heads or params.heads, params.q_tokens, params.batch
     t, on = params.page_tokens, _device_of(q)
+    i32, f32 = _named_dtype("int32"), _named_dtype("float32")
     wb = _nbytes(workspace) if workspace_bytes is None else workspace_bytes
     if on is not None and _device_of(workspace) not in (None, on):
         raise ValueError("workspace: on another device than the tensors")
@@ -706,9 +708,9 @@ def mosaic_bsa_paged_fwd(params: PagedParams, q, k_pages, v_pages, q_lens, k_len
     if params.prefix_tokens <= 0:
         prefix_table = None
     _check(load_library().mosaic_bsa_paged_fwd(
-        ref, q, k_pages, v_pages, _vector_on(on, "q_lens", q_lens, b, "int32"),
-        _vector_on(on, "k_lens", k_lens, b, "int32"),
-        _vector_on(on, "page_table", page_table, b * params.table_pages, "int32"),
-        _vector_on(on, "prefix_table", prefix_table, -(-params.prefix_tokens // max(t, 1)), "int32"),
-        _vector_on(on, "prefix_len", prefix_len, 1, "int32"), out,
-        _vector_on(on, "lse", lse, b * h * n, "float32"), _ptr(workspace), wb, _stream_on(on, stream)))
+        ref, q, k_pages, v_pages, _vector_on(on, "q_lens", q_lens, b, i32),
+        _vector_on(on, "k_lens", k_lens, b, i32),
+        _vector_on(on, "page_table", page_table, b * params.table_pages, i32),
+        _vector_on(on, "prefix_table", prefix_table, -(-params.prefix_tokens // max(t, 1)), i32),
+        _vector_on(on, "prefix_len", prefix_len, 1, i32), out,
+        _vector_on(on, "lse", lse, b * h * n, f32), _ptr(workspace), wb, _stream_on(on, stream)))

@@ -37,6 +37,13 @@ struct Step {
         return row * ROW + ((chunk ^ ((((row & 3) << 1) | ((row >> 2) & 1)) & (CHUNKS - 1))) << 4);
     }
 
+    // Four channels of a row's sums: 16 rows' same channels lie in different banks (without that, and with
+    // rows that are none, the sums of 16 wavefronts took 3 us)
+    static __device__ __forceinline__ int sums_at(int row, int quad)
+    {
+        return row * D * 4 + ((quad ^ (row & (D / 4 < 16 ? D / 4 - 1 : 15))) << 4);
+    }
+
     // Tiles t_a .. t_e - 1 for the given rows.  part: index of the first row's sums; negative: these are
     // all of them, the rows are stored.
     static __device__ __forceinline__ void walk(unsigned char* lds, const Args<T>& g, const Rows& rows,
@@ -281,9 +288,10 @@ struct Step {
             const float f = __builtin_amdgcn_exp2f(m_ref[nr] - top_of(16 * nr + l16));
             const float l = win::row_sum16(l_run[nr]) * f;
             if (grp == 0) l_s[(16 * nr + l16) * W + wave] = l;
+            if (16 * nr + l16 < rows.n)
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt)
-                *(f32x4*)(mine + ((16 * nr + l16) * D + 16 * dt + 4 * grp) * 4) = acc[nr][dt] * f;
+                for (int dt = 0; dt < DT; ++dt)
+                    *(f32x4*)(mine + sums_at(16 * nr + l16, 4 * dt + grp)) = acc[nr][dt] * f;
         }
         __syncthreads();
         const int quads = rows.n * (D / 4);
@@ -296,7 +304,7 @@ struct Step {
 #pragma unroll
             for (int w = 0; w < W; ++w) {
                 l += ls[w];
-                sum += *(const f32x4*)(lds + w * REGION + (r * D + c) * 4);
+                sum += *(const f32x4*)(lds + w * REGION + sums_at(r, c / 4));
             }
             if (part < 0) store_row<T, D>(g, row_at(s, rows, seq, r), c, sum, top, l);
             else store_part<D>(g.plan, part + r, c, sum, top, l);
