@@ -98,6 +98,7 @@ struct Chunk {
 };
 __device__ __forceinline__ Chunk chunk_at(const Shape& s, const Plan& plan, int w, int lane, bool record)
 {
+    constexpr int KEPT = kMostScanned / 64;
     const auto units = [&](int e) -> int {
         return e < plan.entries ? units_of(s, plan, sequence(s, plan.sequence_of(s, e)), plan.tile_of(s, e)) : 0;
     };
@@ -106,22 +107,27 @@ __device__ __forceinline__ Chunk chunk_at(const Shape& s, const Plan& plan, int 
         if (record && lane == 0) plan.found[w] = Entry{w, n};
         return Chunk{n > 0 ? w : -1, w, 1};
     }
-    int kept[2] = {0, 0}, all = 0;                     // units of up to 128 entries
-    for (int base = 0; base < plan.entries; base += 64) {
-        const int u = units(base + lane);
-        if (base < 128) kept[base >> 6] = u;
-        all += u;
+    int kept[KEPT], all = 0;                           // units of the first entries
+#pragma unroll
+    for (int i = 0; i < KEPT; ++i) {
+        kept[i] = 64 * i < plan.entries ? units(64 * i + lane) : 0;
+        all += kept[i];
     }
     const auto sum = [&](int x) { return __builtin_amdgcn_readlane(wave_scan(x), 63); };
     const auto chunks = [&](int e, int u, int per) { return e < plan.entries ? chunks_of(plan, u, per) : 0; };
-    const int per = chunk_units(plan, sum(all), plan.entries <= 128, [&](int c) {
-        return sum(chunks(lane, kept[0], c) + chunks(lane + 64, kept[1], c));
+    const int per = chunk_units(plan, sum(all), [&](int c) {
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < KEPT; ++i) n += chunks(64 * i + lane, kept[i], c);
+        return sum(n);
     });
     Chunk found = {-1, 0, 0};
     int run = 0;
-    for (int base = 0; base < plan.entries; base += 64) {
-        const int e = base + lane;
-        const int n = chunks(e, base == 0 ? kept[0] : base == 64 ? kept[1] : units(e), per);
+#pragma unroll
+    for (int i = 0; i < KEPT; ++i) {
+        const int base = 64 * i, e = base + lane;
+        if (base >= plan.entries) break;
+        const int n = chunks(e, kept[i], per);
         const int end = run + wave_scan(n), first = end - n;
         const uint64_t hit = __builtin_amdgcn_ballot_w64(w >= first && w < end);
         if (record && e < plan.entries) plan.found[e] = Entry{first, n};

@@ -1,5 +1,6 @@
 // Attention over a cache in pages: launches.  Which rows and tokens a workgroup takes is in
 // bsa_paged_plan.h.
+#include "bsa_paged_general.h"
 #include "bsa_paged_step.h"
 #include "bsa_paged_tile.h"
 
@@ -14,10 +15,34 @@ template <typename T, int D, int ROWS, int W, bool ONE>
 struct WalkOf {
     using Type = Step<T, D, ROWS / 16, W>;
 };
-template <int D, int W, bool ONE>
-struct WalkOf<uint16_t, D, 128, W, ONE> {
-    using Type = WideTile<D, ONE>;
+template <typename T, int D, int W, bool ONE>
+struct WalkOf<T, D, 128, W, ONE> {
+    using Type = GeneralTile<T, D>;
 };
+template <int W, bool ONE>
+struct WalkOf<uint16_t, 64, 128, W, ONE> {
+    using Type = WideTile<64, ONE>;
+};
+template <int W, bool ONE>
+struct WalkOf<uint16_t, 128, 128, W, ONE> {
+    using Type = WideTile<128, ONE>;
+};
+// bf16 at head dims 64 and 128: tiles of 128 rows where the rows of a load share a page.  Else only from as many
+// of them on as pay for giving up 32 rows whose tokens wavefronts share out.  us, 32 | 128 rows: bf16, head dim 32, 2 x
+// 8,192 read in, 512 workgroups, 338 | 231, 2 x 2,048, 256, 19 | 30; fp32, head dim 64, 2 x 4,096, 1,024,
+// 673 | 599, 16 x 40 on a prefix of 1,007, 256, 60 | 85; head dim 128, 4,096, 256, 428 | 407, 2 x 1,000, 128,
+// 420 | 298 (32 rows leave one wavefront a SIMD there).
+Kind kind_of(bool is_bf16, int D, const Shape& s, bool fit)
+{
+    const int waves = win::step_waves(is_bf16 ? 2 : 4, D);
+    Kind kind = {32, 32, waves, (is_bf16 ? 128 : 64) * waves};
+    if (is_bf16 && D >= 64) {
+        if (fit && (1 << s.page_shift) >= 1024 / (2 * D)) kind.most_own = kind.most_shared = 128;
+    } else if ((int64_t)s.batch * s.kv_heads * ((s.rows + 127) / 128) >= (D == 128 ? 128 : 512)) {
+        kind.most_own = 128;
+    }
+    return kind;
+}
 // Workgroups that a CU is to hold: as many as the registers of each kernel allow.
 template <typename T, int D, int ROWS, int W>
 constexpr int held_by_cu()
@@ -147,8 +172,7 @@ template <typename T, int D>
 hipError_t launch(const Shape& s, const void* q, const void* k, const void* v, void* out, float* lse,
                   void* workspace, hipStream_t stream)
 {
-    Kind kind = kind_of(sizeof(T) == 2, D, s);
-    kind.wide = kind.wide && strides_fit(s);
+    const Kind kind = kind_of(sizeof(T) == 2, D, s, strides_fit(s));
     Args<T> g = {(const T*)q, (const T*)k, (const T*)v, (T*)out, lse, s, make_plan(s, D, kind)};
     Plan& plan = g.plan;
     if (plan.parts) {
@@ -176,6 +200,9 @@ hipError_t launch(const Shape& s, const void* q, const void* k, const void* v, v
                      : own == 32 ? BSA_PAGED_WIDE(32, 128)
                                  : BSA_PAGED_WIDE(128, 128);
 #undef BSA_PAGED_WIDE
+    } else {
+        if (shared == 0 && own == 128) kernel = paged_kernel<T, D, 128, 0, 4>;
+        if (shared == 32 && own == 128) kernel = paged_kernel<T, D, 128, 32, 4>;
     }
     kernel<<<own_items + shared_items, 64 * plan.waves, 0, stream>>>(g, shared_items);
     hipError_t e = hipGetLastError();
@@ -194,10 +221,9 @@ size_t paged_fwd_workspace(bool is_bf16, int D, const paged::Shape& s)
 {
     using namespace paged;
     // (which kernels run depends on strides as well: enough for both)
-    Kind kind = kind_of(is_bf16, D, s);
     size_t most = 0;
-    for (int i = 0; i < 2; ++i, kind.wide = false) {
-        const Plan p = make_plan(s, D, kind);
+    for (const bool fit : {false, true}) {
+        const Plan p = make_plan(s, D, kind_of(is_bf16, D, s, fit));
         const size_t n = p.parts ? (size_t)p.all_parts(s) * (D + 2) * sizeof(float) + p.entries * sizeof(Entry) : 0;
         if (n > most) most = n;
     }

@@ -93,7 +93,8 @@ struct Tiles {
 // at most `chunks` of them.  Lengths are in device memory: workgroups find c and their chunk by sums over
 // the entries.
 constexpr int kUnit = 128, kLeast = 2;     // c is kLeast at least
-constexpr int kMostScanned = 2048;         // entries; more have a chunk each
+constexpr int kMostScanned = 256;          // entries; more have a chunk each (400 sequences of up to 2,000, 2 heads:
+                                           // 106 us, looked up 118; 130 of up to 4,000, 4 heads: 88, looked up 77)
 struct Entry {
     int32_t first, chunks;
 };
@@ -146,16 +147,15 @@ __host__ __device__ inline int chunks_of(const Plan& plan, int units, int per_ch
     const int n = (int)((uint32_t)(units + per_chunk - 1) / (uint32_t)per_chunk);
     return n > 0 || plan.stacked ? n : 1;
 }
-// The least c for which `all` units make no more chunks than there is room for: total(c) of them.  Without
-// `exact` a c that is large enough.
+// The least c for which `all` units make no more chunks than there is room for: total(c) of them.
 template <class Total>
-__host__ __device__ inline int chunk_units(const Plan& plan, int all, bool exact, Total total)
+__host__ __device__ inline int chunk_units(const Plan& plan, int all, Total total)
 {
     const int room = plan.chunks - plan.entries;       // (each entry's last chunk may be short)
     int lo = (all + plan.chunks - 1) / plan.chunks, hi = (all + room - 1) / room;
     lo = lo > kLeast ? lo : kLeast;
     hi = hi > kLeast ? hi : kLeast;
-    while (exact && lo < hi) {
+    while (lo < hi) {
         const int mid = (lo + hi) / 2;
         if (total(mid) <= plan.chunks) hi = mid;
         else lo = mid + 1;
@@ -163,17 +163,14 @@ __host__ __device__ inline int chunk_units(const Plan& plan, int all, bool exact
     return hi;
 }
 
-// What decides beside the shape: whether bsa_paged_tile.h takes more than 32 rows, and how many wavefronts a
+// What decides beside the shape: the largest tiles of a sequence's rows and of those of all, and how many wavefronts a
 // workgroup has that takes all of up to `few` tokens of up to 16 rows.
 struct Kind {
-    bool wide;
+    int most_own, most_shared;
     int waves, few;
 };
 // Rows of a workgroup's tile, by how many there are.
-inline int tile_rows_of(int64_t rows, const Kind& kind)
-{
-    return rows <= 16 ? 16 : rows <= 32 || !kind.wide ? 32 : 128;
-}
+inline int tile_rows_of(int64_t rows, int most) { return rows <= 16 ? 16 : rows <= 32 ? 32 : most; }
 // Most tokens that a sequence's list can hold.
 inline int64_t most_tokens(const Shape& s, bool stacked)
 {
@@ -186,29 +183,32 @@ inline Plan make_plan(const Shape& s, int D, const Kind& kind)
 {
     Plan p = {};
     p.waves = 4;
-    p.tile = tile_rows_of(s.rows, kind);
+    p.tile = tile_rows_of(s.rows, kind.most_own);
     p.tile_rows = p.tile < s.rows ? p.tile : s.rows;
     p.row_tiles = (s.rows + p.tile - 1) / p.tile;
     p.entries = p.chunks = s.batch * p.row_tiles;
     p.all_rows = 1;
     const int64_t own = (int64_t)s.table_pages << s.page_shift, slices = (int64_t)s.batch * s.kv_heads;
+    // (few tokens and rows: one launch, which the joining would double)
     const bool shares = s.batch > 1 && s.prefix_tokens >= 256 && s.rows < 128 && s.left >= s.prefix_tokens + own;
     if (s.rows <= 16 && kind.waves > 4 && most_tokens(s, false) <= kind.few && (!shares || slices <= 256)) {
         p.waves = kind.waves;
         return p;
     }
-    // Workgroups that the chip holds at once.
+    // Workgroups that the chip holds at once: chunks and shares are as many as fill it once, of at least 256
+    // tokens, 384 where a share's sums are those of 128 rows.  us: 24 members on 28,800, shares of 256 39, 384
+    // 33, 768 43; 8 chunks of up to 100 tokens on 14,000, 512 chunks 112, 768 100.
     const int64_t wide_held = D == 64 ? 768 : 512;
     int64_t shared_items = 0;
     p.stacked = shares;
     if (p.stacked) {
         p.all_rows = s.batch * s.rows;
-        p.shared_tile = tile_rows_of(p.all_rows, kind);
+        p.shared_tile = tile_rows_of(p.all_rows, kind.most_shared);
         const int tokens = p.shared_tile == 128 ? 384 : 256;
         const int64_t items = (int64_t)s.kv_heads * ((p.all_rows + p.shared_tile - 1) / p.shared_tile);
         int64_t n = wide_held / items;
         if (n > s.prefix_tokens / tokens) n = s.prefix_tokens / tokens;
-        if (n > 64) n = 64;
+        if (n > 64) n = 64;                            // (what the joining asks for at once)
         p.shared_splits = n < 1 ? 1 : n >= 8 ? (int)n & ~7 : (int)n;
         shared_items = items * p.shared_splits;
     }

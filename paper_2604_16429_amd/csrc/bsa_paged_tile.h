@@ -16,13 +16,7 @@ namespace bsa {
 
 namespace paged {
 
-// Whether rows of a load share a page, which the shape decides, and whether 31 bits reach from the first to
-// the last row of a tile and 32 hold a page's stride.
-inline Kind kind_of(bool is_bf16, int D, const Shape& s)
-{
-    const int waves = win::step_waves(is_bf16 ? 2 : 4, D);
-    return Kind{is_bf16 && D >= 64 && (1 << s.page_shift) >= 1024 / (2 * D), waves, (is_bf16 ? 128 : 64) * waves};
-}
+// Whether 31 bits reach from the first to the last row of a tile and 32 hold a page's stride.
 inline bool strides_fit(const Shape& s)
 {
     return s.k.token < 1 << 24 && s.v.token < 1 << 24 && s.k.batch >> 32 == 0 && s.v.batch >> 32 == 0;

@@ -148,6 +148,19 @@ def test_entries_that_name_no_page(dtype, N):
     run(dtype, 2, 4, 2, N, 64, 16, [30, 70], bad=[(0, 0), (0, 1)], q_lens=[min(N, 30), N], seed=N)
 
 
+@pytest.mark.parametrize("dtype,D", [(BF16, 32), (FP32, 32), (FP32, 64), (FP32, 128), (BF16, 64)])
+@pytest.mark.parametrize("kw", [
+    dict(B=8, N=70, own=[70, 71, 100, 3, 150, 64, 1, 200], q_lens=[70, 70, 69, 3, 1, 64, 0, 33], T=8),
+    dict(B=8, N=70, own=[70, 71, 100, 3, 150, 64, 1, 200], q_lens=[70, 70, 69, 3, 1, 64, 0, 33], T=64, prefix=75,
+         bad=[(-1, 0), (2, 1), (7, 1), (4, 0)]),
+    dict(B=8, N=70, own=[70, 300, 100, 3, 150, 64, 1, 200], T=4, left=40, sinks=5),
+    dict(B=16, N=50, own=[50 + 3 * b for b in range(16)], T=16, prefix=300),
+    dict(B=8, N=70, own=[700, 300, 100, 3, 650, 64, 1, 200], T=32)])
+def test_many_tiles_of_rows(dtype, D, kw):
+    """As many as fill the chip without the tokens' being shared out."""
+    run(dtype, h=32, kv=16, D=D, seed=D, **kw)
+
+
 @TYPES
 def test_scores_of_any_size(dtype):
     run(dtype, 2, 4, 2, 2, 64, 16, [200, 90], prefix=64, amplitude=60.0, seed=3)

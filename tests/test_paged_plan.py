@@ -48,7 +48,7 @@ extern "C" int64_t plan_of(const int32_t* shape, const int32_t* lens, int32_t* o
     s.prefix_tokens = shape[5];
     s.left = shape[6];
     s.sinks = shape[7];
-    const Plan p = make_plan(s, shape[10], Kind{shape[8] != 0, shape[9], 128 * shape[9]});
+    const Plan p = make_plan(s, shape[10], Kind{shape[8], shape[11], shape[9], 128 * shape[9]});
     const int32_t v[] = {p.chunks, p.scanned, p.stacked, p.shared_splits, p.parts, p.entries, p.all_rows, p.tile_rows,
                          p.tile, p.row_tiles};
     for (int i = 0; i < 10; ++i) out[i] = v[i];
@@ -64,7 +64,7 @@ extern "C" int64_t plan_of(const int32_t* shape, const int32_t* lens, int32_t* o
             for (int e = 0; e < p.entries; ++e) n += chunks_of(p, units(e), c);
             return n;
         };
-        const int per = chunk_units(p, all, p.entries <= 128, total);
+        const int per = chunk_units(p, all, total);
         out[10] = per;
         out[11] = per > kLeast ? total(per - 1) : -1;
         for (int e = 0; e < p.entries; ++e) chunks[e] = chunks_of(p, units(e), per);
@@ -101,13 +101,13 @@ def test_chunks_fit(plan):
     """Whatever the lengths, all chunks have a place, and each tile of rows that needs one has one."""
     plan.plan_of.restype = ctypes.c_int64
     rng = random.Random(0)
-    seen = {"scanned": 0, "stacked": 0, "exact": 0}
+    seen = {"scanned": 0, "stacked": 0}
     for _ in range(1500):
         B, q_tokens = rng.choice([1, 2, 7, 64, 300, 1024, 2500]), rng.choice([1, 1, 1, 5, 40, 1000])
         shape = [B, rng.choice([1, 2, 4, 8, 16]), q_tokens, rng.choice([1, 2, 8]),
                  rng.choice([1, 100, 1000, 30000, 1 << 20, (1 << 29) - 1]), rng.choice([0, 0, 300, 20000, (1 << 29) - 1]),
-                 rng.choice([UNBOUNDED, UNBOUNDED, 1000]), rng.choice([0, 4]), rng.randint(0, 1),
-                 rng.choice([4, 8, 16]), rng.choice([32, 64, 128])]
+                 rng.choice([UNBOUNDED, UNBOUNDED, 1000]), rng.choice([0, 4]), rng.choice([32, 128]),
+                 rng.choice([4, 8, 16]), rng.choice([32, 64, 128]), rng.choice([32, 128])]
         own, prefix = shape[4], shape[5]
         lens = np.array([[rng.choice([0, 1, q_tokens]), rng.choice([0, 1, own, rng.randint(0, own)]), prefix]
                          for _ in range(B)], dtype=np.int32)
@@ -124,9 +124,7 @@ def test_chunks_fit(plan):
         if scanned:
             assert total > entries and int(chunks.sum()) <= total
             assert int(chunks[:entries].min()) >= (0 if stacked else 1)
-            if entries <= 128:
-                assert below == -1 or below > total        # no smaller chunk would do
-                seen["exact"] += 1
+            assert below == -1 or below > total            # no smaller chunk would do
         else:
             assert total == entries
         seen["scanned"] += scanned
