@@ -118,17 +118,8 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const Args<T> g, uint32
     const int slice_row = (int)(blockIdx.x - (uint32_t)b * row_groups) * PER + slot;     // (key/value head, row)
     const int a = min(slice_row / s.rows, s.kv_heads - 1), row = slice_row - a * s.rows;
     const int tile = min(row, s.rows - 1) / plan.tile;
-    const Row x = row_at(s, Rows{row, 1, a, b}, sequence(s, b), 0);
     const Entry entry = plan.found[plan.entry_of(s, b, tile)];
-    // (one chunk and nothing else: stored by its workgroup)
-    const bool there = row < s.rows && (plan.stacked || entry.chunks != 1);
-    const int shared = plan.stacked ? plan.shared_splits : 0;
-    const int parts = there ? shared + entry.chunks : 0;
-    const int64_t shared0 = plan.shared_part(s, a, 0, b * s.rows + row);
-    const int64_t own0 = plan.own_part(a, entry.first) + row - tile * plan.tile;
-    auto part = [&](int i) -> int64_t {
-        return i < shared ? shared0 + (int64_t)i * plan.all_rows : own0 + (int64_t)(i - shared) * plan.tile_rows;
-    };
+    const Row x = row_at(s, Rows{row, 1, a, b}, sequence(s, b), 0);
     float top = kNoRef, l = 0.0f;
     f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
     const auto add = [&](float m, float l_part, const f32x4& v) {
@@ -139,20 +130,29 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const Args<T> g, uint32
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum[e] = fmaf(f, v[e], sum[e] * f0);
     };
-    constexpr int AHEAD = 8;                           // parts asked for at once
-    for (int i0 = pg; i0 < parts; i0 += PG * AHEAD) {
-        float2 ml[AHEAD];
-        f32x4 v[AHEAD];
+    // n parts from `first` on, each `step` rows behind the one before; AHEAD of them are asked for at once
+    const auto take = [&](int64_t first, int64_t step, int n) {
+        constexpr int AHEAD = 8;
+        for (int i0 = pg; i0 < n; i0 += PG * AHEAD) {
+            float2 ml[AHEAD];
+            f32x4 v[AHEAD];
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-            const int64_t x = part(min(i0 + PG * u, parts - 1));
-            ml[u] = plan.ml[x];
-            v[u] = *(const f32x4*)(plan.acc + x * D + 4 * at);
+            for (int u = 0; u < AHEAD; ++u)
+                if (i0 + PG * u < n) {
+                    const int64_t part = first + (i0 + PG * u) * step;
+                    ml[u] = plan.ml[part];
+                    v[u] = *(const f32x4*)(plan.acc + part * D + 4 * at);
+                }
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u)
+                if (i0 + PG * u < n) add(ml[u].x, ml[u].y, v[u]);
         }
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u)
-            if (i0 + PG * u < parts) add(ml[u].x, ml[u].y, v[u]);
-    }
+    };
+    const bool exists = row < s.rows;
+    if (plan.stacked) take(plan.shared_part(s, a, 0, b * s.rows + row), plan.all_rows, exists ? plan.shared_splits : 0);
+    // (one chunk and nothing else: stored by its workgroup)
+    const bool there = exists && (plan.stacked || entry.chunks != 1);
+    take(plan.own_part(a, entry.first) + row - tile * plan.tile, plan.tile_rows, there ? entry.chunks : 0);
     if constexpr (PG > 1) {
         sum_s[pg][slot * LANES + at] = sum;
         ml_s[pg][slot * LANES + at] = make_float2(top, l);
@@ -207,10 +207,13 @@ hipError_t launch(const Shape& s, const void* q, const void* k, const void* v, v
     kernel<<<own_items + shared_items, 64 * plan.waves, 0, stream>>>(g, shared_items);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !plan.parts) return e;
-    const bool many = plan.shared_splits + plan.chunks / plan.entries > 8;
-    const int per = many ? 256 / (D / 4 * 8) : 256 / (D / 4);
+    // as many groups as leave each some eight parts of a row
+    const int parts = plan.shared_splits + plan.chunks / plan.entries, groups = parts > 40 ? 8 : parts > 8 ? 4 : 1;
+    const int per = 256 / (D / 4 * groups);
     const uint32_t row_groups = (uint32_t)((s.kv_heads * s.rows + per - 1) / per);
-    auto join = many ? paged_join_kernel<T, D, 8> : paged_join_kernel<T, D, 1>;
+    auto join = groups == 8   ? paged_join_kernel<T, D, 8>
+                : groups == 4 ? paged_join_kernel<T, D, 4>
+                              : paged_join_kernel<T, D, 1>;
     join<<<row_groups * (uint32_t)s.batch, 256, 0, stream>>>(g, row_groups);
     return hipGetLastError();
 }
