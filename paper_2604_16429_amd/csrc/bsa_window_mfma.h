@@ -8,21 +8,22 @@ namespace bsa {
 namespace win {
 
 // Rows of D channels in LDS, as one load of a wavefront leaves 1 KiB of them (a slab of 4 or 8 rows).
-// LDS serves 16 lanes of 16 bytes at once if they lie in different sixteenths of 256 bytes.  Row
-// fragments take one 16-byte chunk of 16 consecutive rows, transposing reads four chunks of 4
-// rows: a row's chunks are permuted by its place in the slab such that four rows have the four in
-// different quarters, and every slab is shifted by 16 bytes against the one before, which tells apart
-// the 16 rows.  (A permutation by the row modulo 8 alone left half of the LDS cycles in
-// conflicts: 1.5 degrees, head dim 128, window 1,024: forward 1,171 us, dQ 1,480, dK/dV 1,990.)
+// LDS serves 16 lanes of 16 bytes at once if they lie in different sixteenths of 256 bytes: lanes 0 to 3, 12 to 15, 20 to
+// 23 and 24 to 27 of 32, then the others.  Row fragments take one 16-byte chunk of those rows, transposing
+// reads four chunks of 4 rows: a row's chunks are permuted by its place in the slab such that four rows have the
+// four in different quarters, and every slab is shifted against the one before, by 16 bytes, at head dim 64, where
+// a slab has twice four rows, whose chunks differ by their lowest bit as well, by 32.  (A permutation by the row modulo 8
+// alone left half of the LDS cycles in conflicts: 1.5 degrees, head dim 128, window 1,024: forward 1,171 us, dQ
+// 1,480, dK/dV 1,990.  Head dim 64 with 16 bytes and the second bit: a third of them, backward 2 to 3 % slower.)
 template <int D>
 struct Rows {
     static constexpr int ROW_BYTES = 2 * D, CHUNKS = ROW_BYTES / 16, PER_SLAB = 1024 / ROW_BYTES;
-    static constexpr int SLAB = 1024 + 16;
+    static constexpr int SLAB = 1024 + (D == 64 ? 32 : 16);
     static constexpr int bytes(int rows) { return rows / PER_SLAB * SLAB; }
     static __device__ __forceinline__ int swizzled(int row, int chunk)
     {
         if (D == 128) return chunk ^ ((row & 3) << 2);
-        return chunk ^ (((row >> 1) & 1) << 2) ^ (((row >> 2) & 1) << 1);
+        return chunk ^ (((row >> 1) & 1) << 2) ^ ((row >> 2) & 1);
     }
     static __device__ __forceinline__ int place(int row, int chunk)
     {
