@@ -167,6 +167,12 @@ def test_scores_of_any_size(dtype):
     run(dtype, 2, 4, 2, 2, 128, 16, [200, 90], prefix=64, scale=1e-6, seed=4)
 
 
+def test_largest_pages():
+    run(BF16, 2, 4, 2, 1, 32, 65536, [300, 70], prefix=400, seed=1)
+    run(FP32, 2, 4, 2, 40, 32, 65536, [300, 70], prefix=20, seed=2)
+    run(BF16, 2, 4, 2, 40, 64, 65536, [300, 70], prefix=20, seed=3)
+
+
 def cache_on_the_gpu(B, kv, T, D, own, prefix, dtype=BF16, spare=0):
     """A cache of torch.randn without a copy on the CPU, pages in order."""
     gen = torch.Generator(device="cuda").manual_seed(7)
@@ -328,3 +334,26 @@ def test_streams_as_objects():
         M.mosaic_bsa_paged_fwd(p, q, k, v, None, lens, table, prefix_table, None, out, stream=stream)
     torch.cuda.synchronize()
     assert torch.equal(*outs)
+
+
+@TYPES
+@pytest.mark.parametrize("N", [1, 40])
+def test_inputs_that_share_memory(dtype, N):
+    """Key/value heads that are one (stride 0), queries that all sequences share, kv_heads left at 0."""
+    import paper_2604_16429_amd as M
+    from paper_2604_16429_amd import binding
+    k, v, table, prefix_table = cache_on_the_gpu(3, 1, 16, 64, 100, 40, dtype)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    q = torch.randn(1, 4, N, 64, device="cuda", generator=gen).to(dtype)
+    p = M.PagedParams(3, 4, N, 64, k.shape[0], 16, table.shape[1], binding.BF16 if dtype is BF16 else binding.F32,
+                      prefix_tokens=40)
+    lens = torch.tensor([100, 60, 41], dtype=torch.int32, device="cuda")
+    ws = torch.empty(max(M.mosaic_bsa_paged_workspace_bytes(p), 256), dtype=torch.uint8, device="cuda")
+    outs = []
+    for real in (False, True):
+        a = [x.expand(-1, 4, -1, -1) for x in (k, v)] + [q.expand(3, -1, -1, -1)]
+        a = [x.contiguous() for x in a] if real else a
+        out = torch.empty(3, 4, N, 64, dtype=dtype, device="cuda")
+        M.mosaic_bsa_paged_fwd(p, a[2], a[0], a[1], None, lens, table, prefix_table, None, out, workspace=ws)
+        outs.append(out)
+    assert torch.equal(*outs) and bool(outs[0].isfinite().all())

@@ -127,6 +127,10 @@ def test_chunks_fit(plan):
             assert below == -1 or below > total            # no smaller chunk would do
         else:
             assert total == entries
+        # a launch holds fewer than 2^32 work items, as far as the entry point lets sizes through
+        if B * shape[3] * -(-rows // 32) < 1 << 21:
+            shared = splits * shape[3] * -(-all_rows // (128 if shape[11] == 128 and all_rows > 32 else 16))
+            assert (total * shape[3] + (shared if stacked else 0)) * 64 * (4 if parts else shape[9]) < 1 << 32
         seen["scanned"] += scanned
         seen["stacked"] += stacked
     assert min(seen.values()) > 100
