@@ -28,17 +28,19 @@ struct WalkOf<uint16_t, 128, 128, W, ONE> {
     using Type = WideTile<128, ONE>;
 };
 // bf16 at head dims 64 and 128: tiles of 128 rows where the rows of a load share a page.  Else only from as many
-// of them on as pay for giving up 32 rows whose tokens wavefronts share out.  us, 32 | 128 rows: bf16, head dim 32, 2 x
-// 8,192 read in, 512 workgroups, 338 | 231, 2 x 2,048, 256, 19 | 30; fp32, head dim 64, 2 x 4,096, 1,024,
-// 673 | 599, 16 x 40 on a prefix of 1,007, 256, 60 | 85; head dim 128, 4,096, 256, 428 | 407, 2 x 1,000, 128,
-// 420 | 298 (32 rows leave one wavefront a SIMD there).
+// of them on, and of their tokens, as pay for giving up 32 rows whose tokens wavefronts share out.  us, 32 | 128 rows: bf16,
+// head dim 32, 2 x 8,192 read in, 512 workgroups, 338 | 231, 2 x 2,048, 256, 19 | 28; fp32, head dim 64, 2 x
+// 4,096, 1,024, 673 | 599, 16 x 40 on a prefix of 1,007, 256, 60 | 85, 4 x 1,796 on up to 7,090 tokens, 116, 252 | 217,
+// 2 x 300 on up to 20,000, 20, 210 | 257; head dim 128, where 32 rows leave one wavefront a SIMD, 2 x 376 on 36,894 tokens,
+// 48, 1,934 | 1,087, 64 on 3,000, 4, 26 | 48.
 Kind kind_of(bool is_bf16, int D, const Shape& s, bool fit)
 {
     const int waves = win::step_waves(is_bf16 ? 2 : 4, D);
     Kind kind = {32, 32, waves, (is_bf16 ? 128 : 64) * waves};
     if (is_bf16 && D >= 64) {
         if (fit && (1 << s.page_shift) >= 1024 / (2 * D)) kind.most_own = kind.most_shared = 128;
-    } else if ((int64_t)s.batch * s.kv_heads * ((s.rows + 127) / 128) >= (D == 128 ? 128 : 512)) {
+    } else if (const int64_t tiles = (int64_t)s.batch * s.kv_heads * ((s.rows + 127) / 128);
+               tiles >= (D == 128 ? 32 : most_tokens(s, false) >= 4096 ? 96 : 512)) {
         kind.most_own = 128;
     }
     return kind;
