@@ -197,17 +197,21 @@ inline Plan make_plan(const Shape& s, int D, const Kind& kind)
     }
     // Workgroups that the chip holds at once: chunks and shares are as many as fill it once, of at least 256
     // tokens, 384 where a share's sums are those of 128 rows.  us: 24 members on 28,800, shares of 256 39, 384
-    // 33, 768 43; 8 chunks of up to 100 tokens on 14,000, 512 chunks 112, 768 100.
+    // 33, 768 43; 4 x 5 tokens on 4,000, of 192 18, 384 24; 8 chunks of up to 100 tokens on 14,000, 512 chunks
+    // 112, 768 100.
     const int64_t wide_held = D == 64 ? 768 : 512;
     int64_t shared_items = 0;
     p.stacked = shares;
     if (p.stacked) {
         p.all_rows = s.batch * s.rows;
         p.shared_tile = tile_rows_of(p.all_rows, kind.most_shared);
-        const int tokens = p.shared_tile == 128 ? 384 : 256;
         const int64_t items = (int64_t)s.kv_heads * ((p.all_rows + p.shared_tile - 1) / p.shared_tile);
-        int64_t n = wide_held / items;
-        if (n > s.prefix_tokens / tokens) n = s.prefix_tokens / tokens;
+        const auto splits = [&](int64_t workgroups, int tokens) -> int64_t {
+            return workgroups / items < s.prefix_tokens / tokens ? workgroups / items : s.prefix_tokens / tokens;
+        };
+        int64_t n = splits(wide_held, p.shared_tile == 128 ? 384 : 256);
+        // (smaller shares where they leave half of the chip to the own tokens)
+        if (p.shared_tile == 128 && n < splits(wide_held / 2, 192)) n = splits(wide_held / 2, 192);
         if (n > 64) n = 64;                            // (what the joining asks for at once)
         p.shared_splits = n < 1 ? 1 : n >= 8 ? (int)n & ~7 : (int)n;
         shared_items = items * p.shared_splits;
