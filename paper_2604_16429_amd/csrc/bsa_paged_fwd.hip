@@ -35,8 +35,13 @@ struct WalkOf<uint16_t, 128, 128, W, ONE> {
 // 48, 1,934 | 1,087, 64 on 3,000, 4, 26 | 48.
 Kind kind_of(bool is_bf16, int D, const Shape& s, bool fit)
 {
+    // Tokens of up to 16 rows that stay in one workgroup.  us, in one | split: bf16, head dim 64, 16 slices, 1,000 tokens
+    // 10.9 | 11.0, 2,000 15.5 | 11.1, 128 slices, 2,000 17 | 22, 4,000 26 | 30; head dim 128, 16 slices, 600 11.1 | 11.8,
+    // 1,000 15.7 | 12.3; fp32, head dim 32, 16 slices, 600 9.8 | 11.1, 1,000 12.5 | 11.1, 128 slices, head dim 64, 600
+    // 15 | 18.
     const int waves = win::step_waves(is_bf16 ? 2 : 4, D);
-    Kind kind = {32, 32, waves, (is_bf16 ? 128 : 64) * waves};
+    const bool many = (int64_t)s.batch * s.kv_heads >= 128;
+    Kind kind = {32, 32, waves, waves * (is_bf16 ? many ? 256 : 72 : many ? 128 : 48), 2 * D * (is_bf16 ? 2 : 4)};
     if (is_bf16 && D >= 64) {
         if (fit && (1 << s.page_shift) >= 1024 / (2 * D)) kind.most_own = kind.most_shared = 128;
     } else if (const int64_t tiles = (int64_t)s.batch * s.kv_heads * ((s.rows + 127) / 128);

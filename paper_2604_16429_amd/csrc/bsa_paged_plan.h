@@ -163,11 +163,12 @@ __host__ __device__ inline int chunk_units(const Plan& plan, int all, Total tota
     return hi;
 }
 
-// What decides beside the shape: the largest tiles of a sequence's rows and of those of all, and how many wavefronts a
-// workgroup has that takes all of up to `few` tokens of up to 16 rows.
+// What decides beside the shape: the largest tiles of a sequence's rows and of those of all, how many wavefronts a
+// workgroup has that takes all of up to `few` tokens of up to 16 rows, and the bytes of a key and a value.
 struct Kind {
     int most_own, most_shared;
     int waves, few;
+    int token_bytes;
 };
 // Rows of a workgroup's tile, by how many there are.
 inline int tile_rows_of(int64_t rows, int most) { return rows <= 16 ? 16 : rows <= 32 ? 32 : most; }
@@ -188,10 +189,15 @@ inline Plan make_plan(const Shape& s, int D, const Kind& kind)
     p.row_tiles = (s.rows + p.tile - 1) / p.tile;
     p.entries = p.chunks = s.batch * p.row_tiles;
     p.all_rows = 1;
-    const int64_t own = (int64_t)s.table_pages << s.page_shift, slices = (int64_t)s.batch * s.kv_heads;
-    // (few tokens and rows: one launch, which the joining would double)
-    const bool shares = s.batch > 1 && s.prefix_tokens >= 256 && s.rows < 128 && s.left >= s.prefix_tokens + own;
-    if (s.rows <= 16 && kind.waves > 4 && most_tokens(s, false) <= kind.few && (!shares || slices <= 256)) {
+    const int64_t own = (int64_t)s.table_pages << s.page_shift;
+    // The prefix is worked on for all together where that saves 24 MB of reads and more, mostly from L2: less does
+    // not pay for joining.  us, apart | together: 16 rows of all, head dim 128, 4 sequences on 2,000 (12 MB) 12.6 |
+    // 15.0, on 8,000 (49 MB) 21 | 15; head dim 64, 16 on 2,000 (30 MB) 16.7 | 16.7, on 8,000 25 | 15; fp32, 6 on 1,501 (4 MB)
+    // 12.0 | 14.6; 24 members on 28,800 72 | 29.
+    const int64_t saved = (int64_t)(s.batch - 1) * s.prefix_tokens * s.kv_heads * kind.token_bytes;
+    p.stacked = s.prefix_tokens >= 256 && saved >= 24000000 && s.rows < 128 && s.left >= s.prefix_tokens + own;
+    // (few rows and tokens: one launch)
+    if (!p.stacked && s.rows <= 16 && kind.waves > 4 && most_tokens(s, false) <= kind.few) {
         p.waves = kind.waves;
         return p;
     }
@@ -201,7 +207,6 @@ inline Plan make_plan(const Shape& s, int D, const Kind& kind)
     // 112, 768 100.
     const int64_t wide_held = D == 64 ? 768 : 512;
     int64_t shared_items = 0;
-    p.stacked = shares;
     if (p.stacked) {
         p.all_rows = s.batch * s.rows;
         p.shared_tile = tile_rows_of(p.all_rows, kind.most_shared);
@@ -219,7 +224,7 @@ inline Plan make_plan(const Shape& s, int D, const Kind& kind)
     const int64_t tokens = most_tokens(s, p.stacked), units = (tokens + 31) / 32 / (kUnit / 32) + 2;
     const int64_t held = p.tile == 128 || p.shared_tile == 128 ? wide_held : p.tile == 16 ? 1024 : 512;
     if (p.entries <= kMostScanned && p.entries * units < 1 << 30 && (int64_t)p.entries * s.kv_heads < held &&
-        tokens >= 640) {
+        tokens >= 384) {
         int64_t n = (held - shared_items) / s.kv_heads;
         if (n < 2 * (int64_t)p.entries) n = 2 * (int64_t)p.entries;
         const int64_t most = p.entries * ((units + kLeast - 1) / kLeast);

@@ -58,13 +58,15 @@ class Cache:
 
     def sequence(self, b, kl, prefix):
         """(k, v) [kv, tokens, D] in 64 bits and which tokens have a page."""
-        where = [(-1, j) for j in range(prefix)] + [(b, o) for o in range(kl)]
-        k = torch.zeros(self.kv, len(where), self.D, dtype=torch.float64)
-        v, there = torch.zeros_like(k), torch.ones(len(where), dtype=torch.bool)
-        for j, (who, o) in enumerate(where):
-            there[j] = (who, o // self.T) not in self.hidden
-            page = (self.true_prefix_table if who < 0 else self.true_table[who])[o // self.T]
-            k[:, j], v[:, j] = self.k64[page, :, o % self.T], self.v64[page, :, o % self.T]
+        page, row, there = [], [], []
+        for who, tokens, names in ((-1, prefix, self.true_prefix_table), (b, kl, self.true_table[b])):
+            for i in range(-(-tokens // self.T)):
+                n = min(self.T, tokens - i * self.T)
+                page += [names[i]] * n
+                row += range(n)
+                there += [(who, i) not in self.hidden] * n
+        k, v = (x[page, :, row].transpose(0, 1) for x in (self.k64, self.v64))
+        there = torch.tensor(there, dtype=torch.bool)
         return k, v, there
 
 

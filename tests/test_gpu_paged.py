@@ -87,7 +87,39 @@ def test_prefixes(dtype, B, N, h, kv, D, P, own):
     run(dtype, B, h, kv, N, D, 16, own, prefix=P, seed=B + P)
 
 
-@pytest.mark.parametrize("B,most,prefix", [(65, 1500, 0), (70, 900, 300), (130, 1000, 0), (200, 700, 0), (1030, 40, 260)])
+@pytest.mark.parametrize("dtype,B,N,h,kv,D,P,own,T", [
+    # the rows of all sequences together in tiles of 16, 32 and 128, a sequence's own in 16, 32 and 128
+    (BF16, 4, 1, 4, 4, 128, 4001, [1, 0, 300, 40], 16),
+    (BF16, 8, 1, 16, 4, 128, 1700, [9, 700, 1, 64, 65, 0, 3, 1000], 64),
+    (BF16, 17, 1, 8, 1, 128, 3003, [11 * i for i in range(17)], 8),
+    (BF16, 24, 1, 8, 2, 64, 2100, [50 * i for i in range(24)], 32),
+    (BF16, 40, 2, 4, 1, 64, 2500, [2 + i for i in range(40)], 256),
+    (BF16, 8, 5, 8, 2, 128, 3350, [5, 7, 0, 3, 900, 64, 1, 128], 16),
+    (BF16, 8, 5, 8, 2, 64, 6800, [5, 7, 0, 3, 900, 64, 1, 128], 128),
+    (BF16, 8, 10, 8, 2, 128, 3377, [10, 70, 11, 33, 900, 64, 2, 128], 64),
+    (BF16, 8, 12, 8, 2, 64, 6777, [12, 70, 11, 33, 900, 64, 2, 128], 8),
+    (BF16, 8, 12, 8, 2, 64, 6777, [12, 70, 11, 33, 900, 64, 2, 128], 4),
+    (BF16, 20, 1, 16, 8, 32, 1300, [3 * i for i in range(20)], 16),
+    (FP32, 4, 1, 4, 4, 128, 2000, [1, 0, 300, 40], 16),
+    (FP32, 20, 1, 8, 4, 32, 1301, [3 * i for i in range(20)], 8),
+    (FP32, 9, 3, 8, 2, 64, 3001, [3 + 100 * i for i in range(9)], 64),
+    (FP32, 16, 50, 16, 8, 64, 4101, [50 + i for i in range(16)], 32),
+])
+def test_prefixes_for_all_together(dtype, B, N, h, kv, D, P, own, T):
+    """As many sequences, or as long a prefix, that it is read for all of them together."""
+    q_lens = [max(0, N - b % (N + 1)) for b in range(B)]
+    run(dtype, B, h, kv, N, D, T, own, prefix=P, q_lens=q_lens, order="tokens" if B == 8 else "heads", seed=B + P)
+    if N < 50:
+        run(dtype, B, h, kv, N, D, T, own, prefix=P, bad=[(-1, 0), (-1, (P - 1) // T), (-1, 70 // T + 1)] +
+            [(b, 0) for b in (2, B - 1) if own[b]], prefix_len=P - 3, seed=B + P + 1)
+
+
+@pytest.mark.parametrize("P", [0, 1, 63, 64, 1000, 2999, 3000, 9999])
+def test_length_of_a_prefix_for_all_together(P):
+    run(BF16, 17, 8, 1, 1, 128, 16, [11 * i for i in range(17)], prefix=3000, prefix_len=P, seed=P)
+
+
+@pytest.mark.parametrize("B,most,prefix", [(65, 1500, 0), (70, 900, 300), (70, 900, 3000), (130, 1000, 0), (200, 700, 0), (1030, 40, 260)])
 def test_large_batches(B, most, prefix):
     """Chunks are found by a sum over the batch."""
     own = [(37 * b * b + 11 * b) % most if b % 5 else 0 for b in range(B)]
@@ -254,7 +286,7 @@ def test_pages_past_32_bit_offsets():
 def test_another_stream_and_graphs_that_share_a_workspace():
     """Two captured calls with one workspace, replayed in turn with other lengths in place."""
     import paper_2604_16429_amd as M
-    h, kv, D, T, B, prefix = 8, 2, 128, 16, 6, 1500
+    h, kv, D, T, B, prefix = 8, 2, 128, 16, 6, 5000
     k, v, table, prefix_table = cache_on_the_gpu(B, kv, T, D, 900, prefix)
     gen = torch.Generator(device="cuda").manual_seed(5)
     p = [M.PagedParams(B, h, n, D, k.shape[0], T, table.shape[1], kv_heads=kv, prefix_tokens=prefix)
@@ -284,7 +316,7 @@ def test_another_stream_and_graphs_that_share_a_workspace():
     other = torch.empty_like(ws)
     for turn in range(4):
         lens.copy_(torch.randint(40, 900, (B,), generator=gen, device="cuda", dtype=torch.int32))
-        plen.fill_((1500, 7, 0, 1499)[turn])
+        plen.fill_((5000, 7, 0, 4999)[turn])
         for i in (0, 1) if turn % 2 else (1, 0):
             out[i].fill_(float("nan"))
             graphs[i].replay()

@@ -48,7 +48,7 @@ extern "C" int64_t plan_of(const int32_t* shape, const int32_t* lens, int32_t* o
     s.prefix_tokens = shape[5];
     s.left = shape[6];
     s.sinks = shape[7];
-    const Plan p = make_plan(s, shape[10], Kind{shape[8], shape[11], shape[9], 128 * shape[9]});
+    const Plan p = make_plan(s, shape[10], Kind{shape[8], shape[11], shape[9], 128 * shape[9], 4 * shape[10]});
     const int32_t v[] = {p.chunks, p.scanned, p.stacked, p.shared_splits, p.parts, p.entries, p.all_rows, p.tile_rows,
                          p.tile, p.row_tiles};
     for (int i = 0; i < 10; ++i) out[i] = v[i];
