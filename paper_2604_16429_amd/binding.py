@@ -414,16 +414,22 @@ def _ptr(t):
     return t.data_ptr()
 
 
+def _raw():
+    """Functions for a device's current stream and for the current device."""
+    global _raw_stream
+    if _raw_stream is None:
+        import torch
+        torch.cuda.current_device()                   # (initialises the device on first use)
+        _raw_stream = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+    return _raw_stream
+
+
 def _stream(stream):
     if stream is None:
         # the handle of torch.cuda.current_stream() without its Stream object, which
         # took 3.1 us of a call (a forward with its one launch 8.5 us, without 5.6)
-        global _raw_stream
-        if _raw_stream is None:
-            import torch
-            torch.cuda.current_device()               # (initialises the device on first use)
-            _raw_stream = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
-        return _raw_stream[0](_raw_stream[1]())
+        of_device, device = _raw_stream or _raw()
+        return of_device(device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -658,11 +664,14 @@ def _vector_on(device, name, t, size, dtype):
 
 
 def _stream_on(device, stream):
-    """_stream, which has to belong to the tensors' GPU."""
+    """_stream, which has to belong to the tensors' GPU (a handle of 0 to the current one; of other handles
+    that is not known)."""
     handle = _stream(stream)
     if device is not None:
-        there = (_raw_stream[1]() if stream is None else
-                 device if isinstance(stream, int) else stream.device_index)
+        if not isinstance(stream, int):
+            there = _raw_stream[1]() if stream is None else stream.device_index
+        else:
+            there = device if stream else (_raw_stream or _raw())[1]()
         if there != device:
             raise ValueError(f"tensors on cuda:{device}, stream on cuda:{there}")
     return handle

@@ -206,8 +206,11 @@ def test_tensors_of_two_gpus(monkeypatch, call, make):
     rot = M.Rotation(64)
     monkeypatch.setattr(binding, "_lib", lib)
     extra = {"rot": rot} if call is append else {}
-    call(p, **extra, **make(1))
-    call(p, **extra, **make(0))
+    for device in (1, 0):
+        monkeypatch.setattr(binding, "_raw_stream", (lambda device: 0, lambda: device))
+        call(p, **extra, **make(device))
+        with pytest.raises(ValueError):
+            call(p, **extra, **make(1 - device))           # (stream 0 is the current GPU's)
     assert lib.calls == 2
     for name in make(0):
         with pytest.raises(ValueError):
