@@ -126,7 +126,7 @@ class Server:
 
 class MemberServer:
     """Members that go on from one common beginning, which is read and kept once: pages of a pool, those
-    of the beginning in `prefix_table`, each member's own in its row of `table`."""
+    of the beginning in `prefix_table`, each member's own, for `own` tokens, in its row of `table`."""
 
     def __init__(self, layer, members, shared, own, page=64):
         self.layer, self.members, self.shared, self.page = layer, members, shared, page
@@ -167,7 +167,8 @@ class MemberServer:
         return self._run(p, x.unsqueeze(0), lengths, self.prefix_table.view(1, -1), None, ws)[0]
 
     def step(self, x):
-        """x [members, width] -> y [members, width]."""
+        """x [members, width] -> y [members, width]; up to `own` times (a captured step counts on the GPU, so
+        that the host cannot refuse one more, which would take the place of the last)."""
         self.length += 1
         return self._run(self.steps, x.unsqueeze(1), self.length, self.table, self.prefix_table, self.ws)[:, 0]
 
