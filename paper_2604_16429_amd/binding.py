@@ -648,9 +648,14 @@ def mosaic_bsa_window_bwd(params: WindowParams, q, k, v, out, lse, dout, dq, dk,
 # ---- a cache in pages: k_pages and v_pages of shape [pages, kv_heads, page_tokens, head_dim] with any
 # strides of the first three dimensions
 
-def _device_of(t):
-    """The GPU of a call's first tensor; None for an address."""
-    return None if t is None or isinstance(t, int) else t.get_device()
+def _device_of(name, t):
+    """The GPU of a tensor; None for an address."""
+    if t is None or isinstance(t, int):
+        return None
+    device = t.get_device()
+    if device < 0:
+        raise ValueError(f"{name}: on {t.device} instead of a GPU")
+    return device
 
 
 def _vector_on(device, name, t, size, dtype):
@@ -681,7 +686,7 @@ def mosaic_bsa_paged_append(params: PagedParams, rotation: Rotation, positions, 
                             k_weight, q_lens, k_lens, page_table, prefix_len, q_out, k_pages, v_pages,
                             stream=None) -> None:
     h, kv, n, d = params.heads, params.kv_heads or params.heads, params.q_tokens, params.head_dim
-    b, t, on = params.batch, params.page_tokens, _device_of(q)
+    b, t, on = params.batch, params.page_tokens, _device_of("q", q)
     i32, f32 = _named_dtype("int32"), _named_dtype("float32")
     pos, per = params._positions_of(rotation, positions, n)
     if pos is not positions and on is not None and positions.get_device() != on:
@@ -706,10 +711,10 @@ def mosaic_bsa_paged_fwd(params: PagedParams, q, k_pages, v_pages, q_lens, k_len
                          prefix_table, prefix_len, out, lse=None, workspace=None, stream=None,
                          workspace_bytes=None) -> None:
     h, kv, n, b = params.heads, params.kv_heads or params.heads, params.q_tokens, params.batch
-    t, on = params.page_tokens, _device_of(q)
+    t, on = params.page_tokens, _device_of("q", q)
     i32, f32 = _named_dtype("int32"), _named_dtype("float32")
     wb = _nbytes(workspace) if workspace_bytes is None else workspace_bytes
-    if on is not None and _device_of(workspace) not in (None, on):
+    if _device_of("workspace", workspace) not in (None, on) and on is not None:
         raise ValueError("workspace: on another device than the tensors")
     _, ref, (q, k_pages, v_pages, out) = params._call(
         "fwd", ("q", q, h, n), ("k_pages", k_pages, kv, t), ("v_pages", v_pages, kv, t),

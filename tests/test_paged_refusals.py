@@ -239,3 +239,37 @@ def test_copies_of_parameters(copied):
     assert c == p and M.mosaic_bsa_paged_workspace_bytes(c) == n
     c.batch = 1
     assert p.batch == 2
+
+
+@pytest.mark.parametrize("call,make", [(attend, tensors), (append, append_tensors)], ids=["attend", "append"])
+@pytest.mark.parametrize("stream", [0, 12345], ids=["default", "handle"])
+def test_tensors_on_the_cpu_after_a_call_on_a_gpu(monkeypatch, call, make, stream):
+    """A device of -1 is no GPU, whatever the call before with the same shapes had."""
+    lib, p, rot = Library(), params(), M.Rotation(64)
+    monkeypatch.setattr(binding, "_lib", lib)
+    monkeypatch.setattr(binding, "_raw_stream", (lambda device: 0, lambda: 0))
+
+    def go(t):
+        if call is attend:
+            M.mosaic_bsa_paged_fwd(p, *t.values(), stream=stream)
+        else:
+            order = ("q", "k", "v", "q_weight", "k_weight", "q_lens", "k_lens", "page_table", "prefix_len", "q_out",
+                     "k_pages", "v_pages")
+            M.mosaic_bsa_paged_append(p, rot, None, *(t[n] for n in order), stream=stream)
+
+    go(make(0))
+    assert lib.calls == 1
+    with pytest.raises(ValueError):
+        go(make(-1))
+    for name in make(0):
+        with pytest.raises(ValueError):
+            go({**make(0), name: make(-1)[name]})
+    assert lib.calls == 1
+
+
+def test_a_workspace_on_the_cpu_beside_addresses(monkeypatch):
+    lib = Library()
+    monkeypatch.setattr(binding, "_lib", lib)
+    with pytest.raises(ValueError):
+        attend(params(), workspace=torch.zeros(1 << 10, dtype=torch.uint8))
+    assert lib.calls == 0
