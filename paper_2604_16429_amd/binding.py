@@ -668,6 +668,14 @@ def _vector_on(device, name, t, size, dtype):
     return t.data_ptr()
 
 
+def _table_on(device, t, params):
+    """_vector_on for a page table, [batch, table_pages] or flat."""
+    wanted = (params.batch, params.table_pages)
+    if t is not None and not isinstance(t, int) and t.shape != wanted and len(t.shape) != 1:
+        raise ValueError(f"page_table: shape {tuple(t.shape)} instead of {wanted}")
+    return _vector_on(device, "page_table", t, wanted[0] * wanted[1], _named_dtype("int32"))
+
+
 def _stream_on(device, stream):
     """_stream, which has to belong to the tensors' GPU (a handle of 0 to the current one; of other handles
     that is not known)."""
@@ -698,7 +706,7 @@ def mosaic_bsa_paged_append(params: PagedParams, rotation: Rotation, positions, 
         ref, rotation.ref, pos, q, k, v, _vector_on(on, "q_weight", q_weight, d, f32),
         _vector_on(on, "k_weight", k_weight, d, f32), _vector_on(on, "q_lens", q_lens, b, i32),
         _vector_on(on, "k_lens", k_lens, b, i32),
-        _vector_on(on, "page_table", page_table, b * params.table_pages, i32),
+        _table_on(on, page_table, params),
         _vector_on(on, "prefix_len", prefix_len, 1, i32), q_out, k_pages, v_pages,
         _stream_on(on, stream)))
 
@@ -724,7 +732,7 @@ def mosaic_bsa_paged_fwd(params: PagedParams, q, k_pages, v_pages, q_lens, k_len
     _check(load_library().mosaic_bsa_paged_fwd(
         ref, q, k_pages, v_pages, _vector_on(on, "q_lens", q_lens, b, i32),
         _vector_on(on, "k_lens", k_lens, b, i32),
-        _vector_on(on, "page_table", page_table, b * params.table_pages, i32),
+        _table_on(on, page_table, params),
         _vector_on(on, "prefix_table", prefix_table, -(-params.prefix_tokens // max(t, 1)), i32),
         _vector_on(on, "prefix_len", prefix_len, 1, i32), out,
         _vector_on(on, "lse", lse, b * h * n, f32), _ptr(workspace), wb, _stream_on(on, stream)))

@@ -273,3 +273,19 @@ def test_a_workspace_on_the_cpu_beside_addresses(monkeypatch):
     with pytest.raises(ValueError):
         attend(params(), workspace=torch.zeros(1 << 10, dtype=torch.uint8))
     assert lib.calls == 0
+
+
+@pytest.mark.parametrize("call,make", [(attend, tensors), (append, append_tensors)], ids=["attend", "append"])
+def test_page_tables_the_other_way_round(monkeypatch, call, make):
+    """As many entries in another order: [table_pages, batch]."""
+    lib, p = Library(), params()
+    extra = {"rot": M.Rotation(64)} if call is append else {}
+    monkeypatch.setattr(binding, "_lib", lib)
+    monkeypatch.setattr(binding, "_raw_stream", (lambda device: 0, lambda: 0))
+    for shape in ((4, 2), (1, 8), (2, 2, 2), (2, 4, 1)):
+        with pytest.raises(ValueError, match="page_table"):
+            call(p, **extra, **{**make(0), "page_table": OnGpu(0, *shape, dtype=torch.int32)})
+    assert lib.calls == 0
+    for shape in ((2, 4), (8,)):                           # (a flat one has one order only)
+        call(p, **extra, **{**make(0), "page_table": OnGpu(0, *shape, dtype=torch.int32)})
+    assert lib.calls == 2
