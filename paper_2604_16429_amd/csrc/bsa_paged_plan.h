@@ -195,7 +195,14 @@ inline Plan make_plan(const Shape& s, int D, const Kind& kind)
     // 15.0, on 8,000 (49 MB) 21 | 15; head dim 64, 16 on 2,000 (30 MB) 16.7 | 16.7, on 8,000 25 | 15; fp32, 6 on 1,501 (4 MB)
     // 12.0 | 14.6; 24 members on 28,800 72 | 29.
     const int64_t saved = (int64_t)(s.batch - 1) * s.prefix_tokens * s.kv_heads * kind.token_bytes;
-    p.stacked = s.prefix_tokens >= 256 && saved >= 24000000 && s.rows < 128 && s.left >= s.prefix_tokens + own;
+    // And where a sequence's reads of it are 12 times what one sum of each of its rows takes, out and in again, of which
+    // there are two at least, a share's and a chunk's.  us, bf16, apart | together.  Left apart: head dim 128, 128 sequences of
+    // 120 rows on 614 36 | 73, 1,003 on 777 143 | 286, 105 of 60 on 989 67 | 50; head dim 64, 288 of 96 on 1,966 53 | 44.
+    // Together: head dim 128, 448 of 20 on 639 26 | 33, 897 of 120 on 3,710 240 | 298; fp32, head dim 128, 531 of 64 on 1,916
+    // 2,582 | 1,723.  Of 820 drawn calls 82 took a quarter longer than the other way without this, 22 with it.
+    const bool long_enough = (int64_t)s.prefix_tokens * kind.token_bytes >= (int64_t)12 * 2 * 4 * D * s.rows;
+    p.stacked = s.prefix_tokens >= 256 && saved >= 24000000 && long_enough && s.rows < 128 &&
+                s.left >= s.prefix_tokens + own;
     // (few rows and tokens: one launch)
     if (!p.stacked && s.rows <= 16 && kind.waves > 4 && most_tokens(s, false) <= kind.few) {
         p.waves = kind.waves;

@@ -389,3 +389,20 @@ def test_inputs_that_share_memory(dtype, N):
         M.mosaic_bsa_paged_fwd(p, a[2], a[0], a[1], None, lens, table, prefix_table, None, out, workspace=ws)
         outs.append(out)
     assert torch.equal(*outs) and bool(outs[0].isfinite().all())
+
+
+@pytest.mark.parametrize("dtype,B,D,P", [(FP32, 16, 128, 3001), (FP32, 64, 32, 4101), (BF16, 64, 32, 4901)])
+def test_prefixes_for_all_together_beside_tiles_of_rows(dtype, B, D, P):
+    """Own tokens in tiles of 128 rows through registers, the prefix's in tiles of 32."""
+    run(dtype, B, 16, 8, 50, D, 32, [50 + b for b in range(B)], prefix=P, q_lens=[50 - b % 51 for b in range(B)], seed=B + D)
+
+
+@pytest.mark.parametrize("dtype,B,N,P", [(BF16, 128, 15, 614), (BF16, 64, 12, 256), (FP32, 40, 12, 300)])
+def test_short_prefixes_of_many_rows(dtype, B, N, P):
+    """Too short to be worked on for all together beside that many rows, though that would save reads."""
+    import paper_2604_16429_amd as M
+    from paper_2604_16429_amd import binding
+    p = M.PagedParams(B, 32, N, 128, 1000, 64, 1, binding.BF16 if dtype is BF16 else binding.F32, kv_heads=4, prefix_tokens=P)
+    assert M.mosaic_bsa_paged_workspace_bytes(p) == 0
+    run(dtype, B, 32, 4, N, 128, 64, [N + b % 40 for b in range(B)], prefix=P, q_lens=[N - b % (N + 1) for b in range(B)],
+        seed=B + P)

@@ -184,3 +184,33 @@ def test_pages_that_are_none(plan):
     got = [plan.page(8, 3, ptr, at, 50) for at in range(56)]
     want = [3] * 8 + [-1] * 8 + [7] * 8 + [-1] * 24 + [0] * 2 + [-1] * 6
     assert got == want
+
+
+def workspace(B, N, h, kv, D, P, own, page=64, dtype=1, left=-1):
+    import paper_2604_16429_amd as M
+    return M.mosaic_bsa_paged_workspace_bytes(M.PagedParams(
+        B, h, N, D, 1 << 20, page, -(-own // page), dtype, kv_heads=kv, prefix_tokens=P, window_left=left))
+
+
+@pytest.mark.parametrize("B", [64, 1024])
+def test_short_prefixes_of_many_rows_leave_no_sums(B):
+    """A prefix that stays in cache is cheaper to read again than 96 rows a sequence are to join."""
+    assert workspace(B, 12, 64, 8, 128, 256, 256) == 0
+    assert workspace(B, 12, 64, 8, 128, 20000, 256) > 0
+
+
+def test_workspaces_stay_small():
+    """Sums of chunks, twice 512 x 128 rows at most, of shares of a prefix, 512 x 128, and one of each for every row
+    where rows are more: those only beside 11 times as many bytes that would be read again."""
+    rng = random.Random(1)
+    seen = 0
+    for _ in range(20000):
+        B, N, kv, G = rng.choice([1, 8, 64, 300, 1024, 9000]), rng.choice([1, 1, 5, 12, 30, 60, 1000]), rng.choice([1, 2, 8]), \
+            rng.choice([1, 2, 4, 8, 16])
+        D, dtype = rng.choice([32, 64, 128]), rng.choice([0, 1])
+        P, own = rng.choice([0, 256, 400, 800, 1500, 4000, 30000, 200000]), rng.choice([64, 300, 1000, 5000, 30000])
+        n = workspace(B, N, kv * G, kv, D, P, own, dtype=dtype)
+        again = B * P * kv * 2 * D * (2 if dtype else 4)
+        assert n <= 110e6 + again / 11, (B, N, kv, G, D, dtype, P, own)
+        seen += n > 110e6
+    assert seen > 20
