@@ -233,12 +233,7 @@ inline Plan make_plan(const Shape& s, int D, const Kind& kind)
     if (p.entries <= kMostScanned && p.entries * units < 1 << 30 && (int64_t)p.entries * s.kv_heads < held &&
         tokens >= 384) {
         int64_t n = (held - shared_items) / s.kv_heads;
-        if (n < 2 * (int64_t)p.entries) {
-            // (own tokens of a quarter of a share, behind the shares, are over soon enough: 128 members on 131,072,
-            // 500 each 156 us, split 158; 2,000 each 204, split 191)
-            const bool over = p.stacked && 4 * tokens <= s.prefix_tokens / p.shared_splits;
-            n = over ? p.entries : 2 * (int64_t)p.entries;
-        }
+        if (n < 2 * (int64_t)p.entries) n = 2 * (int64_t)p.entries;
         const int64_t most = p.entries * ((units + kLeast - 1) / kLeast);
         p.chunks = (int)(n < most ? n : most);
     }
