@@ -160,7 +160,8 @@ class MemberServer:
         return (out.view(B * N, -1) @ lay.w_out.t()).view(B, N, -1)
 
     def begin(self, x):
-        """x [shared, width], the common beginning -> y [shared, width]."""
+        """x [shared, width], the common beginning -> y [shared, width].  Members have nothing of their own yet."""
+        self.length.zero_()
         p = self._params(1, self.shared, self.prefix_table.numel(), 0)
         lengths = torch.full((1,), self.shared, dtype=torch.int32, device="cuda")
         ws = _space(bsa.mosaic_bsa_paged_workspace_bytes(p))

@@ -43,3 +43,20 @@ def test_captured_steps_of_members():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, want[t]), t
+
+
+def test_a_second_beginning():
+    """What members read after one beginning is forgotten at the next."""
+    from examples.local_layer import LocalLayer, MemberServer
+    layer = LocalLayer(128, 4, 2, 64, 1 << 20, 0)
+    gen = torch.Generator().manual_seed(5)
+    starts = torch.randn(2, 300, 128, generator=gen).to(torch.bfloat16).cuda()
+    x = torch.randn(6, 10, 128, generator=gen).to(torch.bfloat16).cuda()
+    once, twice = MemberServer(layer, 6, 300, 10), MemberServer(layer, 6, 300, 10)
+    twice.begin(starts[0])
+    for t in range(7):
+        twice.step(x[:, t])
+    for server in (once, twice):
+        server.begin(starts[1])
+    for t in range(10):
+        assert torch.equal(twice.step(x[:, t]), once.step(x[:, t])), t
