@@ -406,3 +406,77 @@ def test_short_prefixes_of_many_rows(dtype, B, N, P):
     assert M.mosaic_bsa_paged_workspace_bytes(p) == 0
     run(dtype, B, 32, 4, N, 128, 64, [N + b % 40 for b in range(B)], prefix=P, q_lens=[N - b % (N + 1) for b in range(B)],
         seed=B + P)
+
+
+@pytest.mark.parametrize("N,own,prefix", [(50, 900, 0), (10, 300, 14000), (10, 900, 14000)])
+def test_token_strides_past_32_bits_with_a_workspace(N, own, prefix):
+    """Rows 2^24 elements apart, where tokens are split, the prefix is worked on for all together, or both: the
+    kernels for any stride leave other sums in the workspace, whose size is asked for without strides."""
+    import paper_2604_16429_amd as M
+    T, kv, D, B, h = 8, 1, 64, 8, 4
+    each, shared = -(-own // T), prefix // T
+    pages = shared + B * each
+    gen = torch.Generator(device="cuda").manual_seed(12)
+    near = [torch.randn(pages, kv, T, D, generator=gen, device="cuda").to(BF16) for _ in range(2)]
+    far = [torch.zeros(T << 24, dtype=BF16, device="cuda").as_strided((pages, kv, T, D), (D, 0, 1 << 24, 1))
+           for _ in range(2)]
+    for a, b in zip(far, near):
+        a.copy_(b)
+    ids = torch.randperm(pages, generator=gen, device="cuda").to(torch.int32)
+    q = torch.randn(B, h, N, D, generator=gen, device="cuda").to(BF16)
+    p = M.PagedParams(B, h, N, D, pages, T, each, kv_heads=kv, prefix_tokens=prefix)
+    lens = torch.tensor([own - 31 * b for b in range(B)], dtype=torch.int32, device="cuda")
+    n = M.mosaic_bsa_paged_workspace_bytes(p)
+    assert n > 0
+    outs = []
+    for k, v in (far, near):
+        ws = torch.full((n + 4096,), 0xff, dtype=torch.uint8, device="cuda")
+        out = torch.empty_like(q)
+        M.mosaic_bsa_paged_fwd(p, q, k, v, None, lens, ids[shared:].contiguous().view(B, each), ids[:shared].contiguous(),
+                               None, out, workspace=ws, workspace_bytes=n)
+        assert bool((ws[n:] == 0xff).all())
+        outs.append(out.float())
+    # each within its roundings of the definition: weights and result, a half step each
+    assert float((outs[0] - outs[1]).abs().max()) <= 2 * 2 * 2.0 ** -8 * float(near[1].abs().max())
+
+
+@pytest.mark.parametrize("named", [True, False], ids=["given", "current"])
+def test_calls_wait_for_their_stream(named):
+    """Inputs that work queued on the same stream has yet to make."""
+    import paper_2604_16429_amd as M
+    B, h, kv, D, T, prefix, own = 3, 4, 2, 64, 16, 40, 100
+    k0, v0, table, prefix_table = cache_on_the_gpu(B, kv, T, D, own, prefix)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    new = [torch.randn(B, n, 1, D, device="cuda", generator=gen).to(BF16) for n in (h, kv, kv)]
+    p, rot = M.PagedParams(B, h, 1, D, k0.shape[0], T, table.shape[1], kv_heads=kv, prefix_tokens=prefix), M.Rotation(D)
+    lens = torch.full((B,), own, dtype=torch.int32, device="cuda")
+    ws = torch.empty(max(M.mosaic_bsa_paged_workspace_bytes(p), 256), dtype=torch.uint8, device="cuda")
+    busy = torch.randn(8192, 8192, device="cuda").to(BF16)
+
+    def serve(late, stream):
+        k, v = k0.clone(), v0.clone()
+        inputs = [torch.zeros_like(x) for x in new]
+        turned, out = torch.zeros_like(new[0]), torch.zeros_like(new[0])
+        torch.cuda.synchronize()
+        with torch.cuda.stream(late):
+            for _ in range(20):
+                torch.mm(busy, busy)
+            for x, y in zip(inputs, new):
+                x.copy_(y)
+
+        def calls():
+            M.mosaic_bsa_paged_append(p, rot, None, *inputs, None, None, None, lens, table, None, turned, k, v, stream=stream)
+            M.mosaic_bsa_paged_fwd(p, turned, k, v, None, lens, table, prefix_table, None, out, workspace=ws, stream=stream)
+
+        if stream is None:
+            with torch.cuda.stream(late):
+                calls()
+        else:
+            calls()
+        torch.cuda.synchronize()
+        return turned, k, v, out
+
+    want = serve(torch.cuda.current_stream(), None)
+    side = torch.cuda.Stream()
+    got = serve(side, side if named else None)
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and bool(want[3].count_nonzero() > 0)

@@ -289,3 +289,13 @@ def test_page_tables_the_other_way_round(monkeypatch, call, make):
     for shape in ((2, 4), (8,)):                           # (a flat one has one order only)
         call(p, **extra, **{**make(0), "page_table": OnGpu(0, *shape, dtype=torch.int32)})
     assert lib.calls == 2
+
+
+@pytest.mark.parametrize("kw", [dict(batch=24, heads=16, q_tokens=1, head_dim=128, table_pages=100, prefix_tokens=28800),
+                                dict(batch=2, heads=4, q_tokens=50, table_pages=60, prefix_tokens=0)], ids=["shares", "chunks"])
+def test_workspaces_that_are_needed(kw):
+    p = params(**kw)
+    n = M.mosaic_bsa_paged_workspace_bytes(p)
+    assert n > 0
+    for short in (dict(nbytes=n - 1), dict(nbytes=0), dict(workspace=None), dict(workspace=None, nbytes=0)):
+        assert code_of(lambda: attend(p, **short)) == -6
