@@ -94,7 +94,8 @@ struct Tiles {
 // the entries.
 constexpr int kUnit = 128, kLeast = 2;     // c is kLeast at least
 constexpr int kMostScanned = 256;          // entries; more have a chunk each (400 sequences of up to 2,000, 2 heads:
-                                           // 106 us, looked up 118; 130 of up to 4,000, 4 heads: 88, looked up 77)
+                                           // 106 us, looked up 118; 130 of up to 4,000, 4 heads: 88, looked up 77).  That
+                                           // costs long ones: 256 of up to 4,000, one head, 69 us, 257 83; up to 16,000 233, 360
 struct Entry {
     int32_t first, chunks;
 };
@@ -208,10 +209,15 @@ inline Plan make_plan(const Shape& s, int D, const Kind& kind)
         p.waves = kind.waves;
         return p;
     }
-    // Workgroups that the chip holds at once: chunks and shares are as many as fill it once, of at least 256
-    // tokens, 384 where a share's sums are those of 128 rows.  us: 24 members on 28,800, shares of 256 39, 384
+    // Tiles of 128 rows: chunks and shares are as many as the chip holds in bf16 at head dims 64 and 128, shares of at
+    // least 256 tokens, 384 where a share's sums are those of 128 rows.  us: 24 members on 28,800, shares of 256 39, 384
     // 33, 768 43; 4 x 5 tokens on 4,000, of 192 18, 384 24; 8 chunks of up to 100 tokens on 14,000, 512 chunks
     // 112, 768 100.
+    // Smaller tiles: 1,024 chunks of 16 rows, 512 of 32, though the chip holds 256 to 1,280 by type and head dim: lengths
+    // differ, and a second round of small chunks evens them out.  us with 256, 512, 768, 1,024, 1,280: 4 rows, 64
+    // sequences of 4,000 to 16,000, 4 key/value heads, bf16, head dim 128, 256, 245, 248, 227, 229, 64 182, 126, 125, 127,
+    // 124, 32 147, 86, 72, 68, 69; fp32, head dim 128, 735, 598, 558, 532, 538.  20 rows, 32 sequences, bf16, head dim 128, 153,
+    // 141, 147, 148, 150, 64 95, 64, 66, 70, 69; fp32, head dim 64, 208, 142, 169, 148, 162, 128 442, 389, 376, 395, 388.
     const int64_t wide_held = D == 64 ? 768 : 512;
     int64_t shared_items = 0;
     if (p.stacked) {
